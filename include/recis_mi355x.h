@@ -12,8 +12,10 @@
  * and their state in place — "Backward Update", "Optimizer", "Scatter").
  * Beside the step: the sequence tile (a bag's rows concatenated, keeping its
  * first or last ids), row-wise optimizer state, eviction of stale keys, the
- * ids partition (dedup + split by owner shard) and the bucketize / mod
- * feature transforms fused over columns.
+ * ids partition (dedup + split by owner shard), the bucketize / mod
+ * feature transforms fused over columns, and the sequence operators that
+ * follow the step in a model: layer norm and attention over ragged sequences,
+ * each with its backward.
  *
  * Conventions shared by every entry point
  *  - All array arguments are DEVICE pointers owned by the caller, unless a
@@ -415,6 +417,43 @@ rs_status fused_bucketize(const float* values, int64_t n, const int64_t* col_off
                           rs_stream stream);
 rs_status fused_mod(const int64_t* values, int64_t n, const int64_t* col_offsets, int32_t ncols,
                     const int64_t* moduli, int64_t* out, int32_t validate, rs_stream stream);
+
+/* Layer norm over the last axis of [rows, dim] (a sequence model's first step
+ * on the rows the embedding step hands it: pooled rows, packed sequence rows
+ * or the padded copy).
+ *   mean = sum x / dim,  rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps)
+ *   xhat = (x - mean) * rstd,  y = xhat * weight + bias
+ * x, y: `dtype` (rs_dtype), row r at element r * stride (stride >= dim, any
+ * alignment of the element; 16-byte aligned rows of a multiple of 16 bytes are
+ * fastest).  weight, bias [dim]: `param_dtype`; NULL = 1 and 0.  mask uint8
+ * [rows] (NULL: every row), as the padded copy's: rows of mask 0 are never
+ * read (they may hold anything) and their y is 0.  mean, rstd fp32 [rows]: the
+ * statistics the backward takes (0 for masked rows); NULL where there is no
+ * backward.  rows < 2^31, 1 <= dim <= 2^24, 0 <= eps (0 gives NaN for a
+ * constant row).  Arithmetic in fp32, one rounding at the end.  Inputs and
+ * outputs must not overlap.  Errors: RS_EINVAL (sizes, strides, types, null
+ * pointers), RS_EHIP. */
+rs_status layer_norm_fwd(const void* x, int64_t rows, int64_t dim, int64_t x_stride, int32_t dtype,
+                         const void* weight, const void* bias, int32_t param_dtype, double eps, const uint8_t* mask,
+                         void* y, int64_t y_stride, float* mean, float* rstd, rs_stream stream);
+
+/* Backward of layer_norm_fwd for the output gradient dy, from x and the
+ * forward's mean and rstd:
+ *   g = dy * weight,  dx = rstd * (g - mean_dim(g) - xhat * mean_dim(g * xhat))
+ *   dweight = sum over rows of dy * xhat,  dbias = sum over rows of dy
+ * dx in `dtype` (0 in masked rows; masked rows of dy and x are never read),
+ * dweight and dbias [dim] in `param_dtype`; each may be NULL (not wanted).
+ * The sums over rows are fp32, taken in an order fixed by the sizes, so
+ * repeated calls agree bit for bit.  workspace: device, 256-byte aligned, >=
+ * layer_norm_bwd_workspace_bytes(rows, dim) bytes (0 for sizes the call
+ * refuses), free for the next call once this one has completed in stream
+ * order; not needed when dweight and dbias are NULL.  Errors as the forward's,
+ * and RS_EINVAL for a workspace missing or too small. */
+size_t layer_norm_bwd_workspace_bytes(int64_t rows, int64_t dim);
+rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64_t rows, int64_t dim,
+                         int64_t x_stride, int32_t dtype, const void* weight, int32_t param_dtype,
+                         const uint8_t* mask, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                         void* dweight, void* dbias, void* workspace, size_t workspace_bytes, rs_stream stream);
 
 /* Kernel timing hook: from now on, hipEvent_t `start` / `stop` time every
  * launch of the named kernel (NULL, NULL clears it).  For RS_K_POOL,

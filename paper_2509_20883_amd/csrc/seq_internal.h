@@ -1,0 +1,44 @@
+// Declarations shared by the sequence operators' kernels (layer norm and
+// attention over ragged sequences) and their C ABI entry points.
+#pragma once
+
+#include "rs_internal.h"
+
+namespace rs {
+
+// ---------------------------------------------------------------------------
+// layer norm
+// ---------------------------------------------------------------------------
+
+// Strides are in elements; weight, bias and their gradients are bf16 where
+// param_bf16 is set, else fp32.  Null pointers: weight 1, bias 0, no mask, no
+// statistics wanted, a gradient not wanted.
+struct NormArgs {
+  int64_t rows, dim;
+  float eps;
+  bool param_bf16;
+  const void* x;
+  int64_t x_stride;
+  const void *weight, *bias;
+  const uint8_t* mask;
+  // forward
+  void* y;
+  int64_t y_stride;
+  float *mean_out, *rstd_out;
+  // backward
+  const void* dy;
+  int64_t dy_stride;
+  const float *mean, *rstd;
+  void* dx;
+  int64_t dx_stride;
+  void *dweight, *dbias;
+  float* part;  // [nparts][2 dim] partial column sums
+  int nparts;
+};
+
+// Partial sums of dw and db: the rows of each are added by one block.
+int norm_parts(int64_t rows, int64_t dim);
+hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t s);
+
+}  // namespace rs

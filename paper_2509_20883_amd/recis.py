@@ -6,7 +6,7 @@ fallback: if the library is not built, or no GPU is present, calls raise.
 
 Names follow the C ABI (include/recis_mi355x.h): ht_create, ht_find_or_insert,
 lookup_pool_fwd, lookup_pool_bwd, sparse_opt_step, lookup_pool_bwd_opt,
-ids_partition, fused_bucketize, fused_mod.
+ids_partition, fused_bucketize, fused_mod, layer_norm_fwd, layer_norm_bwd.
 """
 from __future__ import annotations
 
@@ -139,6 +139,9 @@ def lib() -> C.CDLL:
         "fused_mod": (C.c_int, [p, i64, p, i32, p, p, i32, p]),
         "rs_bandwidth_probe": (C.c_int, [i32, p, i64, p, i64, p, i64, i32, p]),
         "ids_partition_static": (C.c_int, [p, i64, i32, C.c_uint64, p, p, p, p, p]),
+        "layer_norm_fwd": (C.c_int, [p, i64, i64, i64, i32, p, p, i32, C.c_double, p, p, i64, p, p, p]),
+        "layer_norm_bwd_workspace_bytes": (C.c_size_t, [i64, i64]),
+        "layer_norm_bwd": (C.c_int, [p, i64, p, i64, i64, i64, i32, p, i32, p, p, p, p, i64, p, p, p, C.c_size_t, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -303,6 +306,123 @@ def fused_mod(values: torch.Tensor, col_offsets: torch.Tensor, moduli: torch.Ten
     _check(lib().fused_mod(_ptr(v), v.numel(), _ptr(co), co.numel() - 1, _ptr(m), _ptr(out), int(validate),
                            _stream()))
     return out
+
+
+_SEQ_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _seq_type(t: torch.Tensor, what: str) -> int:
+    """rs_dtype of a GPU tensor of a sequence operator."""
+    if not t.is_cuda:
+        raise RecisError(EINVAL, "tensors must be on the GPU")
+    dt = _SEQ_TYPES.get(t.dtype)
+    if dt is None:
+        raise RecisError(EINVAL, f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return dt
+
+
+def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """The tensor as equally spaced rows of its last axis, and their stride in
+    elements (a copy is made where its strides do not allow that)."""
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t, t.stride(0)
+    if not t.is_contiguous():
+        t = t.contiguous()
+    return t, t.shape[-1]
+
+
+def _bytes(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
+    """The workspace, replaced if it is too small or on another device.  One
+    that other streams may still read goes back to the caching allocator,
+    which holds a block for the stream it was allocated on."""
+    if ws is None or ws.numel() < need or ws.device != like.device:
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+    return ws
+
+
+class LayerNorm:
+    """Layer norm over the last axis, with a reusable backward workspace.
+
+    ``forward(x, weight, bias, mask)`` returns (y, mean, rstd); ``backward``
+    takes the output gradient, x and those statistics and returns (dx,
+    dweight, dbias).  x: float32 or bfloat16 [..., dim]; weight, bias [dim] in
+    either type or None (1 and 0); mask: uint8 or bool [...], rows of mask 0
+    are never read and give y = dx = 0.  Calls of one object share its
+    workspace: issue them on one stream, or order the streams.
+    """
+
+    def __init__(self, eps: float = 1e-5):
+        self.eps = float(eps)
+        self.ws: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def _params(x, weight, bias):
+        pt = None
+        for t, what in ((weight, "weight"), (bias, "bias")):
+            if t is None:
+                continue
+            dt = _seq_type(t, what)
+            if pt is not None and dt != pt:
+                raise RecisError(EINVAL, "weight and bias must have one type")
+            if t.dim() != 1 or t.shape[0] != x.shape[-1] or not t.is_contiguous():
+                raise RecisError(EINVAL, f"{what} must be a contiguous [{x.shape[-1]}] tensor")
+            pt = dt
+        return F32 if pt is None else pt
+
+    @staticmethod
+    def _mask(x, mask):
+        if mask is None:
+            return None
+        if not mask.is_cuda or mask.dtype not in (torch.uint8, torch.bool):
+            raise RecisError(EINVAL, "mask must be a uint8 or bool GPU tensor")
+        if mask.numel() * x.shape[-1] != x.numel():
+            raise RecisError(EINVAL, "mask must have one element per row of x")
+        return mask.contiguous()
+
+    def forward(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None):
+        dt = _seq_type(x, "x")
+        if x.dim() < 1 or x.shape[-1] < 1:
+            raise RecisError(EINVAL, "x needs a last axis of at least one element")
+        pt = self._params(x, weight, bias)
+        m = self._mask(x, mask)
+        dim = x.shape[-1]
+        rows = x.numel() // dim
+        xr, xs = _rows(x)
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif out.shape != x.shape or out.dtype != x.dtype or not out.is_cuda or not out.is_contiguous():
+            raise RecisError(EINVAL, "out must be a contiguous GPU tensor of x's shape and type")
+        stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean, rstd = stats.unbind(0)
+        _check(lib().layer_norm_fwd(xr.data_ptr(), rows, dim, xs, dt, _ptr(weight), _ptr(bias), pt, self.eps, _ptr(m),
+                                    out.data_ptr(), dim, mean.data_ptr(), rstd.data_ptr(), _stream()))
+        return out, mean, rstd
+
+    def backward(self, grad_out: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                 weight: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None):
+        dt = _seq_type(x, "x")
+        if x.dim() < 1 or x.shape[-1] < 1:
+            raise RecisError(EINVAL, "x needs a last axis of at least one element")
+        if grad_out.shape != x.shape or grad_out.dtype != x.dtype or not grad_out.is_cuda:
+            raise RecisError(EINVAL, "grad_out must be a GPU tensor of x's shape and type")
+        pt = self._params(x, weight, None)
+        m = self._mask(x, mask)
+        dim = x.shape[-1]
+        rows = x.numel() // dim
+        mean, rstd = _dev(mean, torch.float32), _dev(rstd, torch.float32)
+        if mean.numel() != rows or rstd.numel() != rows:
+            raise RecisError(EINVAL, "mean and rstd must have one element per row of x")
+        xr, xs = _rows(x)
+        gr, gs = _rows(grad_out)
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dp = torch.empty((2, dim), dtype=torch.bfloat16 if pt == BF16 else torch.float32, device=x.device)
+        dw, db = dp.unbind(0)
+        self.ws = _bytes(self.ws, lib().layer_norm_bwd_workspace_bytes(rows, dim), x)
+        _check(lib().layer_norm_bwd(gr.data_ptr(), gs, xr.data_ptr(), rows, dim, xs, dt, _ptr(weight), pt, _ptr(m),
+                                    mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dim, dw.data_ptr(),
+                                    db.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream()))
+        return dx, dw, db
 
 
 PROBES = {"read": 0, "write": 1, "copy": 2, "gather": 3, "rmw": 4}
