@@ -455,6 +455,79 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
                          const uint8_t* mask, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
                          void* dweight, void* dbias, void* workspace, size_t workspace_bytes, rs_stream stream);
 
+/* Attention over ragged sequences (behaviour sequences of packed rows with the
+ * batch's CSR offsets, or of the padded copy), with its backward.  Sequence s
+ * has Lq queries and Lk keys (the same offsets: self attention; others: a chunk
+ * of new rows, or single rows and candidates, over a longer history).  Query i
+ * stands at position p_i = i + Lk - Lq, query head h reads key head
+ * h / (heads_q / heads_kv), and
+ *   s_ij  = cap(scale * q_i.k_j) - slope_h * |p_i - j|,
+ *           cap(x) = softcap * tanh(x / softcap) (softcap 0: cap(x) = x)
+ *   out_i = sum_j exp(s_ij - lse_i) v_j,  lse_i = log sum_j exp(s_ij)
+ * over the keys j of its own sequence that query i sees: all of them (causal =
+ * 0), or j <= p_i or j < prefix_s (causal = 1; prefix NULL: none).  A query
+ * that sees no key gets out 0 and lse -infinity.
+ *
+ * Layout.  q [q_rows][heads_q][head_dim], k and v [kv_rows][heads_kv]
+ * [head_dim]: `dtype`, head_dim contiguous, element strides of a row and of a
+ * head given (so q, k and v may be column blocks of one projection); pointers
+ * and strides multiples of 16 bytes.  out and the gradients are contiguous.
+ * q_offsets, kv_offsets: device int64 [seqs + 1], CSR (off[0] = 0,
+ * nondecreasing).  q_pad = 0: packed, sequence s is rows off[s] .. off[s + 1];
+ * rows outside every sequence are neither read nor written.  q_pad > 0: padded,
+ * q_rows = seqs * q_pad, sequence s is the first min(off[s+1] - off[s], q_pad)
+ * rows from s * q_pad; the rows after them are never read (they may hold
+ * anything), and their out and gradients are 0 and their lse -infinity.  kv_pad
+ * the same for k and v.  A row of the sequence itself that is not finite may
+ * reach every query of the sequence, also those that do not see it.
+ *
+ * Scores, softmax statistics and sums are fp32; bf16 probabilities and score
+ * gradients are rounded to bf16 as operands of the matrix instructions. */
+typedef struct {
+  int32_t dtype;     /* rs_dtype of q, k, v, out and their gradients              */
+  int32_t heads_q;   /* a multiple of heads_kv                                    */
+  int32_t heads_kv;  /* 1 .. 1024                                                 */
+  int32_t head_dim;  /* a multiple of 8 in [8, 128]                               */
+  int32_t causal;
+  int32_t reserved;  /* 0 */
+  int64_t seqs, q_rows, kv_rows; /* q_rows * heads_q, kv_rows < 2^31              */
+  int64_t q_pad, kv_pad;         /* rows per sequence of a padded layout; 0: packed */
+  int64_t max_q;     /* the caller's bound of every Lq (0: none known); the launch
+                        shape goes by it, and a longer sequence's rows past it may
+                        be left out                                               */
+  int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+  double scale;      /* > 0                                                       */
+  double softcap;    /* >= 0                                                      */
+} rs_attn_desc;
+
+/* Workspace bytes of seq_attention_fwd (backward = 0) or seq_attention_bwd
+ * (backward = 1); 0 for a descriptor that the call refuses, or where none is
+ * needed.  256-byte aligned, free for the next call once this one has completed
+ * in stream order. */
+size_t seq_attention_workspace_bytes(const rs_attn_desc* d, int32_t backward);
+
+/* out [q_rows][heads_q][head_dim], and for a backward (else NULL) lse fp32
+ * [q_rows][heads_q] and, in bf16, rest of out's shape: what rounding took from
+ * out, in bf16.  prefix: device int64 [seqs] or NULL; slopes: device
+ * fp32 [heads_q] or NULL (0).  validate != 0 checks the offsets on the host
+ * (copies them back: synchronizing).  Errors: RS_EINVAL (sizes, alignment,
+ * null pointers, workspace, what validate rejects), RS_EHIP. */
+rs_status seq_attention_fwd(const rs_attn_desc* d, const void* q, const void* k, const void* v,
+                            const int64_t* q_offsets, const int64_t* kv_offsets, const int64_t* prefix,
+                            const float* slopes, void* out, void* rest, float* lse, void* workspace,
+                            size_t workspace_bytes, int32_t validate, rs_stream stream);
+
+/* Gradients of seq_attention_fwd for the output gradient grad_out (contiguous,
+ * out's shape and type), from its inputs, out, rest (NULL: taken as 0, which
+ * costs some accuracy of dq and dk; fp32 has none) and lse: dq, dk, dv contiguous in `dtype`, dslopes fp32 [heads_q] (NULL: not wanted; needs slopes).  dk and dv
+ * add up the query heads of their key head.  Every sum is taken in an order
+ * fixed by the sizes, so repeated calls agree bit for bit. */
+rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k, const void* v, const void* out,
+                            const void* rest, const float* lse, const void* grad_out, const int64_t* q_offsets,
+                            const int64_t* kv_offsets, const int64_t* prefix, const float* slopes, void* dq,
+                            void* dk, void* dv, float* dslopes, void* workspace, size_t workspace_bytes,
+                            int32_t validate, rs_stream stream);
+
 /* Kernel timing hook: from now on, hipEvent_t `start` / `stop` time every
  * launch of the named kernel (NULL, NULL clears it).  For RS_K_POOL,
  * RS_K_BWD_SHORT and RS_K_BWD_LONG the events are handed to the launch and

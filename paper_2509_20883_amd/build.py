@@ -8,7 +8,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librecis_mi355x.so")
 SOURCES = ["dedup_idmap.hip", "ids_partition.hip", "feature_ops.hip", "pool.hip", "backward.hip", "probes.hip", "ids_static.hip", "layer_norm.hip",
-           "seq_api.hip", "api.hip"]
+           "attn_fwd.hip", "attn_bwd.hip", "seq_api.hip", "api.hip"]
 # sources compiled once per part (-DRS_PART=k): a part is a code object of its
 # own, loaded when a process first launches one of its kernels
 PARTS = {"pool.hip": 4, "backward.hip": 5}

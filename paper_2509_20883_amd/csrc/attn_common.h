@@ -1,0 +1,289 @@
+// Device helpers of the attention kernels (gfx950): sequence geometry, the
+// LDS tile, and fragments of the 32x32 matrix instructions for both types.
+//
+// Fragments.  v_mfma_f32_32x32x16_bf16 takes from lane l (half h = l / 32)
+// eight consecutive k of row l % 32 of A (column l % 32 of B) and leaves in
+// register r of lane l the element of row (r / 4) * 8 + h * 4 + r % 4, column
+// l % 32.  fp32 uses v_mfma_f32_32x32x2_f32 eight times on the same eight
+// values per lane: step e multiplies the k that both operands hold in slot e,
+// so both types share one layout.
+//
+// The products are arranged so that a tile of probabilities never leaves its
+// registers: the first product is taken with the long axis (keys in the
+// forward, query rows in the gradient of k and v) along the rows, so a lane
+// holds one column and 16 of its 32 rows; registers 8 t .. 8 t + 7 are then
+// exactly slot 0 .. 7 of the next product's B operand, with slot e of half h
+// standing for row 16 t + (e / 4) * 8 + h * 4 + e % 4.  The A operand (v, k,
+// q or dout, transposed) is read from LDS in that order of its rows.
+#pragma once
+
+#include "device_common.h"
+#include "seq_internal.h"
+
+#pragma clang fp contract(fast)
+
+namespace rs {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kAttnWaves = 4;
+constexpr int kAttnRows = 32 * kAttnWaves;  // rows of a block's own tile: 32 per wave
+constexpr int kAttnStep = 64;               // rows of the tile it walks over, per step
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct f32x8s {
+  float v[8];
+};
+
+template <typename T>
+struct Frag;
+template <>
+struct Frag<uint16_t> {
+  typedef bf16x8 type;
+};
+template <>
+struct Frag<float> {
+  typedef f32x8s type;
+};
+
+__device__ inline f32x16 mma(const bf16x8& a, const bf16x8& b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mma(const f32x8s& a, const f32x8s& b, f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+  return c;
+}
+
+// Two floats to bf16 (round to nearest even), in one word.
+__device__ inline uint32_t pack_bf16(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+// Registers 8 t .. 8 t + 7 of a product as a B operand.  bf16: the
+// probabilities (or their gradients) are rounded to 8 bits of mantissa here,
+// once, as the matrix instruction takes them; their sum is kept in fp32.
+template <typename T>
+__device__ inline typename Frag<T>::type to_frag(const float (&p)[16], int t);
+template <>
+__device__ inline bf16x8 to_frag<uint16_t>(const float (&p)[16], int t) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = pack_bf16(p[8 * t + 2 * e], p[8 * t + 2 * e + 1]);
+  return __builtin_bit_cast(bf16x8, w);
+}
+template <>
+__device__ inline f32x8s to_frag<float>(const float (&p)[16], int t) {
+  f32x8s f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.v[e] = p[8 * t + e];
+  return f;
+}
+
+template <typename T>
+__device__ inline typename Frag<T>::type zero_frag();
+template <>
+__device__ inline bf16x8 zero_frag<uint16_t>() {
+  return bf16x8{};
+}
+template <>
+__device__ inline f32x8s zero_frag<float>() {
+  return f32x8s{};
+}
+
+// Eight consecutive elements of global memory (16-byte aligned).
+__device__ inline void load_frag(const uint16_t* p, bf16x8& f) { f = *reinterpret_cast<const bf16x8*>(p); }
+__device__ inline void load_frag(const float* p, f32x8s& f) { f = *reinterpret_cast<const f32x8s*>(__builtin_assume_aligned(p, 16)); }
+
+// A tile of rows of HD elements in LDS, in 16-byte chunks.  Chunk c of row r
+// lies at chunk c ^ key(r) of its row, with the key chosen so that both reads
+// spread over the 64 banks: 16 consecutive rows at one chunk (rows as an
+// operand), and 4 consecutive rows times 64 bytes (rows transposed).
+template <typename T, int HD>
+struct Tile {
+  static constexpr int kPer = 16 / sizeof(T);  // elements per chunk
+  static constexpr int kChunks = HD / kPer;    // chunks per row
+  static constexpr int kRowBytes = HD * sizeof(T);
+
+  __device__ static inline int key(int r) {
+    if (kChunks >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if (kChunks == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return (r >> 2) & 3;
+  }
+  // Byte address of chunk c of row r.
+  __device__ static inline int at(int r, int c) { return r * kRowBytes + ((c ^ key(r)) << 4); }
+};
+
+// Operand rows: elements k0 .. k0 + 7 (k0 = 16 t + 8 h) of row r.
+template <int HD>
+__device__ inline void row_frag(const char* tile, int r, int k0, bf16x8& f) {
+  f = *reinterpret_cast<const bf16x8*>(tile + Tile<uint16_t, HD>::at(r, k0 >> 3));
+}
+template <int HD>
+__device__ inline void row_frag(const char* tile, int r, int k0, f32x8s& f) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(tile + Tile<float, HD>::at(r, k0 >> 2));
+  const f32x4 b = *reinterpret_cast<const f32x4*>(tile + Tile<float, HD>::at(r, (k0 >> 2) + 1));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f.v[e] = a[e];
+    f.v[4 + e] = b[e];
+  }
+}
+
+// Transposed operand: for the 16 tile rows from r0, column c0 + l % 32, in the
+// slot order described above.  bf16: ds_read_b64_tr_b16, where 16 lanes read
+// four rows of 32 bytes (lane i the piece i % 4 of row i / 4) and lane i
+// receives column i of the four rows.
+template <int HD>
+__device__ inline void col_frag(const char* tile, int r0, int c0, int lane, bf16x8& f) {
+  const int r = r0 + (lane >> 5) * 4 + ((lane >> 2) & 3);
+  const int c = c0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const char* p0 = tile + Tile<uint16_t, HD>::at(r, c >> 3) + (c & 7) * 2;
+  const char* p1 = tile + Tile<uint16_t, HD>::at(r + 8, c >> 3) + (c & 7) * 2;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p0));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p1));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  f = __builtin_bit_cast(bf16x8, ab);
+}
+template <int HD>
+__device__ inline void col_frag(const char* tile, int r0, int c0, int lane, f32x8s& f) {
+  const int c = c0 + (lane & 31), h = lane >> 5;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int r = r0 + (e >> 2) * 8 + h * 4 + (e & 3);
+    f.v[e] = *reinterpret_cast<const float*>(tile + Tile<float, HD>::at(r, c >> 2) + (c & 3) * 4);
+  }
+}
+
+// The value of the lane's column in the other half of the wave.
+__device__ inline float other_half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float other_half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh.  bf16: 1 - 2 / (e^2x + 1) on the hardware's exp2 and reciprocal, off
+// by about 1e-7 whatever x; fp32 scores keep the relative accuracy near 0
+// that the library function has.
+template <typename T>
+__device__ inline float tanh_of(float x);
+template <>
+__device__ inline float tanh_of<uint16_t>(float x) {
+  return 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_hw(x * (2.0f * kLog2e)) + 1.0f);
+}
+template <>
+__device__ inline float tanh_of<float>(float x) {
+  return tanhf(x);
+}
+
+// First row and length of sequence s among `rows` rows: packed, rows
+// [off[s], off[s + 1]); padded, the first min(length, pad) rows of its block.
+// Offsets outside the tensor are cut to it, so no access leaves it.
+struct SeqSpan {
+  int64_t start;
+  int len;
+};
+__device__ inline SeqSpan seq_span(const int64_t* __restrict__ off, int s, int64_t pad, int64_t rows) {
+  const int64_t o = off[s];
+  int64_t len = off[s + 1] - o;
+  SeqSpan r;
+  if (pad > 0) {
+    r.start = s * pad;
+    len = min(len, pad);
+  } else {
+    r.start = min(max(o, int64_t(0)), rows);
+    len = min(len, rows - r.start);
+  }
+  r.len = static_cast<int>(max(len, int64_t(0)));
+  return r;
+}
+
+// Block numbers over ragged sequences without a table: sequence s owns the
+// numbers from off[s] * mul / per + s on.  They are enough for
+// ceil(len * mul / per) tiles (floor((o + n) / per) - floor(o / per) + 1 >=
+// ceil(n / per)), strictly increasing in s, and end below
+// off[seqs] * mul / per + seqs.  Returns the sequence of block b, found by the
+// wave in steps of 64 sequences at a time, and the tile inside it.
+__device__ inline int64_t tile_base(const int64_t* __restrict__ off, int s, int mul, int per) {
+  return max(off[s], int64_t(0)) * mul / per + s;
+}
+__device__ inline int find_seq(const int64_t* __restrict__ off, int seqs, int mul, int per, int64_t b, int64_t& tile) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave;
+    const int s = lane * step;
+    const bool below = s < n && tile_base(off, lo + s, mul, per) <= b;
+    const int c = max(1, static_cast<int>(__popcll(__ballot(below))));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  tile = b - tile_base(off, lo, mul, per);
+  return lo;
+}
+
+// Rows of a sequence are packed head by head: row r is token r / group, query
+// head kvh * group + r % group, so that the query heads of a key head share
+// its tiles.  Row r sees the keys j < limit.
+struct RowOf {
+  int token, head;
+};
+__device__ inline RowOf row_of(int r, int kvh, int group) {
+  RowOf x;
+  x.token = r / group;
+  x.head = kvh * group + (r - x.token * group);
+  return x;
+}
+__device__ inline int key_limit(int token, int lq, int lk, bool causal, int prefix) {
+  if (!causal) return lk;
+  return min(lk, max(token + lk - lq + 1, prefix));
+}
+
+// Copies rows of a [rows][heads][d] tensor to an LDS tile of N rows, zero where
+// addr(r) is null and past column d.
+template <typename T, int HD, int N, typename F>
+__device__ inline void stage(char* tile, int d, F addr) {
+  typedef Tile<T, HD> L;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int i = 0; i < N * L::kChunks / (kAttnWaves * kWave); ++i) {
+    const int idx = threadIdx.x + i * kAttnWaves * kWave;
+    const int r = idx / L::kChunks, c = idx % L::kChunks;
+    const T* p = addr(r);
+    u32x4 v = {0, 0, 0, 0};
+    if (p && c * L::kPer < d) v = *reinterpret_cast<const u32x4*>(p + c * L::kPer);
+    *reinterpret_cast<u32x4*>(tile + L::at(r, c)) = v;
+  }
+}
+
+// What rounding x to bf16 takes away.
+__device__ inline float rest_bf16(float x) {
+  return x - __uint_as_float(pack_bf16(0.0f, x) & 0xFFFF0000u);
+}
+
+// Four consecutive elements of an output row from registers 4 i .. 4 i + 3.
+__device__ inline void store4(uint16_t* p, float a, float b, float c, float d) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+}
+__device__ inline void store4(float* p, float a, float b, float c, float d) {
+  *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+
+}  // namespace rs

@@ -2,7 +2,9 @@
 // argument checks, workspace layout and dispatch to the kernels.
 #include <hip/hip_runtime.h>
 
-#include <string>
+#include <cmath>
+#include <new>
+#include <vector>
 
 #include "recis_mi355x.h"
 #include "seq_internal.h"
@@ -28,6 +30,87 @@ bool valid_norm(int64_t rows, int64_t dim) {
 }
 
 bool valid_stride(int64_t stride, int64_t width) { return stride >= width && stride < (int64_t(1) << 32); }
+
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// What is wrong with a descriptor, or null.
+const char* check_attn(const rs_attn_desc* d) {
+  if (!d) return "null descriptor";
+  if (!valid_dtype(d->dtype)) return "bad dtype";
+  if (d->heads_kv < 1 || d->heads_kv > 1024) return "heads_kv must be in [1, 1024]";
+  if (d->heads_q < d->heads_kv || d->heads_q > 65536 || d->heads_q % d->heads_kv != 0)
+    return "heads_q must be a multiple of heads_kv, at most 65536";
+  if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8 != 0) return "head_dim must be a multiple of 8 in [8, 128]";
+  if (d->reserved != 0) return "reserved must be 0";
+  constexpr int64_t kMost = int64_t(1) << 31;
+  if (d->seqs < 0 || d->seqs >= (int64_t(1) << 24)) return "seqs must be in [0, 2^24)";
+  if (d->q_rows < 0 || d->q_rows >= kMost || d->q_rows * d->heads_q >= kMost) return "q_rows * heads_q must be below 2^31";
+  if (d->kv_rows < 0 || d->kv_rows >= kMost) return "kv_rows must be in [0, 2^31)";
+  if (d->q_pad < 0 || d->q_pad >= kMost || d->kv_pad < 0 || d->kv_pad >= kMost) return "pad lengths must be in [0, 2^31)";
+  if (d->q_pad > 0 && d->seqs * d->q_pad != d->q_rows) return "padded: q_rows must be seqs * q_pad";
+  if (d->kv_pad > 0 && d->seqs * d->kv_pad != d->kv_rows) return "padded: kv_rows must be seqs * kv_pad";
+  if (d->max_q < 0) return "max_q must be >= 0";
+  const int64_t unit = d->dtype == RS_BF16 ? 8 : 4;
+  for (const int64_t st : {d->q_stride, d->q_head_stride, d->k_stride, d->k_head_stride, d->v_stride, d->v_head_stride})
+    if (st < 0 || st >= kMost || st % unit != 0) return "strides must be multiples of 16 bytes in [0, 2^31) elements";
+  if (!(d->scale > 0.0) || !std::isfinite(d->scale)) return "scale must be finite and > 0";
+  if (!(d->softcap >= 0.0) || !std::isfinite(d->softcap)) return "softcap must be finite and >= 0";
+  return nullptr;
+}
+
+AttnArgs attn_args(const rs_attn_desc& d) {
+  AttnArgs a{};
+  a.q = HeadRows{nullptr, d.q_stride, d.q_head_stride};
+  a.k = HeadRows{nullptr, d.k_stride, d.k_head_stride};
+  a.v = HeadRows{nullptr, d.v_stride, d.v_head_stride};
+  a.q_rows = d.q_rows;
+  a.kv_rows = d.kv_rows;
+  a.q_pad = d.q_pad;
+  a.kv_pad = d.kv_pad;
+  a.seqs = static_cast<int>(d.seqs);
+  a.hq = d.heads_q;
+  a.hkv = d.heads_kv;
+  a.group = d.heads_q / d.heads_kv;
+  a.d = d.head_dim;
+  a.causal = d.causal != 0;
+  a.scale = static_cast<float>(d.scale);
+  a.cap = static_cast<float>(d.softcap);
+  return a;
+}
+
+// Host check of the offsets: copies them back, so it synchronizes.
+rs_status check_offsets(const rs_attn_desc& d, const int64_t* q_off, const int64_t* kv_off, hipStream_t s) {
+  try {
+    RS_HIP(hipStreamSynchronize(s));
+    std::vector<int64_t> off(static_cast<size_t>(d.seqs) + 1);
+    for (int side = 0; side < 2; ++side) {
+      RS_HIP(hipMemcpy(off.data(), side ? kv_off : q_off, sizeof(int64_t) * off.size(), hipMemcpyDeviceToHost));
+      if (off[0] != 0) return fail(RS_EINVAL, "offsets must start at 0");
+      for (int64_t i = 0; i < d.seqs; ++i) {
+        if (off[i + 1] < off[i]) return fail(RS_EINVAL, "offsets must be nondecreasing");
+        if (side == 0 && d.max_q > 0 && off[i + 1] - off[i] > d.max_q && (d.q_pad == 0 || d.q_pad > d.max_q))
+          return fail(RS_EINVAL, "a sequence has more than max_q queries");
+      }
+      if ((side ? d.kv_pad : d.q_pad) == 0 && off[d.seqs] != (side ? d.kv_rows : d.q_rows))
+        return fail(RS_EINVAL, "packed offsets must end at the number of rows");
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(RS_ENOMEM, "no host memory for the offsets' check");
+  }
+  return RS_OK;
+}
+
+struct BwdWork {
+  size_t delta, slope_part, total;
+};
+BwdWork bwd_work(const AttnArgs& a) {
+  BwdWork w{};
+  w.slope_part = align_up(sizeof(float) * static_cast<size_t>(a.q_rows) * static_cast<size_t>(a.hq));
+  w.total = w.slope_part + align_up(sizeof(float) * static_cast<size_t>(attn_row_tiles(a)) * static_cast<size_t>(a.hq));
+  return w;
+}
 
 }  // namespace
 
@@ -98,6 +181,86 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
   a.dweight = dweight;
   a.dbias = dbias;
   RS_HIP(launch_norm_bwd(a, dtype == RS_BF16, static_cast<hipStream_t>(stream)));
+  return RS_OK;
+}
+
+size_t seq_attention_workspace_bytes(const rs_attn_desc* d, int32_t backward) {
+  if (check_attn(d)) return 0;
+  return backward ? bwd_work(attn_args(*d)).total : 0;
+}
+
+rs_status seq_attention_fwd(const rs_attn_desc* d, const void* q, const void* k, const void* v,
+                            const int64_t* q_offsets, const int64_t* kv_offsets, const int64_t* prefix,
+                            const float* slopes, void* out, void* rest, float* lse, void* workspace, size_t workspace_bytes,
+                            int32_t validate, rs_stream stream) {
+  if (const char* bad = check_attn(d)) return fail(RS_EINVAL, bad);
+  if (!q_offsets || !kv_offsets) return fail(RS_EINVAL, "null offsets");
+  if (d->q_rows > 0 && (!q || !out)) return fail(RS_EINVAL, "null q or out");
+  if (d->kv_rows > 0 && (!k || !v)) return fail(RS_EINVAL, "null k or v");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(rest))
+    return fail(RS_EINVAL, "q, k, v, out and rest must be 16-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (validate) {
+    const rs_status st = check_offsets(*d, q_offsets, kv_offsets, s);
+    if (st != RS_OK) return st;
+  }
+  if (d->seqs == 0 || d->q_rows == 0) return RS_OK;
+  AttnArgs a = attn_args(*d);
+  a.q.p = q;
+  a.k.p = k;
+  a.v.p = v;
+  a.q_off = q_offsets;
+  a.kv_off = kv_offsets;
+  a.prefix = d->causal ? prefix : nullptr;
+  a.slopes = slopes;
+  a.out = out;
+  a.rest = d->dtype == RS_BF16 ? rest : nullptr;
+  a.lse = lse;
+  RS_HIP(launch_attn_fwd(a, d->dtype == RS_BF16, s));
+  return RS_OK;
+}
+
+rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k, const void* v, const void* out,
+                            const void* rest, const float* lse, const void* grad_out, const int64_t* q_offsets,
+                            const int64_t* kv_offsets, const int64_t* prefix, const float* slopes, void* dq,
+                            void* dk, void* dv, float* dslopes, void* workspace, size_t workspace_bytes,
+                            int32_t validate, rs_stream stream) {
+  if (const char* bad = check_attn(d)) return fail(RS_EINVAL, bad);
+  if (!q_offsets || !kv_offsets) return fail(RS_EINVAL, "null offsets");
+  if (d->q_rows > 0 && (!q || !out || !lse || !grad_out || !dq)) return fail(RS_EINVAL, "null q, out, lse, grad_out or dq");
+  if (d->kv_rows > 0 && (!k || !v || !dk || !dv)) return fail(RS_EINVAL, "null k, v, dk or dv");
+  if (dslopes && !slopes) return fail(RS_EINVAL, "dslopes needs slopes");
+  for (const void* p : {q, k, v, out, rest, grad_out, static_cast<const void*>(dq), static_cast<const void*>(dk),
+                        static_cast<const void*>(dv)})
+    if (!aligned16(p)) return fail(RS_EINVAL, "q, k, v, out, rest, grad_out, dq, dk and dv must be 16-byte aligned");
+  AttnArgs a = attn_args(*d);
+  const BwdWork w = bwd_work(a);
+  if (w.total > 0 && (!workspace || workspace_bytes < w.total)) return fail(RS_EINVAL, "workspace missing or too small");
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(RS_EINVAL, "workspace must be 256-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (validate) {
+    const rs_status st = check_offsets(*d, q_offsets, kv_offsets, s);
+    if (st != RS_OK) return st;
+  }
+  a.q.p = q;
+  a.k.p = k;
+  a.v.p = v;
+  a.q_off = q_offsets;
+  a.kv_off = kv_offsets;
+  a.prefix = d->causal ? prefix : nullptr;
+  a.slopes = slopes;
+  a.o = out;
+  a.o_rest = d->dtype == RS_BF16 ? rest : nullptr;
+  a.dout = grad_out;
+  a.lse_in = lse;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.dslopes = dslopes;
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  a.delta = reinterpret_cast<float*>(base);
+  a.slope_part = dslopes ? reinterpret_cast<float*>(base + w.slope_part) : nullptr;
+  RS_HIP(launch_attn_bwd(a, d->dtype == RS_BF16, s));
   return RS_OK;
 }
 

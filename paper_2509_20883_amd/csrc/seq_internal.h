@@ -41,4 +41,38 @@ int norm_parts(int64_t rows, int64_t dim);
 hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t s);
 
+// ---------------------------------------------------------------------------
+// attention over ragged sequences
+// ---------------------------------------------------------------------------
+
+// Element strides of a [rows][heads][d] tensor whose d is contiguous.
+struct HeadRows {
+  const void* p;
+  int64_t row, head;
+};
+
+struct AttnArgs {
+  HeadRows q, k, v;
+  const int64_t *q_off, *kv_off, *prefix;
+  const float* slopes;
+  int64_t q_rows, kv_rows, q_pad, kv_pad;
+  int seqs, hq, hkv, group, d, causal;
+  float scale, cap;
+  // outputs (and the backward's inputs): contiguous [rows][heads][d]
+  void* out;
+  void* rest;  // what rounding to bf16 took from out, in bf16; null: not wanted
+  float* lse;  // [q_rows][hq], natural logarithm
+  // backward
+  const void *o, *o_rest, *dout;
+  const float* lse_in;
+  void *dq, *dk, *dv;
+  float *dslopes, *delta, *slope_part;
+};
+
+hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, hipStream_t s);
+// Blocks of the pass over query rows (each leaves one partial sum per head
+// of the slopes' gradient).
+int64_t attn_row_tiles(const AttnArgs& a);
+
 }  // namespace rs

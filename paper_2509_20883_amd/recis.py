@@ -6,13 +6,14 @@ fallback: if the library is not built, or no GPU is present, calls raise.
 
 Names follow the C ABI (include/recis_mi355x.h): ht_create, ht_find_or_insert,
 lookup_pool_fwd, lookup_pool_bwd, sparse_opt_step, lookup_pool_bwd_opt,
-ids_partition, fused_bucketize, fused_mod, layer_norm_fwd, layer_norm_bwd.
+ids_partition, fused_bucketize, fused_mod, layer_norm_fwd, layer_norm_bwd,
+seq_attention_fwd, seq_attention_bwd.
 """
 from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -98,6 +99,15 @@ class RsCtx(C.Structure):
                 ("mode", C.c_int32), ("dim", C.c_int32), ("priv", C.c_int64 * 16)]
 
 
+class AttnDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32), ("head_dim", C.c_int32),
+                ("causal", C.c_int32), ("reserved", C.c_int32), ("seqs", C.c_int64), ("q_rows", C.c_int64),
+                ("kv_rows", C.c_int64), ("q_pad", C.c_int64), ("kv_pad", C.c_int64), ("max_q", C.c_int64),
+                ("q_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("v_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("scale", C.c_double), ("softcap", C.c_double)]
+
+
 _lib = None
 
 
@@ -142,6 +152,9 @@ def lib() -> C.CDLL:
         "layer_norm_fwd": (C.c_int, [p, i64, i64, i64, i32, p, p, i32, C.c_double, p, p, i64, p, p, p]),
         "layer_norm_bwd_workspace_bytes": (C.c_size_t, [i64, i64]),
         "layer_norm_bwd": (C.c_int, [p, i64, p, i64, i64, i64, i32, p, i32, p, p, p, p, i64, p, p, p, C.c_size_t, p]),
+        "seq_attention_workspace_bytes": (C.c_size_t, [C.POINTER(AttnDesc), i32]),
+        "seq_attention_fwd": (C.c_int, [C.POINTER(AttnDesc)] + [p] * 11 + [C.c_size_t, i32, p]),
+        "seq_attention_bwd": (C.c_int, [C.POINTER(AttnDesc)] + [p] * 16 + [C.c_size_t, i32, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -340,6 +353,12 @@ def _bytes(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.T
     return ws
 
 
+def _packed(t: torch.Tensor) -> torch.Tensor:
+    """Contiguous and 16-byte aligned (a copy where it is not)."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 class LayerNorm:
     """Layer norm over the last axis, with a reusable backward workspace.
 
@@ -423,6 +442,131 @@ class LayerNorm:
                                     mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dim, dw.data_ptr(),
                                     db.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream()))
         return dx, dw, db
+
+
+class AttnStats(NamedTuple):
+    """What SeqAttention.forward keeps for the backward: lse (float32 [...,
+    heads_q], the log of each query's softmax sum, -inf where it sees no key)
+    and rest (bf16, out's shape: what rounding took from out; None in fp32)."""
+    lse: torch.Tensor
+    rest: Optional[torch.Tensor]
+
+
+class SeqAttention:
+    """Attention over ragged sequences, with a reusable workspace.
+
+    q [rows, heads_q, d] packed with q_offsets (int64 [seqs + 1]), or the
+    padded [seqs, pad, heads_q, d]; k, v [rows, heads_kv, d] or [seqs, pad,
+    heads_kv, d] with kv_offsets (default: q_offsets).  float32 or bfloat16,
+    d a multiple of 8 up to 128.  The last axis must be contiguous; other
+    strides are taken as they are where they are multiples of 16 bytes, else
+    the tensor is copied.  ``forward`` returns (out, stats); ``backward`` takes
+    the output gradient and both and returns (dq, dk, dv, dslopes).
+
+    causal: query i of Lq sees key j of Lk when j <= i + Lk - Lq, or j <
+    prefix[s] (int64 [seqs]); softcap: scores capped by softcap * tanh(x /
+    softcap); slopes (float32 [heads_q]): the score falls by slope * |i + Lk -
+    Lq - j|, and the backward returns their gradient.  max_q: a bound of the
+    query lengths where the caller knows one (0: none): it only shapes the
+    launches, so that few queries over long keys are split along the keys.
+    Calls of one object share its workspace: issue them on one stream, or
+    order the streams.
+    """
+
+    def __init__(self, scale: Optional[float] = None, softcap: float = 0.0, causal: bool = True):
+        self.scale, self.softcap, self.causal = scale, float(softcap), bool(causal)
+        self.ws: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def _layout(t: torch.Tensor, what: str):
+        """The tensor (copied if its strides do not serve), rows, pad, row and head strides."""
+        if t.dim() not in (3, 4):
+            raise RecisError(EINVAL, f"{what} must be [rows, heads, d] or [seqs, pad, heads, d]")
+        unit = 16 // t.element_size()
+        st = t.stride()
+        if (st[-1] != 1 or st[-2] % unit or st[-3] % unit or (t.dim() == 4 and st[0] != t.shape[1] * st[1]) or
+                t.data_ptr() % 16):
+            t = _packed(t)
+            st = t.stride()
+        if t.dim() == 4:
+            return t, t.shape[0] * t.shape[1], t.shape[1], st[1], st[2]
+        return t, t.shape[0], 0, st[0], st[1]
+
+    def _desc(self, q, k, v, q_offsets, kv_offsets, prefix, slopes, max_q):
+        dt = _seq_type(q, "q")
+        if not (k.is_cuda and v.is_cuda) or k.dtype != q.dtype or v.dtype != q.dtype:
+            raise RecisError(EINVAL, "q, k and v must be GPU tensors of one type")
+        q, q_rows, q_pad, qs, qh = self._layout(q, "q")
+        k, kv_rows, kv_pad, ks, kh = self._layout(k, "k")
+        v, v_rows, v_pad, vs, vh = self._layout(v, "v")
+        if k.shape != v.shape or q.shape[-1] != k.shape[-1]:
+            raise RecisError(EINVAL, "k and v must have one shape, and q their last axis")
+        qo = _dev(q_offsets, torch.int64)
+        ko = qo if kv_offsets is None else _dev(kv_offsets, torch.int64)
+        seqs = qo.numel() - 1
+        if seqs < 0 or ko.numel() - 1 != seqs:
+            raise RecisError(EINVAL, "q_offsets and kv_offsets must both be [seqs + 1]")
+        if (q_pad and q.shape[0] != seqs) or (kv_pad and k.shape[0] != seqs):
+            raise RecisError(EINVAL, "a padded tensor must have one block per sequence")
+        if prefix is not None:
+            prefix = _dev(prefix, torch.int64)
+            if prefix.numel() != seqs:
+                raise RecisError(EINVAL, "prefix must have one length per sequence")
+        if slopes is not None:
+            slopes = _dev(slopes, torch.float32)
+            if slopes.numel() != q.shape[-2]:
+                raise RecisError(EINVAL, "slopes must have one value per query head")
+        d = q.shape[-1]
+        scale = self.scale if self.scale is not None else (d ** -0.5 if d else 1.0)
+        desc = AttnDesc(dt, q.shape[-2], k.shape[-2], d, int(self.causal), 0, seqs, q_rows, kv_rows, q_pad, kv_pad,
+                        max_q, qs, qh, ks, kh, vs, vh, scale, self.softcap)
+        return desc, q, k, v, qo, ko, prefix, slopes
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                kv_offsets: Optional[torch.Tensor] = None, prefix: Optional[torch.Tensor] = None,
+                slopes: Optional[torch.Tensor] = None, max_q: int = 0, out: Optional[torch.Tensor] = None,
+                validate: bool = False):
+        shape = q.shape
+        desc, q, k, v, qo, ko, prefix, slopes = self._desc(q, k, v, q_offsets, kv_offsets, prefix, slopes, max_q)
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        elif out.shape != shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
+            raise RecisError(EINVAL, "out must be a contiguous GPU tensor of q's shape and type")
+        stats = AttnStats(torch.empty(shape[:-1], dtype=torch.float32, device=q.device),
+                          torch.empty(shape, dtype=q.dtype, device=q.device) if q.dtype == torch.bfloat16 else None)
+        need = lib().seq_attention_workspace_bytes(C.byref(desc), 0)
+        if need:
+            self.ws = _bytes(self.ws, need, q)
+        _check(lib().seq_attention_fwd(C.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), qo.data_ptr(),
+                                       ko.data_ptr(), _ptr(prefix), _ptr(slopes), out.data_ptr(), _ptr(stats.rest),
+                                       stats.lse.data_ptr(), _ptr(self.ws) if need else None,
+                                       self.ws.numel() if need else 0, int(validate), _stream()))
+        return out, stats
+
+    def backward(self, grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                 stats: AttnStats, q_offsets: torch.Tensor, kv_offsets: Optional[torch.Tensor] = None,
+                 prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, max_q: int = 0,
+                 validate: bool = False):
+        lse, rest = stats
+        for t, what in ((grad_out, "grad_out"), (out, "out"), (out if rest is None else rest, "stats.rest")):
+            if t.shape != q.shape or t.dtype != q.dtype or not t.is_cuda:
+                raise RecisError(EINVAL, f"{what} must be a GPU tensor of q's shape and type")
+        if lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_cuda:
+            raise RecisError(EINVAL, "stats.lse must be the forward's float32 [..., heads_q]")
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=k.dtype, device=q.device)
+        dv = torch.empty(v.shape, dtype=v.dtype, device=q.device)
+        desc, q, k, v, qo, ko, prefix, slopes = self._desc(q, k, v, q_offsets, kv_offsets, prefix, slopes, max_q)
+        grad_out, out, lse = _packed(grad_out), _packed(out), lse.contiguous()
+        rest = None if rest is None else _packed(rest)
+        dslopes = None if slopes is None else torch.empty_like(slopes)
+        need = lib().seq_attention_workspace_bytes(C.byref(desc), 1)
+        self.ws = _bytes(self.ws, need, q)
+        _check(lib().seq_attention_bwd(C.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                       _ptr(rest), lse.data_ptr(), grad_out.data_ptr(), qo.data_ptr(), ko.data_ptr(),
+                                       _ptr(prefix), _ptr(slopes), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                       _ptr(dslopes), self.ws.data_ptr(), self.ws.numel(), int(validate), _stream()))
+        return dq, dk, dv, dslopes
 
 
 PROBES = {"read": 0, "write": 1, "copy": 2, "gather": 3, "rmw": 4}
