@@ -130,10 +130,12 @@ rs_status layer_norm_fwd(const void* x, int64_t rows, int64_t dim, int64_t x_str
   a.dim = dim;
   a.eps = static_cast<float>(eps);
   a.param_bf16 = param_dtype == RS_BF16;
+  a.stream = norm_stream(rows, dim, dtype == RS_BF16);
   a.x = x;
   a.x_stride = x_stride;
   a.weight = weight;
   a.bias = bias;
+  a.param16 = norm_param16(weight, bias);
   a.mask = mask;
   a.y = y;
   a.y_stride = y_stride;
@@ -163,14 +165,16 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
       return fail(RS_EINVAL, "workspace missing or too small");
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(RS_EINVAL, "workspace must be 256-byte aligned");
     a.part = static_cast<float*>(workspace);
-    a.nparts = norm_parts(rows, dim);
   }
+  a.nparts = norm_parts(rows, dim);
   a.rows = rows;
   a.dim = dim;
   a.param_bf16 = param_dtype == RS_BF16;
+  a.stream = norm_stream(rows, dim, dtype == RS_BF16);
   a.x = x;
   a.x_stride = x_stride;
   a.weight = weight;
+  a.param16 = norm_param16(weight, nullptr);
   a.mask = mask;
   a.dy = dy;
   a.dy_stride = dy_stride;

@@ -17,6 +17,8 @@ struct NormArgs {
   int64_t rows, dim;
   float eps;
   bool param_bf16;
+  bool stream;   // y / dx is stored past the caches
+  bool param16;  // weight and bias start at multiples of 16 bytes
   const void* x;
   int64_t x_stride;
   const void *weight, *bias;
@@ -38,6 +40,8 @@ struct NormArgs {
 
 // Partial sums of dw and db: the rows of each are added by one block.
 int norm_parts(int64_t rows, int64_t dim);
+bool norm_stream(int64_t rows, int64_t dim, bool bf16);
+bool norm_param16(const void* weight, const void* bias);
 hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t s);
 
