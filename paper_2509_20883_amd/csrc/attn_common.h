@@ -256,8 +256,64 @@ __device__ inline int key_limit(int token, int lq, int lk, bool causal, int pref
   return min(lk, max(token + lk - lq + 1, prefix));
 }
 
-// Copies rows of a [rows][heads][d] tensor to an LDS tile of N rows, zero where
-// addr(r) is null and past column d.
+// Rows of a [rows][heads][d] tensor to an LDS tile of kAttnStep rows, by loads
+// that write LDS themselves (16 bytes per lane, a wave's 1 KiB back to back):
+// no registers hold them and the wave goes on; wait_tiles() before their use.
+// The lane picks the chunk that belongs at its place, so the tile's chunk
+// order costs nothing.  The buffer's bounds do the masking: rows past the
+// sequence's end and columns past d lie outside and arrive as zeros.
+template <typename T, int HD>
+struct TileLoader {
+  typedef Tile<T, HD> L;
+  static constexpr int kLoads = kAttnStep * L::kRowBytes / (kAttnWaves * kWave * 16);  // per thread
+  uint32_t off[kLoads];  // byte offset of the thread's chunks from the tile's first row
+  int64_t row_bytes;
+  const char* base;  // the sequence's first row
+  int len, d_bytes;
+
+  __device__ inline void init(const void* p, int64_t start, int64_t row, int64_t head_off, int d, int n) {
+    row_bytes = row * static_cast<int64_t>(sizeof(T));
+    base = static_cast<const char*>(p) + (start * row + head_off) * static_cast<int64_t>(sizeof(T));
+    len = n;
+    d_bytes = d * static_cast<int>(sizeof(T));
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = ((wave * kLoads + i) * kWave + lane) * 16;
+      const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(r);
+      off[i] = c * 16 < d_bytes ? static_cast<uint32_t>(r * row_bytes) + c * 16 : 0x80000000u;
+    }
+  }
+  // Rows j0 .. j0 + kAttnStep - 1 of the sequence (j0 < len).
+  __device__ inline void load(char* tile, int j0) const {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass has no buffer descriptors
+    const int rows = min(kAttnStep, len - j0);
+    const int bytes = static_cast<int>(max(rows - 1, 0) * row_bytes) + d_bytes;
+    const char* p = base + j0 * row_bytes;
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    // readfirstlane gives a signed int: no sign may reach the upper word
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes),
+        0x00020000);
+    char* dst = tile + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kLoads * kWave * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc, (__attribute__((address_space(3))) void*)(dst + i * kWave * 16), 16, off[i], 0, 0, 0);
+#endif
+  }
+};
+
+// Every load of the wave has arrived, and then every wave's.
+__device__ inline void wait_tiles() {
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+}
+
+// Copies rows of a [rows][heads][d] tensor to an LDS tile of N rows through
+// registers, zero where addr(r) is null and past column d.
 template <typename T, int HD, int N, typename F>
 __device__ inline void stage(char* tile, int d, F addr) {
   typedef Tile<T, HD> L;

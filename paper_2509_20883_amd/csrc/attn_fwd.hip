@@ -8,7 +8,12 @@
 // in base 2.  A block takes 128 packed rows (tokens times the query heads of
 // one key head) and walks over the keys 64 at a time; a wave owns 32 rows, one
 // per lane column: its maximum, sum and rescaling are the lane's own scalars.
+// The next step's keys and values are on their way to LDS while a step is
+// computed.  Where the rows alone make too few blocks (single tokens, short
+// chunks), a block takes a chunk of the keys and a second kernel joins them.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "attn_common.h"
 
@@ -17,22 +22,39 @@
 namespace rs {
 namespace {
 
+// Blocks per CU that the registers are kept down for: the two of one that is
+// in its products and one that is in its softmax; fp32 rows of 128 fill a CU.
 template <typename T, int HD>
-__global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a) {
+constexpr int kResidentBlocks = HD * sizeof(T) > 256 ? 1 : 2;
+
+template <typename T, int HD, bool SPLIT>
+__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k_attn_fwd(const AttnArgs a) {
   typedef Tile<T, HD> L;
   typedef typename Frag<T>::type F;
   constexpr int KS = HD / 16;  // product steps over d
   constexpr int DT = HD / 32;  // 32-column tiles of the output
-  extern __shared__ __align__(16) char lds[];
-  char* kt = lds;
-  char* vt = lds + kAttnStep * L::kRowBytes;
+  constexpr int kTile = kAttnStep * L::kRowBytes;
+  __shared__ __align__(1024) char lds[4 * kTile];  // keys and values, two steps of each
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
   const int kvh = blockIdx.y;
   int s;
   int64_t tile;
-  if (a.q_pad > 0) {
+  int c0 = 0;  // the block's first key
+  if (SPLIT) {
+    int64_t c;
+    if (a.kv_pad > 0) {
+      const int64_t per = (a.kv_pad + a.chunk - 1) / a.chunk;
+      s = static_cast<int>(blockIdx.x / per);
+      c = blockIdx.x - s * per;
+    } else {
+      s = find_seq(a.kv_off, a.seqs, 1, a.chunk, blockIdx.x, c);
+    }
+    tile = blockIdx.z;
+    if (c * a.chunk >= int64_t(1) << 31) return;
+    c0 = static_cast<int>(c) * a.chunk;
+  } else if (a.q_pad > 0) {
     const int64_t per = (a.q_pad * a.group + kAttnRows - 1) / kAttnRows;
     s = static_cast<int>(blockIdx.x / per);
     tile = blockIdx.x - s * per;
@@ -40,7 +62,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
     s = find_seq(a.q_off, a.seqs, a.group, kAttnRows, blockIdx.x, tile);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
-  const int rows = qs.len * a.group;  // with a key: the others are padding
+  const int rows = qs.len * a.group;  // the others of a padded sequence have no key
   const int64_t out_rows = a.q_pad > 0 ? a.q_pad * a.group : rows;
   if (tile * kAttnRows >= out_rows) return;  // block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
@@ -50,10 +72,25 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
   const RowOf me = row_of(r, kvh, a.group);
   const bool live = r < rows;
   const int limit = live ? key_limit(me.token, qs.len, ks.len, a.causal, prefix) : 0;
-  // limits do not fall along the rows: the block's last row sees the most keys
+  // limits do not fall along the rows: the last row sees the most keys
   const int last = min(r0 + kAttnRows, rows) - 1;
-  const int block_limit = last >= r0 ? key_limit(last / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  int end = last >= r0 ? key_limit(last / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  const bool joined = SPLIT && ks.len > a.chunk;  // other blocks hold parts of these rows
+  if (SPLIT) {
+    if (c0 > 0 && c0 >= end) return;  // block-uniform; the join does not look here
+    end = min(end, c0 + a.chunk);
+  }
+  const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows) - 1;
+  const int wave_least = w0 < rows ? key_limit(w0 / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  const int wave_most = w1 >= w0 ? key_limit(w1 / a.group, qs.len, ks.len, a.causal, prefix) : 0;
 
+  TileLoader<T, HD> kl, vl;
+  kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
+  vl.init(a.v.p, ks.start, a.v.row, kvh * a.v.head, a.d, ks.len);
+  if (c0 < end) {
+    kl.load(lds, c0);
+    vl.load(lds + 2 * kTile, c0);
+  }
   F qf[KS];
   {
     const T* q = static_cast<const T*>(a.q.p) + (qs.start + me.token) * a.q.row + me.head * a.q.head;
@@ -66,23 +103,28 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
   }
   const float pos = static_cast<float>(me.token + ks.len - qs.len);
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
-  const float c = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+  const float inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e, scale2 = a.scale * kLog2e;
+  // scores without cap and slope are scaled inside the exponent
+  const bool plain = !(a.cap > 0.0f) && !a.slopes;
+  const float c = plain ? scale2 : 1.0f;
 
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
   float m = -INFINITY, l = 0.0f;
 
-  const T* kp = static_cast<const T*>(a.k.p) + ks.start * a.k.row + kvh * a.k.head;
-  const T* vp = static_cast<const T*>(a.v.p) + ks.start * a.v.row + kvh * a.v.head;
-  for (int j0 = 0; j0 < block_limit; j0 += kAttnStep) {
-    __syncthreads();  // the previous step's tiles have been read
-    stage<T, HD, kAttnStep>(kt, a.d, [&](int i) { return j0 + i < ks.len ? kp + (j0 + i) * a.k.row : nullptr; });
-    stage<T, HD, kAttnStep>(vt, a.d, [&](int i) { return j0 + i < ks.len ? vp + (j0 + i) * a.v.row : nullptr; });
-    __syncthreads();
+  int buf = 0;
+  for (int j0 = c0; j0 < end; j0 += kAttnStep, buf ^= 1) {
+    wait_tiles();  // this step's tiles are there, the other step's have been read
+    if (j0 + kAttnStep < end) {
+      kl.load(lds + (buf ^ 1) * kTile, j0 + kAttnStep);
+      vl.load(lds + (2 + (buf ^ 1)) * kTile, j0 + kAttnStep);
+    }
+    if (j0 >= wave_most) continue;  // wave-uniform: none of its rows sees these keys
+    const char* kt = lds + buf * kTile;
+    const char* vt = lds + (2 + buf) * kTile;
 
     float p[2][16];
-    float top = m;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 sc = {};
@@ -93,30 +135,65 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
         sc = mma(kf, qf[t], sc);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int j = j0 + kb * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-        float x = a.cap > 0.0f ? cap2 * tanh_of<T>(sc[i] * inv_cap) : sc[i] * c;
-        if (a.slopes) x -= slope * fabsf(static_cast<float>(j) - pos);
-        x = j < limit ? x : -INFINITY;
-        p[kb][i] = x;
-        top = fmaxf(top, x);
+      for (int i = 0; i < 16; ++i) p[kb][i] = sc[i];
+    }
+    const int j = j0 + half * 4;  // register i of block kb is key j + kb * 32 + (i / 4) * 8 + i % 4
+    if (!plain) {
+      if (a.cap > 0.0f) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[kb][i] = cap2 * tanh_of<T>(p[kb][i] * inv_cap);
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[kb][i] *= scale2;
+      }
+      if (a.slopes) {
+        const float dist = static_cast<float>(j) - pos;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            p[kb][i] -= slope * fabsf(dist + static_cast<float>(kb * 32 + (i >> 2) * 8 + (i & 3)));
       }
     }
-    top = other_half_max(top);
-    const float base = top == -INFINITY ? 0.0f : top;  // no key seen yet
-    const float alpha = exp2_hw(m - base);
-    m = top;
+    if (j0 + kAttnStep > wave_least) {
+      const int left = limit - j;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          p[kb][i] = kb * 32 + (i >> 2) * 8 + (i & 3) < left ? p[kb][i] : -INFINITY;
+    }
+    float top = p[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
+    top = other_half_max(top) * c;
+    // the running maximum moves only when a score passes it by 2^8: until then
+    // the probabilities are larger than 1 by at most that, which neither fp32
+    // sums nor bf16's relative rounding notice
+    if (__any(top > m + 8.0f)) {
+      const float next = fmaxf(m, top);
+      const float alpha = exp2_hw(next == -INFINITY ? 0.0f : m - next);
+      m = next;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[i] *= alpha;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;  // no key seen yet
     float sum = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        p[kb][i] = exp2_hw(p[kb][i] - base);
+        p[kb][i] = exp2_hw(p[kb][i] * c - base);
         sum += p[kb][i];
       }
-    l = l * alpha + sum;  // this half's keys
-#pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] *= alpha;
+    l += sum;  // this half's keys
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -133,7 +210,23 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
 
   if (r >= out_rows) return;
   l = other_half_sum(l);
-  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);  // no key: 0; NaN stays
+  if (joined) {
+    const int at = wave * 32 + col;
+    if (at >= a.part_rows) return;
+    const int64_t slot = ((static_cast<int64_t>(blockIdx.x) * a.hkv + kvh) * a.row_tiles + tile) * a.part_rows + at;
+    float* po = a.part_o + slot * a.d;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d0 = i * 32 + g * 8 + half * 4;
+        if (d0 < a.d) store4(po + d0, acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]);
+      }
+    if (half == 0) reinterpret_cast<float2*>(a.part_ml)[slot] = make_float2(m, l);
+    return;
+  }
+  const bool none = !live || l == 0.0f;  // no key: 0 (a NaN sum stays)
+  const float inv = none ? 0.0f : 1.0f / l;
   const int64_t row = (qs.start + me.token) * a.hq + me.head;
   T* out = static_cast<T*>(a.out) + row * a.d;
 #pragma unroll
@@ -144,20 +237,112 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_fwd(const AttnArgs a
       if (d0 >= a.d) continue;
       float x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = acc[i][4 * g + e] * inv;
+      for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : acc[i][4 * g + e] * inv;
       store4(out + d0, x[0], x[1], x[2], x[3]);
       if (sizeof(T) == 2 && a.rest)
         store4(static_cast<uint16_t*>(a.rest) + row * a.d + d0, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]),
                rest_bf16(x[3]));
     }
-  if (a.lse && half == 0) a.lse[row] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
+  if (a.lse && half == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
+}
+
+// Joins the chunks of a row: a block per query token and head, threads four
+// columns and a share of the chunks each.
+//   m = max m_c,  l = sum l_c 2^(m_c - m),  out = sum acc_c 2^(m_c - m) / l
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
+  __shared__ float4 sh_o[kBlock];
+  __shared__ float sh_l[kBlock];
+  __shared__ float sh_m[kBlock / kWave];
+  const int head = blockIdx.y, kvh = head / a.group;
+  int s;
+  int64_t token;
+  if (a.q_pad > 0) {
+    s = static_cast<int>(blockIdx.x / a.q_pad);
+    token = blockIdx.x - s * a.q_pad;
+  } else {
+    s = find_seq(a.q_off, a.seqs, 1, 1, blockIdx.x, token);
+  }
+  const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
+  if (ks.len <= a.chunk || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // written, or no row; block-uniform
+  const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
+  const int limit = token < qs.len ? key_limit(static_cast<int>(token), qs.len, ks.len, a.causal, prefix) : 0;
+  const int chunks = (limit + a.chunk - 1) / a.chunk;
+  const int64_t first = a.kv_pad > 0 ? s * ((a.kv_pad + a.chunk - 1) / a.chunk) : tile_base(a.kv_off, s, 1, a.chunk);
+  const int r = static_cast<int>(token) * a.group + head - kvh * a.group;
+  const int64_t tile = r / kAttnRows, at = r % kAttnRows;
+  if (tile >= a.row_tiles || at >= a.part_rows) return;  // past the caller's bound of the queries
+  const int64_t slot0 = ((first * a.hkv + kvh) * a.row_tiles + tile) * a.part_rows + at;
+  const int64_t step = static_cast<int64_t>(a.hkv) * a.row_tiles * a.part_rows;
+
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float m = -INFINITY;
+  for (int c = threadIdx.x; c < chunks; c += kBlock) m = fmaxf(m, ml[slot0 + c * step].x);
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
+  if ((threadIdx.x & (kWave - 1)) == 0) sh_m[threadIdx.x / kWave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kBlock / kWave; ++w) m = fmaxf(m, sh_m[w]);
+  const float base = m == -INFINITY ? 0.0f : m;
+
+  const int quads = a.d / 4;  // at most 32
+  const int shares = kBlock / quads, q = threadIdx.x % quads, share = threadIdx.x / quads;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float l = 0.0f;
+  if (share < shares) {
+#pragma unroll 4
+    for (int c = share; c < chunks; c += shares) {
+      const int64_t slot = slot0 + c * step;
+      const float2 x = ml[slot];
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + slot * a.d + 4 * q);
+      const float w = exp2_hw(x.x - base);
+      l += w * x.y;
+      o.x += w * y.x;
+      o.y += w * y.y;
+      o.z += w * y.z;
+      o.w += w * y.w;
+    }
+  }
+  sh_o[threadIdx.x] = o;
+  sh_l[threadIdx.x] = l;
+  __syncthreads();
+  if (share > 0) return;
+  for (int k = 1; k < shares; ++k) {
+    const float4 y = sh_o[k * quads + q];
+    l += sh_l[k * quads + q];
+    o.x += y.x;
+    o.y += y.y;
+    o.z += y.z;
+    o.w += y.w;
+  }
+  const bool none = l == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / l;
+  const int64_t row = (qs.start + token) * a.hq + head;
+  const float x[4] = {none ? 0.0f : o.x * inv, none ? 0.0f : o.y * inv, none ? 0.0f : o.z * inv, none ? 0.0f : o.w * inv};
+  store4(static_cast<T*>(a.out) + row * a.d + 4 * q, x[0], x[1], x[2], x[3]);
+  if (sizeof(T) == 2 && a.rest)
+    store4(static_cast<uint16_t*>(a.rest) + row * a.d + 4 * q, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]),
+           rest_bf16(x[3]));
+  if (a.lse && q == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
+}
+
+int64_t key_chunks(const AttnArgs& a) {
+  if (a.kv_pad > 0) return a.seqs * ((a.kv_pad + a.chunk - 1) / a.chunk);
+  return a.kv_rows / a.chunk + a.seqs;
 }
 
 template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(attn_row_tiles(a)), a.hkv);
-  const size_t lds = 2 * kAttnStep * Tile<T, HD>::kRowBytes;
-  k_attn_fwd<T, HD><<<grid, kAttnWaves * kWave, lds, s>>>(a);
+  if (a.chunk > 0) {
+    const dim3 grid(static_cast<unsigned>(key_chunks(a)), a.hkv, a.row_tiles);
+    k_attn_fwd<T, HD, true><<<grid, kAttnWaves * kWave, 0, s>>>(a);
+    const dim3 jg(static_cast<unsigned>(a.q_pad > 0 ? a.q_rows : a.q_rows + a.seqs), a.hq);
+    k_attn_join<T><<<jg, kBlock, 0, s>>>(a);
+  } else {
+    const dim3 rows(static_cast<unsigned>(attn_row_tiles(a)), a.hkv);
+    k_attn_fwd<T, HD, false><<<rows, kAttnWaves * kWave, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -174,6 +359,32 @@ int64_t attn_row_tiles(const AttnArgs& a) {
   if (a.seqs == 0) return 0;
   if (a.q_pad > 0) return a.seqs * ((a.q_pad * a.group + kAttnRows - 1) / kAttnRows);
   return a.q_rows * a.group / kAttnRows + a.seqs;
+}
+
+// Split where the row tiles alone are fewer blocks than the GPU runs at once
+// twice over, into about kSplitBlocks, of at least kLeastChunk keys.
+constexpr int64_t kFewBlocks = 1024, kSplitBlocks = 2048, kLeastChunk = 256;
+
+size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at) {
+  a->chunk = 0;
+  *ml_at = 0;
+  if (a->seqs == 0 || a->q_rows == 0 || attn_row_tiles(*a) * a->hkv >= kFewBlocks) return 0;
+  const int64_t most_keys = a->kv_pad > 0 ? a->kv_pad : a->kv_rows;  // of one sequence
+  if (most_keys < 2 * kLeastChunk) return 0;
+  int64_t most_q = a->q_pad > 0 ? a->q_pad : a->q_rows;
+  if (a->q_pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
+  const int64_t tiles = (most_q * a->group + kAttnRows - 1) / kAttnRows;
+  const int64_t chunk = a->kv_rows * a->hkv * tiles / kSplitBlocks;
+  a->chunk = static_cast<int>(std::max(kLeastChunk, (chunk + kAttnStep - 1) / kAttnStep * kAttnStep));
+  if (a->chunk >= most_keys) {
+    a->chunk = 0;
+    return 0;
+  }
+  a->row_tiles = static_cast<int>(tiles);
+  a->part_rows = static_cast<int>(std::min(most_q * a->group, int64_t(kAttnRows)));
+  const size_t slots = static_cast<size_t>(key_chunks(*a)) * a->hkv * a->row_tiles * a->part_rows;
+  *ml_at = (slots * a->d * sizeof(float) + 255) / 256 * 256;
+  return *ml_at + slots * 2 * sizeof(float);
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, hipStream_t s) {

@@ -54,7 +54,8 @@ const char* check_attn(const rs_attn_desc* d) {
   if (d->max_q < 0) return "max_q must be >= 0";
   const int64_t unit = d->dtype == RS_BF16 ? 8 : 4;
   for (const int64_t st : {d->q_stride, d->q_head_stride, d->k_stride, d->k_head_stride, d->v_stride, d->v_head_stride})
-    if (st < 0 || st >= kMost || st % unit != 0) return "strides must be multiples of 16 bytes in [0, 2^31) elements";
+    if (st < 0 || st >= (int64_t(1) << 23) || st % unit != 0)
+      return "strides must be multiples of 16 bytes in [0, 2^23) elements";
   if (!(d->scale > 0.0) || !std::isfinite(d->scale)) return "scale must be finite and > 0";
   if (!(d->softcap >= 0.0) || !std::isfinite(d->softcap)) return "softcap must be finite and >= 0";
   return nullptr;
@@ -190,7 +191,9 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
 
 size_t seq_attention_workspace_bytes(const rs_attn_desc* d, int32_t backward) {
   if (check_attn(d)) return 0;
-  return backward ? bwd_work(attn_args(*d)).total : 0;
+  AttnArgs a = attn_args(*d);
+  size_t at = 0;
+  return backward ? bwd_work(a).total : plan_attn_split(&a, d->max_q, &at);
 }
 
 rs_status seq_attention_fwd(const rs_attn_desc* d, const void* q, const void* k, const void* v,
@@ -203,13 +206,21 @@ rs_status seq_attention_fwd(const rs_attn_desc* d, const void* q, const void* k,
   if (d->kv_rows > 0 && (!k || !v)) return fail(RS_EINVAL, "null k or v");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(rest))
     return fail(RS_EINVAL, "q, k, v, out and rest must be 16-byte aligned");
+  AttnArgs a = attn_args(*d);
+  size_t ml_at = 0;
+  const size_t need = plan_attn_split(&a, d->max_q, &ml_at);
+  if (need > 0) {
+    if (!workspace || workspace_bytes < need) return fail(RS_EINVAL, "workspace missing or too small");
+    if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(RS_EINVAL, "workspace must be 256-byte aligned");
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + ml_at);
+  }
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {
     const rs_status st = check_offsets(*d, q_offsets, kv_offsets, s);
     if (st != RS_OK) return st;
   }
   if (d->seqs == 0 || d->q_rows == 0) return RS_OK;
-  AttnArgs a = attn_args(*d);
   a.q.p = q;
   a.k.p = k;
   a.v.p = v;

@@ -66,6 +66,10 @@ struct AttnArgs {
   void* out;
   void* rest;  // what rounding to bf16 took from out, in bf16; null: not wanted
   float* lse;  // [q_rows][hq], natural logarithm
+  // forward split along the keys (chunk > 0): chunks of that many keys, partial
+  // results of up to part_rows rows of each block
+  int chunk, row_tiles, part_rows;
+  float *part_o, *part_ml;
   // backward
   const void *o, *o_rest, *dout;
   const float* lse_in;
@@ -73,6 +77,10 @@ struct AttnArgs {
   float *dslopes, *delta, *slope_part;
 };
 
+// Fills the split of the forward (chunk 0: none) for at most max_q queries a
+// sequence (0: unknown); returns the workspace bytes its parts need, the
+// probabilities' sums and maxima after the first *ml_at of them.
+size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at);
 hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, hipStream_t s);
 // Blocks of the pass over query rows (each leaves one partial sum per head

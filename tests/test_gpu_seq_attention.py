@@ -380,7 +380,7 @@ def test_refusals():
     for field, v in (("dtype", 2), ("heads_q", 3), ("heads_q", 0), ("heads_kv", 0), ("heads_kv", 1025), ("head_dim", 12),
                      ("head_dim", 136), ("head_dim", 0), ("reserved", 1), ("seqs", -1), ("q_rows", -1), ("q_rows", 1 << 30),
                      ("kv_rows", 1 << 31), ("q_pad", 4), ("kv_pad", 5), ("q_pad", -1), ("max_q", -2), ("q_stride", 62),
-                     ("k_stride", -4), ("v_head_stride", 1 << 31), ("scale", -1.0), ("softcap", -2.0)):
+                     ("k_stride", -4), ("v_head_stride", 1 << 23), ("scale", -1.0), ("softcap", -2.0)):
         d = R.AttnDesc(**dict(good, **{field: v}))
         assert L.seq_attention_workspace_bytes(C.byref(d), 1) == 0
         assert L.seq_attention_fwd(C.byref(d), q.data_ptr(), k.data_ptr(), k.data_ptr(), off.data_ptr(), off.data_ptr(),
