@@ -471,7 +471,8 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
  * Layout.  q [q_rows][heads_q][head_dim], k and v [kv_rows][heads_kv]
  * [head_dim]: `dtype`, head_dim contiguous, element strides of a row and of a
  * head given (so q, k and v may be column blocks of one projection); pointers
- * and strides multiples of 16 bytes, strides below 2^23 elements.  out and the gradients are contiguous.
+ * and strides multiples of 16 bytes, strides below 2^23 elements, 64 rows and
+ * a group of q's heads within 2^31 bytes.  out and the gradients are contiguous.
  * q_offsets, kv_offsets: device int64 [seqs + 1], CSR (off[0] = 0,
  * nondecreasing).  q_pad = 0: packed, sequence s is rows off[s] .. off[s + 1];
  * rows outside every sequence are neither read nor written.  q_pad > 0: padded,
@@ -485,7 +486,7 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
  * gradients are rounded to bf16 as operands of the matrix instructions. */
 typedef struct {
   int32_t dtype;     /* rs_dtype of q, k, v, out and their gradients              */
-  int32_t heads_q;   /* a multiple of heads_kv                                    */
+  int32_t heads_q;   /* a multiple of heads_kv, at most 8192                      */
   int32_t heads_kv;  /* 1 .. 1024                                                 */
   int32_t head_dim;  /* a multiple of 8 in [8, 128]                               */
   int32_t causal;

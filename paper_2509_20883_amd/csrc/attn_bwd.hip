@@ -18,96 +18,71 @@
 namespace rs {
 namespace {
 
-// delta of every row, a wave per row (0 where the row is padding).  In bf16
-// it is taken from the output and what its rounding left: where few keys
-// matter, delta is of dP's size and the output's rounding alone would be the
-// largest error of dq and dk (2.7e-3 of their norm instead of 2.4e-3, on
-// sequences of 100 to 1024 keys with distances weighed).
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_attn_delta(const AttnArgs a) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const int64_t n = a.q_rows * a.hq;
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave; r < n;
-       r += static_cast<int64_t>(gridDim.x) * (kBlock / kWave)) {
-    float s = 0.0f;
-    if (a.lse_in[r] != -INFINITY)  // a row without keys, or past its sequence's end, is not read
-      for (int i = lane; i < a.d; i += kWave) {
-        const T x = static_cast<const T*>(a.o)[r * a.d + i], y = static_cast<const T*>(a.dout)[r * a.d + i];
-        if (sizeof(T) == 2) {
-          float o = bf16_to_f32(static_cast<uint16_t>(x));
-          if (a.o_rest) o += bf16_to_f32(static_cast<const uint16_t*>(a.o_rest)[r * a.d + i]);
-          s += o * bf16_to_f32(static_cast<uint16_t>(y));
-        } else s += static_cast<float>(x) * static_cast<float>(y);
-      }
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) s += __shfl_xor(s, d, kWave);
-    if (lane == 0) a.delta[r] = s;
-  }
-}
+// Four consecutive tile rows' values from LDS.
+__device__ inline f32x4 four(const float* p, int r) { return *reinterpret_cast<const f32x4*>(p + r); }
 
-// Capped score in base 2 (and, for the gradient, the cap's derivative).
-template <typename T>
-__device__ inline float score2(float dot, float c, float inv_cap, float cap2, float& deriv) {
-  if (cap2 > 0.0f) {
-    const float th = tanh_of<T>(dot * inv_cap);
-    deriv = 1.0f - th * th;
-    return cap2 * th;
-  }
-  deriv = 1.0f;
-  return dot * c;
-}
-
+// Rows of 256 bytes and more (128 bf16, 64 fp32) leave no registers for the keys
+// beside the values and both gradients if two blocks are to share a CU, one in
+// its products while the other is in its exponentials: the keys then stay in
+// LDS, and a step takes 32 rows instead of 64 to make room for them there.
 template <typename T, int HD>
-__global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dkdv(const AttnArgs a) {
+constexpr bool kKeysInLds = HD * sizeof(T) >= 256;
+template <typename T, int HD>
+constexpr int kResidentBlocks = HD * sizeof(T) > 256 ? 1 : 2;
+
+// dk and dv of a key tile, a wave 32 keys, one per lane column.
+template <typename T, int HD>
+__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k_attn_dkdv(const AttnArgs a) {
   typedef Tile<T, HD> L;
   typedef typename Frag<T>::type F;
   constexpr int KS = HD / 16, DT = HD / 32;
-  extern __shared__ __align__(16) char lds[];
-  char* qt = lds;
-  char* dt = lds + kAttnStep * L::kRowBytes;
-  float* row_lse = reinterpret_cast<float*>(lds + 2 * kAttnStep * L::kRowBytes);  // base 2, +inf: no key seen
-  float* row_delta = row_lse + kAttnStep;
-  float* row_pos = row_delta + kAttnStep;
-  float* row_slope = row_pos + kAttnStep;
-  int* row_limit = reinterpret_cast<int*>(row_slope + kAttnStep);
+  constexpr bool kLdsKeys = kKeysInLds<T, HD>;
+  constexpr int kStep = kLdsKeys ? 32 : 64;  // rows per step
+  constexpr int kTile = kStep * L::kRowBytes;
+  __shared__ __align__(1024) char lds[4 * kTile + (kLdsKeys ? kAttnRows * L::kRowBytes : 0)];  // q, dout: two steps
+  char* key_tile = lds + 4 * kTile;
+  // of the step's rows: -lse in base 2 (-inf: no key seen, or no row), delta, position, slope, limit
+  __shared__ __align__(16) float stat[2][4][kStep];
+  __shared__ __align__(16) int stat_limit[2][kStep];
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
-  const int kvh = blockIdx.y;
+  const BlockOf blk = block_of(a.hkv, false);
+  const int kvh = blk.kvh;
   int s;
   int64_t tile;
   if (a.kv_pad > 0) {
-    const int64_t per = (a.kv_pad + kAttnRows - 1) / kAttnRows;
-    s = static_cast<int>(blockIdx.x / per);
-    tile = blockIdx.x - s * per;
+    const uint32_t per = static_cast<uint32_t>((a.kv_pad + kAttnRows - 1) / kAttnRows);
+    s = static_cast<uint32_t>(blk.tile) / per;
+    tile = blk.tile - static_cast<int64_t>(s) * per;
   } else {
-    s = find_seq(a.kv_off, a.seqs, 1, kAttnRows, blockIdx.x, tile);
+    s = find_seq(a.kv_off, a.seqs, 1, kAttnRows, blk.tile, tile);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int64_t out_rows = a.kv_pad > 0 ? a.kv_pad : ks.len;
   if (tile * kAttnRows >= out_rows) return;  // block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
-  const int rows = qs.len * a.group;
 
   const int j0 = static_cast<int>(tile) * kAttnRows;
-  const int j = j0 + wave * 32 + col;  // the lane's key
+  const int jw = j0 + wave * 32;  // the wave's first key
+  const int j = jw + col;         // the lane's key
   const bool live = j < ks.len;
-  F kf[KS], vf[KS];
+  F kf[kLdsKeys ? 1 : KS], vf[KS];
   {
     const T* k = static_cast<const T*>(a.k.p) + (ks.start + j) * a.k.row + kvh * a.k.head;
     const T* v = static_cast<const T*>(a.v.p) + (ks.start + j) * a.v.row + kvh * a.v.head;
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
       const int k0 = t * 16 + half * 8;
-      kf[t] = zero_frag<T>();
+      if (!kLdsKeys) kf[t] = zero_frag<T>();
       vf[t] = zero_frag<T>();
       if (live && k0 < a.d) {
-        load_frag(k + k0, kf[t]);
+        if (!kLdsKeys) load_frag(k + k0, kf[t]);
         load_frag(v + k0, vf[t]);
       }
     }
   }
-  const float c = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+  const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
   const float key = static_cast<float>(j);
 
   f32x16 dk[DT], dv[DT];
@@ -120,45 +95,69 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dkdv(const AttnArgs 
   int first = 0;
   if (a.causal && j0 >= prefix) first = max(0, j0 - (ks.len - qs.len));
   if (j0 >= ks.len) first = qs.len;
-  for (int r0 = first * a.group; r0 < rows; r0 += kAttnStep) {
-    __syncthreads();
-    auto addr = [&](const void* base, int64_t row, int64_t head, int i) -> const T* {
-      if (r0 + i >= rows) return nullptr;
-      const RowOf x = row_of(r0 + i, kvh, a.group);
-      return static_cast<const T*>(base) + (qs.start + x.token) * row + x.head * head;
-    };
-    stage<T, HD, kAttnStep>(qt, a.d, [&](int i) { return addr(a.q.p, a.q.row, a.q.head, i); });
-    stage<T, HD, kAttnStep>(dt, a.d, [&](int i) { return addr(a.dout, int64_t(a.hq) * a.d, a.d, i); });
-    if (threadIdx.x < kAttnStep) {
-      const int i = threadIdx.x, r = r0 + i;
-      float lse = INFINITY, delta = 0.0f, slope = 0.0f, pos = 0.0f;
-      int limit = 0;
-      if (r < rows) {
-        const RowOf x = row_of(r, kvh, a.group);
-        const int64_t at = (qs.start + x.token) * a.hq + x.head;
-        lse = a.lse_in[at] * kLog2e;
-        if (lse == -INFINITY) lse = INFINITY;
-        delta = a.delta[at];
-        pos = static_cast<float>(x.token + ks.len - qs.len);
-        limit = key_limit(x.token, qs.len, ks.len, a.causal, prefix);
-        if (a.slopes) slope = a.slopes[x.head] * kLog2e;
-      }
-      row_lse[i] = lse;
-      row_delta[i] = delta;
-      row_pos[i] = pos;
-      row_slope[i] = slope;
-      row_limit[i] = limit;
-    }
-    __syncthreads();
 
+  const RowSteps<kStep> steps(a.group);
+  RowLoader<T, HD, kStep> ql, ol;
+  ql.init(a.q, qs.start, kvh, a.group, a.d);
+  ol.init(HeadRows{a.dout, int64_t(a.hq) * a.d, a.d}, qs.start, kvh, a.group, a.d);
+  // Step n: token first + n / parts * tokens, head n % parts * kStep of the group.
+  const int n_steps = first < qs.len ? (qs.len - first + steps.tokens - 1) / steps.tokens * steps.parts : 0;
+  auto fetch = [&](int n, int buf) {
+    const int tok = first + (steps.parts > 1 ? n / steps.parts : n * steps.tokens);
+    const int head = steps.parts > 1 ? n % steps.parts * kStep : 0;
+    const int count = min(min(steps.tokens, qs.len - tok) * a.group - head, kStep);
+    ql.load(lds + buf * kTile, tok, head, count);
+    ol.load(lds + (2 + buf) * kTile, tok, head, count);
+    if (threadIdx.x < kStep) {
+      const int i = threadIdx.x;
+      float lse = -INFINITY, delta = 0.0f, pos = 0.0f, slope = 0.0f;
+      int limit = 0;
+      if (i < count) {
+        const int up = steps.parts > 1 ? 0 : div_group(i, a.group);
+        const int t = tok + up, h = kvh * a.group + head + i - up * a.group;
+        const int64_t at = (qs.start + t) * a.hq + h;
+        const float x = a.lse_in[at];
+        if (x != -INFINITY) lse = -x * kLog2e;
+        delta = a.delta[at];
+        pos = static_cast<float>(t + ks.len - qs.len);
+        limit = key_limit(t, qs.len, ks.len, a.causal, prefix);
+        if (a.slopes) slope = a.slopes[h] * kLog2e;
+      }
+      stat[buf][0][i] = lse;
+      stat[buf][1][i] = delta;
+      stat[buf][2][i] = pos;
+      stat[buf][3][i] = slope;
+      stat_limit[buf][i] = limit;
+    }
+  };
+
+  if (kLdsKeys && n_steps > 0) {  // a step needs a key: j0 < ks.len
+    TileLoader<T, HD, kAttnRows> kl;
+    kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
+    kl.load(key_tile, j0);
+  }
+  if (n_steps > 0) fetch(0, 0);
+  for (int n = 0; n < n_steps; ++n) {
+    const int buf = n & 1;
+    wait_tiles();  // this step's rows are there, the other step's have been read
+    if (n + 1 < n_steps) fetch(n + 1, buf ^ 1);
+    const int tok = first + (steps.parts > 1 ? n / steps.parts : n * steps.tokens);
+    const int last_tok = min(tok + steps.tokens, qs.len) - 1;
+    const int least = key_limit(tok, qs.len, ks.len, a.causal, prefix);
+    const int most = key_limit(last_tok, qs.len, ks.len, a.causal, prefix);
+    if (jw >= most) continue;  // wave-uniform: no row of the step sees these keys
+    const bool masked = min(jw + 32, ks.len) > least;
+    const char* qt = lds + buf * kTile;
+    const char* dt = lds + (2 + buf) * kTile;
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
+    for (int rb = 0; rb < kStep / 32; ++rb) {
       f32x16 sc = {}, dp = {};
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
         F f;
         row_frag<HD>(qt, rb * 32 + col, t * 16 + half * 8, f);
-        sc = mma(f, kf[t], sc);
+        if (kLdsKeys) row_frag<HD>(key_tile, wave * 32 + col, t * 16 + half * 8, kf[0]);
+        sc = mma(f, kf[kLdsKeys ? 0 : t], sc);
       }
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
@@ -166,16 +165,47 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dkdv(const AttnArgs 
         row_frag<HD>(dt, rb * 32 + col, t * 16 + half * 8, f);
         dp = mma(f, vf[t], dp);
       }
+      // registers 4 g .. 4 g + 3 are rows r, r + 1, r + 2, r + 3
       float p[16], ds[16];
+      const int r = rb * 32 + half * 4;
+      float c = scale2;
+      if (a.cap > 0.0f) {
+        c = cap2;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = rb * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-        float deriv;
-        float x = score2<T>(sc[i], c, inv_cap, cap2, deriv);
-        if (a.slopes) x -= row_slope[r] * fabsf(key - row_pos[r]);
-        const bool sees = j < row_limit[r];
-        p[i] = sees ? exp2_hw(x - row_lse[r]) : 0.0f;
-        ds[i] = sees ? p[i] * (dp[i] - row_delta[r]) * deriv : 0.0f;
+        for (int i = 0; i < 16; ++i) {
+          sc[i] = tanh_of<T>(sc[i] * inv_cap);
+          ds[i] = 1.0f - sc[i] * sc[i];
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 lse = four(stat[buf][0], r + g * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[4 * g + e] = sc[4 * g + e] * c + lse[e];
+      }
+      if (a.slopes) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 pos = four(stat[buf][2], r + g * 8), slope = four(stat[buf][3], r + g * 8);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - pos[e]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exp2_hw(p[i]);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = j < stat_limit[buf][r + (i >> 2) * 8 + (i & 3)] ? p[i] : 0.0f;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 delta = four(stat[buf][1], r + g * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * g + e;
+          const float x = p[i] * (dp[i] - delta[e]);
+          ds[i] = a.cap > 0.0f ? x * ds[i] : x;
+        }
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -201,38 +231,63 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dkdv(const AttnArgs 
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int d0 = i * 32 + g * 8 + half * 4;
-      if (d0 < a.d) {
-        store4(dkp + d0, dk[i][4 * g] * a.scale, dk[i][4 * g + 1] * a.scale, dk[i][4 * g + 2] * a.scale,
-               dk[i][4 * g + 3] * a.scale);
-        store4(dvp + d0, dv[i][4 * g], dv[i][4 * g + 1], dv[i][4 * g + 2], dv[i][4 * g + 3]);
+      if (d0 >= a.d) continue;
+      float x[4], y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = live ? dk[i][4 * g + e] * a.scale : 0.0f;  // padding: 0
+        y[e] = live ? dv[i][4 * g + e] : 0.0f;
       }
+      store4(dkp + d0, x[0], x[1], x[2], x[3]);
+      store4(dvp + d0, y[0], y[1], y[2], y[3]);
     }
 }
 
-// dq of a row tile, and its sum of the slopes' gradient per head.  The latter
-// is taken per row as sum_j P dP t - (sum_j P dP)(sum_j P t), t = |p - j|, all
-// fp32 from this pass's own P and dP: delta comes from the rounded output and
-// would carry its error into a sum that cancels.
+// Sum over the lane's part of a row of x y (eight elements).
+__device__ inline float dot8(const bf16x8& x, const bf16x8& y) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s += static_cast<float>(x[e]) * static_cast<float>(y[e]);
+  return s;
+}
+__device__ inline float dot8(const f32x8s& x, const f32x8s& y) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s += x.v[e] * y.v[e];
+  return s;
+}
+
+// dq of a row tile, delta of its rows (which k_attn_dkdv reads), and its sum
+// of the slopes' gradient per head.
+//
+// delta, in bf16, is taken from the output and what its rounding left: where
+// few keys matter, delta is of dP's size and the output's rounding alone would
+// be the largest error of dq and dk (2.7e-3 of their norm instead of 2.4e-3, on
+// sequences of 100 to 1024 keys with distances weighed).
+//
+// The slopes' gradient is taken per row, with x_j = P (dP - delta) and t = |p -
+// j|, as sum_j x t - (sum_j x) (sum_j P t): the sum of x is 0 but for delta's
+// own error, which would else be weighed by every distance.
 template <typename T, int HD>
-__global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dq(const AttnArgs a) {
+__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k_attn_dq(const AttnArgs a) {
   typedef Tile<T, HD> L;
   typedef typename Frag<T>::type F;
   constexpr int KS = HD / 16, DT = HD / 32;
-  extern __shared__ __align__(16) char lds[];
-  char* kt = lds;
-  char* vt = lds + kAttnStep * L::kRowBytes;
+  constexpr int kTile = kAttnStep * L::kRowBytes;
+  __shared__ __align__(1024) char lds[4 * kTile];  // keys and values, two steps of each
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
-  const int kvh = blockIdx.y;
+  const BlockOf blk = block_of(a.hkv, true);
+  const int kvh = blk.kvh;
   int s;
   int64_t tile;
   if (a.q_pad > 0) {
-    const int64_t per = (a.q_pad * a.group + kAttnRows - 1) / kAttnRows;
-    s = static_cast<int>(blockIdx.x / per);
-    tile = blockIdx.x - s * per;
+    const uint32_t per = static_cast<uint32_t>((a.q_pad * a.group + kAttnRows - 1) / kAttnRows);
+    s = static_cast<uint32_t>(blk.tile) / per;
+    tile = blk.tile - static_cast<int64_t>(s) * per;
   } else {
-    s = find_seq(a.q_off, a.seqs, a.group, kAttnRows, blockIdx.x, tile);
+    s = find_seq(a.q_off, a.seqs, a.group, kAttnRows, blk.tile, tile);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int rows = qs.len * a.group;
@@ -248,42 +303,73 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dq(const AttnArgs a)
   const int64_t row = (qs.start + me.token) * a.hq + me.head;
   const int limit = live ? key_limit(me.token, qs.len, ks.len, a.causal, prefix) : 0;
   const int last = min(r0 + kAttnRows, rows) - 1;
-  const int block_limit = !none && last >= r0 ? key_limit(last / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  const int end = !none && last >= r0 ? key_limit(div_group(last, a.group), qs.len, ks.len, a.causal, prefix) : 0;
+  const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows) - 1;
+  const int wave_least = w0 < rows ? key_limit(div_group(w0, a.group), qs.len, ks.len, a.causal, prefix) : 0;
+  const int wave_most = w1 >= w0 ? key_limit(div_group(w1, a.group), qs.len, ks.len, a.causal, prefix) : 0;
 
+  TileLoader<T, HD> kl, vl;
+  kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
+  vl.init(a.v.p, ks.start, a.v.row, kvh * a.v.head, a.d, ks.len);
+  if (end > 0) {
+    kl.load(lds, 0);
+    vl.load(lds + 2 * kTile, 0);
+  }
   F qf[KS], of[KS];
+  float delta = 0.0f;
   {
     const T* q = static_cast<const T*>(a.q.p) + (qs.start + me.token) * a.q.row + me.head * a.q.head;
-    const T* o = static_cast<const T*>(a.dout) + row * a.d;
+    const T* go = static_cast<const T*>(a.dout) + row * a.d;
+    const T* o = static_cast<const T*>(a.o) + row * a.d;
+    const T* rest = static_cast<const T*>(a.o_rest) + row * a.d;
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
       const int k0 = t * 16 + half * 8;
       qf[t] = zero_frag<T>();
       of[t] = zero_frag<T>();
       if (live && k0 < a.d) {
+        F x;
         load_frag(q + k0, qf[t]);
-        load_frag(o + k0, of[t]);
+        load_frag(go + k0, of[t]);
+        load_frag(o + k0, x);
+        delta += dot8(x, of[t]);
+        if (sizeof(T) == 2 && a.o_rest) {
+          load_frag(rest + k0, x);
+          delta += dot8(x, of[t]);
+        }
       }
     }
+    delta = other_half_sum(delta);
   }
   float lse = live ? a.lse_in[row] * kLog2e : INFINITY;
-  if (lse == -INFINITY) lse = INFINITY;
-  const float delta = live ? a.delta[row] : 0.0f;
+  if (lse == -INFINITY) {  // no key seen: P is 0
+    lse = INFINITY;
+    delta = 0.0f;
+  }
+  if (live && half == 0) a.delta[row] = delta;
   const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
+  const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
-  const float c = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+  const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
 
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-  float sum_pt = 0.0f, sum_pd = 0.0f, sum_pdt = 0.0f;
+  float sum_pt = 0.0f, sum_x = 0.0f, sum_xt = 0.0f;
 
-  const T* kp = static_cast<const T*>(a.k.p) + ks.start * a.k.row + kvh * a.k.head;
-  const T* vp = static_cast<const T*>(a.v.p) + ks.start * a.v.row + kvh * a.v.head;
-  for (int j0 = 0; j0 < block_limit; j0 += kAttnStep) {
-    __syncthreads();
-    stage<T, HD, kAttnStep>(kt, a.d, [&](int i) { return j0 + i < ks.len ? kp + (j0 + i) * a.k.row : nullptr; });
-    stage<T, HD, kAttnStep>(vt, a.d, [&](int i) { return j0 + i < ks.len ? vp + (j0 + i) * a.v.row : nullptr; });
-    __syncthreads();
+  int buf = 0;
+  for (int j0 = 0; j0 < end; j0 += kAttnStep, buf ^= 1) {
+    wait_tiles();
+    if (j0 + kAttnStep < end) {
+      kl.load(lds + (buf ^ 1) * kTile, j0 + kAttnStep);
+      vl.load(lds + (2 + (buf ^ 1)) * kTile, j0 + kAttnStep);
+    }
+    if (j0 >= wave_most) continue;  // wave-uniform
+    const bool masked = j0 + kAttnStep > wave_least;
+    const int sign = dist_sign(j0, j0 + kAttnStep - 1, wave_pos0, wave_pos1);
+    const char* kt = lds + buf * kTile;
+    const char* vt = lds + (2 + buf) * kTile;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 sc = {}, dp = {};
@@ -299,23 +385,51 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dq(const AttnArgs a)
         row_frag<HD>(vt, kb * 32 + col, t * 16 + half * 8, f);
         dp = mma(f, of[t], dp);
       }
-      float ds[16];
+      const int j = j0 + kb * 32 + half * 4;  // register i is key j + (i / 4) * 8 + i % 4
+      const float dist = static_cast<float>(j) - pos;
+      float p[16], ds[16];
+      float c = scale2;
+      if (a.cap > 0.0f) {
+        c = cap2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[i] = tanh_of<T>(sc[i] * inv_cap);
+          ds[i] = 1.0f - sc[i] * sc[i];
+        }
+      }
+      if (!a.slopes) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = sc[i] * c - lse;
+      } else if (sign != 0) {
+        const float e = sign > 0 ? slope : -slope, b = dist * e - lse;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = sc[i] * c + (e * static_cast<float>((i >> 2) * 8 + (i & 3)) + b);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          p[i] = sc[i] * c - (slope * fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3))) + lse);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exp2_hw(p[i]);
+      if (masked) {
+        const int left = limit - j;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = (i >> 2) * 8 + (i & 3) < left ? p[i] : 0.0f;
+      }
+      if (a.slope_part) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float t = fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3)));
+          const float x = p[i] * (dp[i] - delta);
+          sum_pt += p[i] * t;
+          sum_x += x;
+          sum_xt += x * t;
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int j = j0 + kb * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-        float deriv;
-        float x = score2<T>(sc[i], c, inv_cap, cap2, deriv);
-        const float t = fabsf(static_cast<float>(j) - pos);
-        if (a.slopes) x -= slope * t;
-        const bool sees = j < limit;
-        const float p = sees ? exp2_hw(x - lse) : 0.0f;
-        ds[i] = sees ? p * (dp[i] - delta) * deriv : 0.0f;
-        if (a.slope_part) {
-          const float pd = sees ? p * dp[i] : 0.0f;
-          sum_pt += p * t;
-          sum_pd += pd;
-          sum_pdt += pd * t;
-        }
+        const float x = p[i] * (dp[i] - delta);
+        ds[i] = a.cap > 0.0f ? x * ds[i] : x;
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -337,33 +451,37 @@ __global__ __launch_bounds__(kAttnWaves* kWave) void k_attn_dq(const AttnArgs a)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int d0 = i * 32 + g * 8 + half * 4;
-        if (d0 < a.d)
-          store4(dq + d0, acc[i][4 * g] * a.scale, acc[i][4 * g + 1] * a.scale, acc[i][4 * g + 2] * a.scale,
-                 acc[i][4 * g + 3] * a.scale);
+        if (d0 >= a.d) continue;
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = live ? acc[i][4 * g + e] * a.scale : 0.0f;  // padding: 0
+        store4(dq + d0, x[0], x[1], x[2], x[3]);
       }
   }
   if (a.slope_part) {
     __syncthreads();  // the tiles have been read
     float* per_row = reinterpret_cast<float*>(lds);
-    const float pt = other_half_sum(sum_pt), pd = other_half_sum(sum_pd), pdt = other_half_sum(sum_pdt);
-    if (half == 0) per_row[wave * 32 + col] = live ? pd * pt - pdt : 0.0f;
+    const float pt = other_half_sum(sum_pt), sx = other_half_sum(sum_x), sxt = other_half_sum(sum_xt);
+    if (half == 0) per_row[wave * 32 + col] = live ? sx * pt - sxt : 0.0f;
     __syncthreads();
     // rows of one head are `group` apart; every block's first row is head r0 % group
     for (int g = threadIdx.x; g < a.group; g += kAttnWaves * kWave) {
       float sum = 0.0f;
       for (int i = (g - r0 % a.group + a.group) % a.group; i < kAttnRows; i += a.group) sum += per_row[i];
-      a.slope_part[static_cast<int64_t>(blockIdx.x) * a.hq + kvh * a.group + g] = sum;
+      a.slope_part[blk.tile * a.hq + kvh * a.group + g] = sum;
     }
   }
 }
 
 // Adds up the row tiles' parts of the slopes' gradient, a block per head.
-__global__ __launch_bounds__(kBlock) void k_attn_dslopes(const AttnArgs a, int64_t tiles) {
-  __shared__ double sh[kBlock];
+constexpr int kSlopeThreads = 1024;
+__global__ __launch_bounds__(kSlopeThreads) void k_attn_dslopes(const AttnArgs a, int64_t tiles) {
+  __shared__ double sh[kSlopeThreads];
   double s = 0.0;
-  for (int64_t t = threadIdx.x; t < tiles; t += kBlock) s += a.slope_part[t * a.hq + blockIdx.x];
+#pragma unroll 8
+  for (int64_t t = threadIdx.x; t < tiles; t += kSlopeThreads) s += a.slope_part[t * a.hq + blockIdx.x];
   sh[threadIdx.x] = s;
-  for (int w = kBlock / 2; w > 0; w >>= 1) {
+  for (int w = kSlopeThreads / 2; w > 0; w >>= 1) {
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < w) sh[threadIdx.x] += sh[threadIdx.x + w];
   }
@@ -378,12 +496,10 @@ int64_t key_tiles(const AttnArgs& a) {
 
 template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
-  const size_t lds = 2 * kAttnStep * Tile<T, HD>::kRowBytes;
-  const dim3 kg(static_cast<unsigned>(key_tiles(a)), a.hkv), qg(static_cast<unsigned>(attn_row_tiles(a)), a.hkv);
-  if (a.q_rows > 0) k_attn_delta<T><<<grid_for(a.q_rows * a.hq, kBlock / kWave, 1 << 16), kBlock, 0, s>>>(a);
-  if (kg.x > 0) k_attn_dkdv<T, HD><<<kg, kAttnWaves * kWave, lds + 5 * 4 * kAttnStep, s>>>(a);
-  if (qg.x > 0) k_attn_dq<T, HD><<<qg, kAttnWaves * kWave, lds, s>>>(a);
-  if (a.dslopes) k_attn_dslopes<<<a.hq, kBlock, 0, s>>>(a, qg.x);
+  const int64_t kt = key_tiles(a), qt = attn_row_tiles(a);
+  if (qt > 0) k_attn_dq<T, HD><<<static_cast<unsigned>(qt * a.hkv), kAttnWaves * kWave, 0, s>>>(a);
+  if (kt > 0) k_attn_dkdv<T, HD><<<static_cast<unsigned>(kt * a.hkv), kAttnWaves * kWave, 0, s>>>(a);
+  if (a.dslopes) k_attn_dslopes<<<a.hq, kSlopeThreads, 0, s>>>(a, qt);
   return hipGetLastError();
 }
 

@@ -166,6 +166,13 @@ __device__ inline void col_frag(const char* tile, int r0, int c0, int lane, f32x
   }
 }
 
+// Where the distances |p - j| of a tile all have one sign, the distance term is
+// linear in j and needs one operation with the register's constant instead of
+// three: +1 if every key lies at or before every position, -1 if at or after.
+__device__ inline int dist_sign(int first_key, int last_key, int least_pos, int most_pos) {
+  return last_key <= least_pos ? 1 : first_key >= most_pos ? -1 : 0;
+}
+
 // The value of the lane's column in the other half of the wave.
 __device__ inline float other_half_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -239,6 +246,32 @@ __device__ inline int find_seq(const int64_t* __restrict__ off, int seqs, int mu
   return lo;
 }
 
+// r / group; most models have one query head per key head, or a power of two.
+__device__ inline int div_group(int r, int group) {
+  if ((group & (group - 1)) == 0) return r >> (31 - __builtin_clz(group));  // uniform
+  return r / group;
+}
+
+// A one-dimensional grid of tiles times key heads.  Neighbouring tiles read the
+// same keys (or rows), so runs of kTileRun consecutive tiles of one key head go
+// to one XCD and its L2; `back` takes the tiles from the last, which see the
+// most keys under a causal mask, to the first, so that the short ones fill in
+// at the end.
+constexpr uint32_t kTileRun = 8;
+struct BlockOf {
+  int64_t tile;
+  int kvh;
+};
+__device__ inline BlockOf block_of(int hkv, bool back) {
+  const uint32_t tiles = gridDim.x / hkv;
+  uint32_t b = xcd_runs<kTileRun>(blockIdx.x, gridDim.x);
+  if (back) b = gridDim.x - 1 - b;
+  BlockOf x;
+  x.kvh = b / tiles;
+  x.tile = b - x.kvh * tiles;
+  return x;
+}
+
 // Rows of a sequence are packed head by head: row r is token r / group, query
 // head kvh * group + r % group, so that the query heads of a key head share
 // its tiles.  Row r sees the keys j < limit.
@@ -247,7 +280,7 @@ struct RowOf {
 };
 __device__ inline RowOf row_of(int r, int kvh, int group) {
   RowOf x;
-  x.token = r / group;
+  x.token = div_group(r, group);
   x.head = kvh * group + (r - x.token * group);
   return x;
 }
@@ -256,16 +289,16 @@ __device__ inline int key_limit(int token, int lq, int lk, bool causal, int pref
   return min(lk, max(token + lk - lq + 1, prefix));
 }
 
-// Rows of a [rows][heads][d] tensor to an LDS tile of kAttnStep rows, by loads
+// Rows of a [rows][heads][d] tensor to an LDS tile of N rows, by loads
 // that write LDS themselves (16 bytes per lane, a wave's 1 KiB back to back):
 // no registers hold them and the wave goes on; wait_tiles() before their use.
 // The lane picks the chunk that belongs at its place, so the tile's chunk
 // order costs nothing.  The buffer's bounds do the masking: rows past the
 // sequence's end and columns past d lie outside and arrive as zeros.
-template <typename T, int HD>
+template <typename T, int HD, int N = kAttnStep>
 struct TileLoader {
   typedef Tile<T, HD> L;
-  static constexpr int kLoads = kAttnStep * L::kRowBytes / (kAttnWaves * kWave * 16);  // per thread
+  static constexpr int kLoads = N * L::kRowBytes / (kAttnWaves * kWave * 16);  // per thread
   uint32_t off[kLoads];  // byte offset of the thread's chunks from the tile's first row
   int64_t row_bytes;
   const char* base;  // the sequence's first row
@@ -281,14 +314,14 @@ struct TileLoader {
     for (int i = 0; i < kLoads; ++i) {
       const int at = ((wave * kLoads + i) * kWave + lane) * 16;
       const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(r);
-      off[i] = c * 16 < d_bytes ? static_cast<uint32_t>(r * row_bytes) + c * 16 : 0x80000000u;
+      off[i] = c * 16 < d_bytes ? r * static_cast<uint32_t>(row_bytes) + c * 16 : 0x80000000u;
     }
   }
-  // Rows j0 .. j0 + kAttnStep - 1 of the sequence (j0 < len).
+  // Rows j0 .. j0 + N - 1 of the sequence (j0 < len).
   __device__ inline void load(char* tile, int j0) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass has no buffer descriptors
-    const int rows = min(kAttnStep, len - j0);
-    const int bytes = static_cast<int>(max(rows - 1, 0) * row_bytes) + d_bytes;
+    const int rows = min(N, len - j0);
+    const int bytes = max(rows - 1, 0) * static_cast<int>(row_bytes) + d_bytes;
     const char* p = base + j0 * row_bytes;
     const uint64_t u = reinterpret_cast<uint64_t>(p);
     // readfirstlane gives a signed int: no sign may reach the upper word
@@ -306,32 +339,75 @@ struct TileLoader {
   }
 };
 
+// The same for packed query rows, a step of N rows of whole tokens: floor(N /
+// group) tokens with all their heads, or where a group has more than N heads,
+// N of one token's.  The offsets inside a step never change; rows past the step's
+// tokens or the sequence's end are sent out of the buffer's bounds.
+template <int N>
+struct RowSteps {
+  int tokens, parts;  // tokens per step, steps per token (one of them is 1)
+  __device__ inline explicit RowSteps(int g) : tokens(g <= N ? N / g : 1), parts(g <= N ? 1 : (g + N - 1) / N) {}
+};
+template <typename T, int HD, int N>
+struct RowLoader {
+  typedef Tile<T, HD> L;
+  static constexpr int kLoads = N * L::kRowBytes / (kAttnWaves * kWave * 16);
+  uint32_t off[kLoads];
+  int64_t row_bytes, head_bytes;
+  const char* base;  // the sequence's first token, the group's first head
+
+  __device__ inline void init(const HeadRows& t, int64_t start, int kvh, int group, int d) {
+    row_bytes = t.row * static_cast<int64_t>(sizeof(T));
+    head_bytes = t.head * static_cast<int64_t>(sizeof(T));
+    base = static_cast<const char*>(t.p) + start * row_bytes + static_cast<int64_t>(kvh) * group * head_bytes;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = ((wave * kLoads + i) * kWave + lane) * 16;
+      const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(r);
+      const int tok = group <= N ? div_group(r, group) : 0;
+      off[i] = c * 16 < d * static_cast<int>(sizeof(T))
+                   ? tok * static_cast<uint32_t>(row_bytes) + (r - tok * group) * static_cast<uint32_t>(head_bytes) + c * 16
+                   : 0x80000000u;
+    }
+  }
+  // The step from token `tok`, head `head` of the group; `count` rows of it exist.
+  __device__ inline void load(char* tile, int tok, int head, int count) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const char* p = base + tok * row_bytes + head * head_bytes;
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0, 0x7FFFFFFF, 0x00020000);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
+    char* dst = tile + wave * kLoads * kWave * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = ((wave * kLoads + i) * kWave + lane) * 16 / L::kRowBytes;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc, (__attribute__((address_space(3))) void*)(dst + i * kWave * 16), 16, r < count ? off[i] : 0x80000000u, 0,
+          0, 0);
+    }
+#endif
+  }
+};
+
 // Every load of the wave has arrived, and then every wave's.
 __device__ inline void wait_tiles() {
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 }
 
-// Copies rows of a [rows][heads][d] tensor to an LDS tile of N rows through
-// registers, zero where addr(r) is null and past column d.
-template <typename T, int HD, int N, typename F>
-__device__ inline void stage(char* tile, int d, F addr) {
-  typedef Tile<T, HD> L;
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-  for (int i = 0; i < N * L::kChunks / (kAttnWaves * kWave); ++i) {
-    const int idx = threadIdx.x + i * kAttnWaves * kWave;
-    const int r = idx / L::kChunks, c = idx % L::kChunks;
-    const T* p = addr(r);
-    u32x4 v = {0, 0, 0, 0};
-    if (p && c * L::kPer < d) v = *reinterpret_cast<const u32x4*>(p + c * L::kPer);
-    *reinterpret_cast<u32x4*>(tile + L::at(r, c)) = v;
-  }
-}
-
-// What rounding x to bf16 takes away.
-__device__ inline float rest_bf16(float x) {
-  return x - __uint_as_float(pack_bf16(0.0f, x) & 0xFFFF0000u);
+// Four elements of an output row, and what rounding them to bf16 took.
+__device__ inline void store4_rest(uint16_t* p, uint16_t* rest, float a, float b, float c, float d) {
+  const uint2 w = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+  *reinterpret_cast<uint2*>(p) = w;
+  a -= __uint_as_float(w.x << 16);
+  b -= __uint_as_float(w.x & 0xFFFF0000u);
+  c -= __uint_as_float(w.y << 16);
+  d -= __uint_as_float(w.y & 0xFFFF0000u);
+  *reinterpret_cast<uint2*>(rest) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
 
 // Four consecutive elements of an output row from registers 4 i .. 4 i + 3.

@@ -38,15 +38,20 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
-  const int kvh = blockIdx.y;
+  int kvh = blockIdx.y;
   int s;
   int64_t tile;
   int c0 = 0;  // the block's first key
+  BlockOf blk{};
+  if (!SPLIT) {
+    blk = block_of(a.hkv, true);
+    kvh = blk.kvh;
+  }
   if (SPLIT) {
     int64_t c;
     if (a.kv_pad > 0) {
-      const int64_t per = (a.kv_pad + a.chunk - 1) / a.chunk;
-      s = static_cast<int>(blockIdx.x / per);
+      const uint32_t per = static_cast<uint32_t>(a.kv_pad + a.chunk - 1) / a.chunk;
+      s = blockIdx.x / per;
       c = blockIdx.x - s * per;
     } else {
       s = find_seq(a.kv_off, a.seqs, 1, a.chunk, blockIdx.x, c);
@@ -55,11 +60,11 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     if (c * a.chunk >= int64_t(1) << 31) return;
     c0 = static_cast<int>(c) * a.chunk;
   } else if (a.q_pad > 0) {
-    const int64_t per = (a.q_pad * a.group + kAttnRows - 1) / kAttnRows;
-    s = static_cast<int>(blockIdx.x / per);
-    tile = blockIdx.x - s * per;
+    const uint32_t per = static_cast<uint32_t>((a.q_pad * a.group + kAttnRows - 1) / kAttnRows);
+    s = static_cast<uint32_t>(blk.tile) / per;
+    tile = blk.tile - static_cast<int64_t>(s) * per;
   } else {
-    s = find_seq(a.q_off, a.seqs, a.group, kAttnRows, blockIdx.x, tile);
+    s = find_seq(a.q_off, a.seqs, a.group, kAttnRows, blk.tile, tile);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int rows = qs.len * a.group;  // the others of a padded sequence have no key
@@ -74,15 +79,15 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   const int limit = live ? key_limit(me.token, qs.len, ks.len, a.causal, prefix) : 0;
   // limits do not fall along the rows: the last row sees the most keys
   const int last = min(r0 + kAttnRows, rows) - 1;
-  int end = last >= r0 ? key_limit(last / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  int end = last >= r0 ? key_limit(div_group(last, a.group), qs.len, ks.len, a.causal, prefix) : 0;
   const bool joined = SPLIT && ks.len > a.chunk;  // other blocks hold parts of these rows
   if (SPLIT) {
     if (c0 > 0 && c0 >= end) return;  // block-uniform; the join does not look here
     end = min(end, c0 + a.chunk);
   }
   const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows) - 1;
-  const int wave_least = w0 < rows ? key_limit(w0 / a.group, qs.len, ks.len, a.causal, prefix) : 0;
-  const int wave_most = w1 >= w0 ? key_limit(w1 / a.group, qs.len, ks.len, a.causal, prefix) : 0;
+  const int wave_least = w0 < rows ? key_limit(div_group(w0, a.group), qs.len, ks.len, a.causal, prefix) : 0;
+  const int wave_most = w1 >= w0 ? key_limit(div_group(w1, a.group), qs.len, ks.len, a.causal, prefix) : 0;
 
   TileLoader<T, HD> kl, vl;
   kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
@@ -102,16 +107,16 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     }
   }
   const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
+  const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
   const float inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e, scale2 = a.scale * kLog2e;
-  // scores without cap and slope are scaled inside the exponent
-  const bool plain = !(a.cap > 0.0f) && !a.slopes;
-  const float c = plain ? scale2 : 1.0f;
-
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-  float m = -INFINITY, l = 0.0f;
+  // the running maximum in base 2 and the height above it at which it moves:
+  // any, while no key has been seen
+  float m = 0.0f, move = -INFINITY, l = 0.0f;
 
   int buf = 0;
   for (int j0 = c0; j0 < end; j0 += kAttnStep, buf ^= 1) {
@@ -137,26 +142,37 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[kb][i] = sc[i];
     }
+    // in base 2, relative to the running maximum
     const int j = j0 + half * 4;  // register i of block kb is key j + kb * 32 + (i / 4) * 8 + i % 4
-    if (!plain) {
-      if (a.cap > 0.0f) {
+    float c = scale2;
+    if (a.cap > 0.0f) {
+      c = cap2;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) p[kb][i] = cap2 * tanh_of<T>(p[kb][i] * inv_cap);
-      } else {
+        for (int i = 0; i < 16; ++i) p[kb][i] = tanh_of<T>(p[kb][i] * inv_cap);
+    }
+    if (!a.slopes) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) p[kb][i] *= scale2;
-      }
-      if (a.slopes) {
-        const float dist = static_cast<float>(j) - pos;
+        for (int i = 0; i < 16; ++i) p[kb][i] = p[kb][i] * c - m;
+    } else {
+      const float dist = static_cast<float>(j) - pos;
+      const int sign = dist_sign(j0, j0 + kAttnStep - 1, wave_pos0, wave_pos1);
+      if (sign != 0) {
+        const float e = sign > 0 ? slope : -slope, b = dist * e - m;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            p[kb][i] -= slope * fabsf(dist + static_cast<float>(kb * 32 + (i >> 2) * 8 + (i & 3)));
+            p[kb][i] = p[kb][i] * c + (e * static_cast<float>(kb * 32 + (i >> 2) * 8 + (i & 3)) + b);
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            p[kb][i] = p[kb][i] * c - (slope * fabsf(dist + static_cast<float>(kb * 32 + (i >> 2) * 8 + (i & 3))) + m);
       }
     }
     if (j0 + kAttnStep > wave_least) {
@@ -172,25 +188,30 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
-    top = other_half_max(top) * c;
+    top = other_half_max(top);
     // the running maximum moves only when a score passes it by 2^8: until then
     // the probabilities are larger than 1 by at most that, which neither fp32
     // sums nor bf16's relative rounding notice
-    if (__any(top > m + 8.0f)) {
-      const float next = fmaxf(m, top);
-      const float alpha = exp2_hw(next == -INFINITY ? 0.0f : m - next);
-      m = next;
+    if (__any(top > move)) {
+      const bool up = top > move;
+      const float by = up ? top : 0.0f;
+      const float alpha = move == -INFINITY ? 0.0f : exp2_hw(-by);
+      m += by;
+      move = up ? 8.0f : move;
       l *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i) acc[i] *= alpha;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[kb][i] -= by;
     }
-    const float base = m == -INFINITY ? 0.0f : m;  // no key seen yet
     float sum = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        p[kb][i] = exp2_hw(p[kb][i] * c - base);
+        p[kb][i] = exp2_hw(p[kb][i]);
         sum += p[kb][i];
       }
     l += sum;  // this half's keys
@@ -238,10 +259,13 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
       float x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : acc[i][4 * g + e] * inv;
+      if constexpr (sizeof(T) == 2) {
+        if (a.rest && live) {
+          store4_rest(out + d0, static_cast<uint16_t*>(a.rest) + row * a.d + d0, x[0], x[1], x[2], x[3]);
+          continue;
+        }
+      }
       store4(out + d0, x[0], x[1], x[2], x[3]);
-      if (sizeof(T) == 2 && a.rest)
-        store4(static_cast<uint16_t*>(a.rest) + row * a.d + d0, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]),
-               rest_bf16(x[3]));
     }
   if (a.lse && half == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
 }
@@ -277,7 +301,10 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
 
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   float m = -INFINITY;
-  for (int c = threadIdx.x; c < chunks; c += kBlock) m = fmaxf(m, ml[slot0 + c * step].x);
+  for (int c = threadIdx.x; c < chunks; c += kBlock) {
+    const float2 x = ml[slot0 + c * step];
+    m = fmaxf(m, x.y == 0.0f ? -INFINITY : x.x);  // a part may see no key
+  }
 #pragma unroll
   for (int d = kWave / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
   if ((threadIdx.x & (kWave - 1)) == 0) sh_m[threadIdx.x / kWave] = m;
@@ -296,7 +323,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
       const int64_t slot = slot0 + c * step;
       const float2 x = ml[slot];
       const float4 y = *reinterpret_cast<const float4*>(a.part_o + slot * a.d + 4 * q);
-      const float w = exp2_hw(x.x - base);
+      const float w = x.y == 0.0f ? 0.0f : exp2_hw(x.x - base);
       l += w * x.y;
       o.x += w * y.x;
       o.y += w * y.y;
@@ -320,10 +347,13 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
   const float inv = none ? 0.0f : 1.0f / l;
   const int64_t row = (qs.start + token) * a.hq + head;
   const float x[4] = {none ? 0.0f : o.x * inv, none ? 0.0f : o.y * inv, none ? 0.0f : o.z * inv, none ? 0.0f : o.w * inv};
-  store4(static_cast<T*>(a.out) + row * a.d + 4 * q, x[0], x[1], x[2], x[3]);
-  if (sizeof(T) == 2 && a.rest)
-    store4(static_cast<uint16_t*>(a.rest) + row * a.d + 4 * q, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]),
-           rest_bf16(x[3]));
+  T* out = static_cast<T*>(a.out) + row * a.d + 4 * q;
+  if constexpr (sizeof(T) == 2) {
+    if (a.rest) store4_rest(out, static_cast<uint16_t*>(a.rest) + row * a.d + 4 * q, x[0], x[1], x[2], x[3]);
+    else store4(out, x[0], x[1], x[2], x[3]);
+  } else {
+    store4(out, x[0], x[1], x[2], x[3]);
+  }
   if (a.lse && q == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
 }
 
@@ -340,8 +370,8 @@ hipError_t run(const AttnArgs& a, hipStream_t s) {
     const dim3 jg(static_cast<unsigned>(a.q_pad > 0 ? a.q_rows : a.q_rows + a.seqs), a.hq);
     k_attn_join<T><<<jg, kBlock, 0, s>>>(a);
   } else {
-    const dim3 rows(static_cast<unsigned>(attn_row_tiles(a)), a.hkv);
-    k_attn_fwd<T, HD, false><<<rows, kAttnWaves * kWave, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(attn_row_tiles(a) * a.hkv);
+    k_attn_fwd<T, HD, false><<<grid, kAttnWaves * kWave, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -364,13 +394,17 @@ int64_t attn_row_tiles(const AttnArgs& a) {
 // Split where the row tiles alone are fewer blocks than the GPU runs at once
 // twice over, into about kSplitBlocks, of at least kLeastChunk keys.
 constexpr int64_t kFewBlocks = 1024, kSplitBlocks = 2048, kLeastChunk = 256;
+// Short sequences on the average are not split (nothing to join: 64 sessions of
+// up to 50 keys 7.6 + 3.5 -> 7.6 us) unless the keys are many enough for a long
+// one among them to matter.
+constexpr int64_t kShortKeyRows = 8192;
 
 size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at) {
   a->chunk = 0;
   *ml_at = 0;
   if (a->seqs == 0 || a->q_rows == 0 || attn_row_tiles(*a) * a->hkv >= kFewBlocks) return 0;
   const int64_t most_keys = a->kv_pad > 0 ? a->kv_pad : a->kv_rows;  // of one sequence
-  if (most_keys < 2 * kLeastChunk) return 0;
+  if (most_keys < 2 * kLeastChunk || (a->kv_rows < kShortKeyRows && a->kv_rows / a->seqs < kLeastChunk)) return 0;
   int64_t most_q = a->q_pad > 0 ? a->q_pad : a->q_rows;
   if (a->q_pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
   const int64_t tiles = (most_q * a->group + kAttnRows - 1) / kAttnRows;

@@ -2,6 +2,7 @@
 // argument checks, workspace layout and dispatch to the kernels.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -35,13 +36,21 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// An upper bound of the blocks of any launch.
+int64_t attn_blocks(const rs_attn_desc& d) {
+  const int64_t group = d.heads_q / d.heads_kv;
+  const int64_t q = d.q_pad > 0 ? d.seqs * (d.q_pad * group / 128 + 1) : d.q_rows * group / 128 + d.seqs;
+  const int64_t k = d.kv_pad > 0 ? d.seqs * (d.kv_pad / 128 + 1) : d.kv_rows / 128 + d.seqs;
+  return std::max(q, k) * d.heads_kv;
+}
+
 // What is wrong with a descriptor, or null.
 const char* check_attn(const rs_attn_desc* d) {
   if (!d) return "null descriptor";
   if (!valid_dtype(d->dtype)) return "bad dtype";
   if (d->heads_kv < 1 || d->heads_kv > 1024) return "heads_kv must be in [1, 1024]";
-  if (d->heads_q < d->heads_kv || d->heads_q > 65536 || d->heads_q % d->heads_kv != 0)
-    return "heads_q must be a multiple of heads_kv, at most 65536";
+  if (d->heads_q < d->heads_kv || d->heads_q > 8192 || d->heads_q % d->heads_kv != 0)
+    return "heads_q must be a multiple of heads_kv, at most 8192";
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8 != 0) return "head_dim must be a multiple of 8 in [8, 128]";
   if (d->reserved != 0) return "reserved must be 0";
   constexpr int64_t kMost = int64_t(1) << 31;
@@ -56,6 +65,11 @@ const char* check_attn(const rs_attn_desc* d) {
   for (const int64_t st : {d->q_stride, d->q_head_stride, d->k_stride, d->k_head_stride, d->v_stride, d->v_head_stride})
     if (st < 0 || st >= (int64_t(1) << 23) || st % unit != 0)
       return "strides must be multiples of 16 bytes in [0, 2^23) elements";
+  // a step of 64 packed rows is addressed with 32 bits
+  const int64_t es = d->dtype == RS_BF16 ? 2 : 4;
+  if ((64 * d->q_stride + d->heads_q / d->heads_kv * d->q_head_stride) * es >= kMost)
+    return "64 rows and a group of heads of q must span less than 2^31 bytes";
+  if (attn_blocks(*d) >= kMost) return "too many sequences and rows for one launch";
   if (!(d->scale > 0.0) || !std::isfinite(d->scale)) return "scale must be finite and > 0";
   if (!(d->softcap >= 0.0) || !std::isfinite(d->softcap)) return "softcap must be finite and >= 0";
   return nullptr;

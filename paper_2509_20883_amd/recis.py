@@ -484,7 +484,8 @@ class SeqAttention:
             raise RecisError(EINVAL, f"{what} must be [rows, heads, d] or [seqs, pad, heads, d]")
         unit = 16 // t.element_size()
         st = t.stride()
-        if (st[-1] != 1 or st[-2] % unit or st[-3] % unit or max(st[-2], st[-3]) >= 1 << 23 or (t.dim() == 4 and st[0] != t.shape[1] * st[1]) or
+        if (st[-1] != 1 or st[-2] % unit or st[-3] % unit or max(st[-2], st[-3]) >= 1 << 23 or
+                64 * st[-3] + t.shape[-2] * st[-2] >= 1 << 29 or (t.dim() == 4 and st[0] != t.shape[1] * st[1]) or
                 t.data_ptr() % 16):
             t = _packed(t)
             st = t.stride()
