@@ -222,25 +222,19 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     }
   }
 
-  if (j >= out_rows) return;
-  const int64_t row = (ks.start + j) * a.hkv + kvh;
-  T* dkp = static_cast<T*>(a.dk) + row * a.d;
-  T* dvp = static_cast<T*>(a.dv) + row * a.d;
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d0 = i * 32 + g * 8 + half * 4;
-      if (d0 >= a.d) continue;
-      float x[4], y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = live ? dk[i][4 * g + e] * a.scale : 0.0f;  // padding: 0
-        y[e] = live ? dv[i][4 * g + e] : 0.0f;
-      }
-      store4(dkp + d0, x[0], x[1], x[2], x[3]);
-      store4(dvp + d0, y[0], y[1], y[2], y[3]);
-    }
+  typedef RowWriter<T, HD> S;
+  constexpr int kShare = sizeof(lds) / kAttnWaves;
+  static_assert(S::kBytes <= kShare, "a wave's rows fit its share of the tiles");
+  __syncthreads();  // the tiles have been read
+  char* mine = lds + wave * kShare;
+  auto at = [&](void* base, int i) -> T* {
+    if (jw + i >= out_rows) return nullptr;
+    return static_cast<T*>(base) + ((ks.start + jw + i) * a.hkv + kvh) * a.d;
+  };
+  S::put(mine, lane, [&](int i, int e) { return live ? dk[i][e] * a.scale : 0.0f; });  // padding: 0
+  S::flush(mine, lane, a.d, [&](int i) { return at(a.dk, i); });
+  S::put(mine, lane, [&](int i, int e) { return live ? dv[i][e] : 0.0f; });
+  S::flush(mine, lane, a.d, [&](int i) { return at(a.dv, i); });
 }
 
 // Sum over the lane's part of a row of x y (eight elements).
@@ -444,22 +438,20 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     }
   }
 
-  if (!none && r < out_rows) {
-    T* dq = static_cast<T*>(a.dq) + row * a.d;
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d0 = i * 32 + g * 8 + half * 4;
-        if (d0 >= a.d) continue;
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = live ? acc[i][4 * g + e] * a.scale : 0.0f;  // padding: 0
-        store4(dq + d0, x[0], x[1], x[2], x[3]);
-      }
+  typedef RowWriter<T, HD> S;
+  static_assert(S::kBytes <= kTile, "a wave's rows fit its share of the tiles");
+  __syncthreads();  // the tiles have been read
+  if (!none) {
+    char* mine = lds + wave * kTile;
+    S::put(mine, lane, [&](int i, int e) { return live ? acc[i][e] * a.scale : 0.0f; });  // padding: 0
+    S::flush(mine, lane, a.d, [&](int i) -> T* {
+      if (w0 + i >= out_rows) return nullptr;
+      const RowOf x = row_of(w0 + i, kvh, a.group);
+      return static_cast<T*>(a.dq) + ((qs.start + x.token) * a.hq + x.head) * a.d;
+    });
   }
   if (a.slope_part) {
-    __syncthreads();  // the tiles have been read
+    __syncthreads();  // the rows have been read
     float* per_row = reinterpret_cast<float*>(lds);
     const float pt = other_half_sum(sum_pt), sx = other_half_sum(sum_x), sxt = other_half_sum(sum_xt);
     if (half == 0) per_row[wave * 32 + col] = live ? sx * pt - sxt : 0.0f;

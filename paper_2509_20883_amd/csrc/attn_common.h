@@ -399,15 +399,9 @@ __device__ inline void wait_tiles() {
   __syncthreads();
 }
 
-// Four elements of an output row, and what rounding them to bf16 took.
-__device__ inline void store4_rest(uint16_t* p, uint16_t* rest, float a, float b, float c, float d) {
-  const uint2 w = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
-  *reinterpret_cast<uint2*>(p) = w;
-  a -= __uint_as_float(w.x << 16);
-  b -= __uint_as_float(w.x & 0xFFFF0000u);
-  c -= __uint_as_float(w.y << 16);
-  d -= __uint_as_float(w.y & 0xFFFF0000u);
-  *reinterpret_cast<uint2*>(rest) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+// What rounding to bf16 takes away from x.
+__device__ inline float rest_bf16(float x) {
+  return x - __uint_as_float(pack_bf16(x, 0.0f) << 16);
 }
 
 // Four consecutive elements of an output row from registers 4 i .. 4 i + 3.
@@ -417,5 +411,39 @@ __device__ inline void store4(uint16_t* p, float a, float b, float c, float d) {
 __device__ inline void store4(float* p, float a, float b, float c, float d) {
   *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
 }
+
+// A wave's 32 output rows, one per lane column, through LDS: a lane holds four
+// elements of a row at a time, and storing them as they lie would send 32
+// requests of 16 bytes per instruction to L2 (half the time of the forward on
+// sequences of 560 keys of 64); from LDS, consecutive lanes store whole rows.
+template <typename T, int HD>
+struct RowWriter {
+  static constexpr int kStride = HD * sizeof(T) + 16;  // rows start on other banks
+  static constexpr int kBytes = 32 * kStride;
+  // value(i, e): the lane's element of register e (0 .. 15) of column tile i
+  template <typename V>
+  __device__ static inline void put(char* region, int lane, V value) {
+    char* row = region + (lane & 31) * kStride + (lane >> 5) * 4 * sizeof(T);
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        store4(reinterpret_cast<T*>(row) + i * 32 + g * 8, value(i, 4 * g), value(i, 4 * g + 1), value(i, 4 * g + 2),
+               value(i, 4 * g + 3));
+  }
+  // at(row): where row 0 .. 31 goes, or null
+  template <typename A>
+  __device__ static inline void flush(const char* region, int lane, int d, A at) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kPer = 16 / sizeof(T), kChunks = HD / kPer;
+#pragma unroll
+    for (int n = 0; n < 32 * kChunks / kWave; ++n) {
+      const int idx = n * kWave + lane, r = idx / kChunks, c = idx % kChunks;
+      T* p = at(r);
+      if (p && c * kPer < d)
+        *reinterpret_cast<u32x4*>(p + c * kPer) = *reinterpret_cast<const u32x4*>(region + r * kStride + c * 16);
+    }
+  }
+};
 
 }  // namespace rs

@@ -229,11 +229,10 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
       }
   }
 
-  if (r >= out_rows) return;
   l = other_half_sum(l);
   if (joined) {
     const int at = wave * 32 + col;
-    if (at >= a.part_rows) return;
+    if (r >= out_rows || at >= a.part_rows) return;
     const int64_t slot = ((static_cast<int64_t>(blockIdx.x) * a.hkv + kvh) * a.row_tiles + tile) * a.part_rows + at;
     float* po = a.part_o + slot * a.d;
 #pragma unroll
@@ -248,26 +247,27 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   }
   const bool none = !live || l == 0.0f;  // no key: 0 (a NaN sum stays)
   const float inv = none ? 0.0f : 1.0f / l;
-  const int64_t row = (qs.start + me.token) * a.hq + me.head;
-  T* out = static_cast<T*>(a.out) + row * a.d;
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d0 = i * 32 + g * 8 + half * 4;
-      if (d0 >= a.d) continue;
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : acc[i][4 * g + e] * inv;
-      if constexpr (sizeof(T) == 2) {
-        if (a.rest && live) {
-          store4_rest(out + d0, static_cast<uint16_t*>(a.rest) + row * a.d + d0, x[0], x[1], x[2], x[3]);
-          continue;
-        }
-      }
-      store4(out + d0, x[0], x[1], x[2], x[3]);
-    }
-  if (a.lse && half == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
+    for (int e = 0; e < 16; ++e) acc[i][e] = none ? 0.0f : acc[i][e] * inv;
+  typedef RowWriter<T, HD> S;
+  static_assert(S::kBytes <= kTile, "a wave's rows fit its share of the tiles");
+  __syncthreads();  // the tiles have been read
+  char* mine = lds + wave * kTile;
+  S::put(mine, lane, [&](int i, int e) { return acc[i][e]; });
+  auto at = [&](void* base, int64_t end_row, int i) -> T* {
+    if (w0 + i >= end_row) return nullptr;
+    const RowOf x = row_of(w0 + i, kvh, a.group);
+    return static_cast<T*>(base) + ((qs.start + x.token) * a.hq + x.head) * a.d;
+  };
+  S::flush(mine, lane, a.d, [&](int i) { return at(a.out, out_rows, i); });
+  if (sizeof(T) == 2 && a.rest) {
+    S::put(mine, lane, [&](int i, int e) { return rest_bf16(acc[i][e]); });
+    S::flush(mine, lane, a.d, [&](int i) { return at(a.rest, rows, i); });
+  }
+  if (a.lse && half == 0 && r < out_rows)
+    a.lse[(qs.start + me.token) * a.hq + me.head] = none ? -INFINITY : m * kLn2 + logf(l);
 }
 
 // Joins the chunks of a row: a block per query token and head, threads four
@@ -347,13 +347,9 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
   const float inv = none ? 0.0f : 1.0f / l;
   const int64_t row = (qs.start + token) * a.hq + head;
   const float x[4] = {none ? 0.0f : o.x * inv, none ? 0.0f : o.y * inv, none ? 0.0f : o.z * inv, none ? 0.0f : o.w * inv};
-  T* out = static_cast<T*>(a.out) + row * a.d + 4 * q;
-  if constexpr (sizeof(T) == 2) {
-    if (a.rest) store4_rest(out, static_cast<uint16_t*>(a.rest) + row * a.d + 4 * q, x[0], x[1], x[2], x[3]);
-    else store4(out, x[0], x[1], x[2], x[3]);
-  } else {
-    store4(out, x[0], x[1], x[2], x[3]);
-  }
+  store4(static_cast<T*>(a.out) + row * a.d + 4 * q, x[0], x[1], x[2], x[3]);
+  if (sizeof(T) == 2 && a.rest)
+    store4(static_cast<T*>(a.rest) + row * a.d + 4 * q, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]), rest_bf16(x[3]));
   if (a.lse && q == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
 }
 
