@@ -18,6 +18,23 @@
 namespace rs {
 namespace {
 
+// What the pass over keys needs of a row, four arrays of q_rows * heads_q words
+// written by k_attn_dq: -lse in base 2 (-infinity: no key seen, P = 0), delta,
+// the position (an integer), the slope in base 2 (where there are slopes).
+enum : int { kStatLse = 0, kStatDelta = 1, kStatPos = 2, kStatSlope = 3, kStats = 4 };
+
+// A word per lane from p + off (bytes; past 2^31: 0) to 64 consecutive words of LDS.
+__device__ inline void load_words(const float* p, uint32_t off, float* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0, 0x7FFFFFFF, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)dst, 4, off, 0, 0, 0);
+#endif
+}
+
 // Four consecutive tile rows' values from LDS.
 __device__ inline f32x4 four(const float* p, int r) { return *reinterpret_cast<const f32x4*>(p + r); }
 
@@ -29,6 +46,10 @@ template <typename T, int HD>
 constexpr bool kKeysInLds = HD * sizeof(T) >= 256;
 template <typename T, int HD>
 constexpr int kResidentBlocks = HD * sizeof(T) > 256 ? 1 : 2;
+// The dq pass holds one gradient, and up to 128 bytes a row three blocks fit
+// (padded sequences of 560 keys of 64: 990 us with two, 809 with three).
+template <typename T, int HD>
+constexpr int kResidentRowBlocks = HD * sizeof(T) <= 128 ? 3 : kResidentBlocks<T, HD>;
 
 // dk and dv of a key tile, a wave 32 keys, one per lane column.
 template <typename T, int HD>
@@ -41,9 +62,8 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   constexpr int kTile = kStep * L::kRowBytes;
   __shared__ __align__(1024) char lds[4 * kTile + (kLdsKeys ? kAttnRows * L::kRowBytes : 0)];  // q, dout: two steps
   char* key_tile = lds + 4 * kTile;
-  // of the step's rows: -lse in base 2 (-inf: no key seen, or no row), delta, position, slope, limit
-  __shared__ __align__(16) float stat[2][4][kStep];
-  __shared__ __align__(16) int stat_limit[2][kStep];
+  // of the step's rows, as k_attn_dq left them; 0 where there is no row: its q and dout are 0 too, and add nothing
+  __shared__ __align__(16) float stat[2][kStats][kWave];
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
@@ -84,6 +104,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   }
   const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
   const float key = static_cast<float>(j);
+  const int see_all = a.causal ? prefix : ks.len;  // keys that every row sees
 
   f32x16 dk[DT], dv[DT];
 #pragma unroll
@@ -102,32 +123,20 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   ol.init(HeadRows{a.dout, int64_t(a.hq) * a.d, a.d}, qs.start, kvh, a.group, a.d);
   // Step n: token first + n / parts * tokens, head n % parts * kStep of the group.
   const int n_steps = first < qs.len ? (qs.len - first + steps.tokens - 1) / steps.tokens * steps.parts : 0;
+  const bool first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) == 0;
+  const int stat_up = steps.parts > 1 ? 0 : div_group(lane, a.group);
+  const uint32_t stat_off = static_cast<uint32_t>(stat_up * a.hq + lane - stat_up * a.group) * 4;
   auto fetch = [&](int n, int buf) {
     const int tok = first + (steps.parts > 1 ? n / steps.parts : n * steps.tokens);
     const int head = steps.parts > 1 ? n % steps.parts * kStep : 0;
     const int count = min(min(steps.tokens, qs.len - tok) * a.group - head, kStep);
     ql.load(lds + buf * kTile, tok, head, count);
     ol.load(lds + (2 + buf) * kTile, tok, head, count);
-    if (threadIdx.x < kStep) {
-      const int i = threadIdx.x;
-      float lse = -INFINITY, delta = 0.0f, pos = 0.0f, slope = 0.0f;
-      int limit = 0;
-      if (i < count) {
-        const int up = steps.parts > 1 ? 0 : div_group(i, a.group);
-        const int t = tok + up, h = kvh * a.group + head + i - up * a.group;
-        const int64_t at = (qs.start + t) * a.hq + h;
-        const float x = a.lse_in[at];
-        if (x != -INFINITY) lse = -x * kLog2e;
-        delta = a.delta[at];
-        pos = static_cast<float>(t + ks.len - qs.len);
-        limit = key_limit(t, qs.len, ks.len, a.causal, prefix);
-        if (a.slopes) slope = a.slopes[h] * kLog2e;
-      }
-      stat[buf][0][i] = lse;
-      stat[buf][1][i] = delta;
-      stat[buf][2][i] = pos;
-      stat[buf][3][i] = slope;
-      stat_limit[buf][i] = limit;
+    if (first_wave) {
+      const int64_t at = (qs.start + tok) * a.hq + kvh * a.group + head;
+      const uint32_t off = lane < count ? stat_off : 0x80000000u;
+#pragma unroll
+      for (int k = 0; k < kStats; ++k) load_words(a.stat + k * a.q_rows * a.hq + at, off, stat[buf][k]);
     }
   };
 
@@ -145,10 +154,11 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     const int last_tok = min(tok + steps.tokens, qs.len) - 1;
     const int least = key_limit(tok, qs.len, ks.len, a.causal, prefix);
     const int most = key_limit(last_tok, qs.len, ks.len, a.causal, prefix);
-    if (jw >= most) continue;  // wave-uniform: no row of the step sees these keys
     const bool masked = min(jw + 32, ks.len) > least;
     const char* qt = lds + buf * kTile;
     const char* dt = lds + (2 + buf) * kTile;
+    // wave-uniform: some row of the step sees the wave's keys
+    if (jw < most)
 #pragma unroll
     for (int rb = 0; rb < kStep / 32; ++rb) {
       f32x16 sc = {}, dp = {};
@@ -179,27 +189,30 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 lse = four(stat[buf][0], r + g * 8);
+        const f32x4 lse = four(stat[buf][kStatLse], r + g * 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[4 * g + e] = sc[4 * g + e] * c + lse[e];
       }
       if (a.slopes) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 pos = four(stat[buf][2], r + g * 8), slope = four(stat[buf][3], r + g * 8);
+          const f32x4 pos = four(stat[buf][kStatPos], r + g * 8), slope = four(stat[buf][kStatSlope], r + g * 8);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - pos[e]);
+          for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - static_cast<float>(__float_as_int(pos[e])));
         }
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exp2_hw(p[i]);
       if (masked) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = j < stat_limit[buf][r + (i >> 2) * 8 + (i & 3)] ? p[i] : 0.0f;
+        for (int i = 0; i < 16; ++i) {
+          const int pos = __float_as_int(stat[buf][kStatPos][r + (i >> 2) * 8 + (i & 3)]);
+          p[i] = j <= pos || j < see_all ? p[i] : 0.0f;
+        }
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 delta = four(stat[buf][1], r + g * 8);
+        const f32x4 delta = four(stat[buf][kStatDelta], r + g * 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * g + e;
@@ -251,8 +264,8 @@ __device__ inline float dot8(const f32x8s& x, const f32x8s& y) {
   return s;
 }
 
-// dq of a row tile, delta of its rows (which k_attn_dkdv reads), and its sum
-// of the slopes' gradient per head.
+// dq of a row tile, what k_attn_dkdv needs of its rows, and its sum of the
+// slopes' gradient per head.
 //
 // delta, in bf16, is taken from the output and what its rounding left: where
 // few keys matter, delta is of dP's size and the output's rounding alone would
@@ -263,7 +276,7 @@ __device__ inline float dot8(const f32x8s& x, const f32x8s& y) {
 // j|, as sum_j x t - (sum_j x) (sum_j P t): the sum of x is 0 but for delta's
 // own error, which would else be weighed by every distance.
 template <typename T, int HD>
-__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k_attn_dq(const AttnArgs a) {
+__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) void k_attn_dq(const AttnArgs a) {
   typedef Tile<T, HD> L;
   typedef typename Frag<T>::type F;
   constexpr int KS = HD / 16, DT = HD / 32;
@@ -340,7 +353,13 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     lse = INFINITY;
     delta = 0.0f;
   }
-  if (live && half == 0) a.delta[row] = delta;
+  if (live && half == 0) {
+    const int64_t n = a.q_rows * a.hq;
+    a.stat[kStatLse * n + row] = -lse;
+    a.stat[kStatDelta * n + row] = delta;
+    a.stat[kStatPos * n + row] = __int_as_float(me.token + ks.len - qs.len);
+    a.stat[kStatSlope * n + row] = a.slopes ? a.slopes[me.head] * kLog2e : 0.0f;
+  }
   const float pos = static_cast<float>(me.token + ks.len - qs.len);
   const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
   const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;

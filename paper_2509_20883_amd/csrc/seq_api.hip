@@ -118,11 +118,11 @@ rs_status check_offsets(const rs_attn_desc& d, const int64_t* q_off, const int64
 }
 
 struct BwdWork {
-  size_t delta, slope_part, total;
+  size_t slope_part, total;  // the rows' statistics come first
 };
 BwdWork bwd_work(const AttnArgs& a) {
   BwdWork w{};
-  w.slope_part = align_up(sizeof(float) * static_cast<size_t>(a.q_rows) * static_cast<size_t>(a.hq));
+  w.slope_part = align_up(4 * sizeof(float) * static_cast<size_t>(a.q_rows) * static_cast<size_t>(a.hq));
   w.total = w.slope_part + align_up(sizeof(float) * static_cast<size_t>(attn_row_tiles(a)) * static_cast<size_t>(a.hq));
   return w;
 }
@@ -287,7 +287,7 @@ rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k,
   a.dv = dv;
   a.dslopes = dslopes;
   uint8_t* base = static_cast<uint8_t*>(workspace);
-  a.delta = reinterpret_cast<float*>(base);
+  a.stat = reinterpret_cast<float*>(base);
   a.slope_part = dslopes ? reinterpret_cast<float*>(base + w.slope_part) : nullptr;
   RS_HIP(launch_attn_bwd(a, d->dtype == RS_BF16, s));
   return RS_OK;

@@ -74,7 +74,7 @@ struct AttnArgs {
   const void *o, *o_rest, *dout;
   const float* lse_in;
   void *dq, *dk, *dv;
-  float *dslopes, *delta, *slope_part;
+  float *dslopes, *stat, *slope_part;
 };
 
 // Fills the split of the forward (chunk 0: none) for at most max_q queries a
