@@ -38,12 +38,6 @@ __device__ inline void load_words(const float* p, uint32_t off, float* dst) {
 // Four consecutive tile rows' values from LDS.
 __device__ inline f32x4 four(const float* p, int r) { return *reinterpret_cast<const f32x4*>(p + r); }
 
-// Rows of 256 bytes and more (128 bf16, 64 fp32) leave no registers for the keys
-// beside the values and both gradients if two blocks are to share a CU, one in
-// its products while the other is in its exponentials: the keys then stay in
-// LDS, and a step takes 32 rows instead of 64 to make room for them there.
-template <typename T, int HD>
-constexpr bool kKeysInLds = HD * sizeof(T) >= 256;
 template <typename T, int HD>
 constexpr int kResidentBlocks = HD * sizeof(T) > 256 ? 1 : 2;
 // The dq pass holds one gradient, and up to 128 bytes a row three blocks fit
@@ -51,55 +45,80 @@ constexpr int kResidentBlocks = HD * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int HD>
 constexpr int kResidentRowBlocks = HD * sizeof(T) <= 128 ? 3 : kResidentBlocks<T, HD>;
 
+// How a block of the pass over keys is shaped: KW waves side by side on 32 keys
+// each, times RW waves that take turns on the 32-row parts of a step of STEP
+// rows and add up their gradients at the end.
+//
+// Two gradients of 32 keys take HD / 2 + HD / 2 registers a lane.  To leave room
+// for two blocks a CU (three up to 128 bytes a row), one in its products while
+// another is in its exponentials, the keys stay in LDS as operands, and up to
+// 128 bytes a row the values too (padded sequences of 560 keys of 64, dk and dv:
+// keys and values in registers, two blocks 1087 us, in LDS, three 978).
+//
+// Few key tiles (long sequences, many query heads on a key head) are bound by
+// the longest one, not by the rate: tiles of 64 keys with more waves along the
+// rows then take a quarter (a half) of the time each.
+template <typename T, int HD, bool FEW>
+struct KeyShape {
+  static constexpr int kRow = HD * sizeof(T);
+  static constexpr bool kNarrow = kRow <= 128, kWide = kRow > 256;
+  static constexpr int KW = FEW && !kWide ? 2 : 4;
+  static constexpr int RW = !FEW || kWide ? 1 : kNarrow ? 2 : 4;
+  static constexpr int W = KW * RW;       // waves
+  static constexpr int STEP = 32 * RW;    // rows per step
+  static constexpr int KEYS = 32 * KW;    // keys per block
+  static constexpr bool VALUES_IN_LDS = kNarrow;
+  static constexpr int BLOCKS = kWide ? 1 : kNarrow ? 3 : 8 / W;  // per CU
+};
+
 // dk and dv of a key tile, a wave 32 keys, one per lane column.
-template <typename T, int HD>
-__global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k_attn_dkdv(const AttnArgs a) {
+template <typename T, int HD, bool FEW>
+__global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD, FEW>::BLOCKS * KeyShape<T, HD, FEW>::W / 4)) void k_attn_dkdv(
+    const AttnArgs a) {
+  typedef KeyShape<T, HD, FEW> C;
   typedef Tile<T, HD> L;
   typedef typename Frag<T>::type F;
   constexpr int KS = HD / 16, DT = HD / 32;
-  constexpr bool kLdsKeys = kKeysInLds<T, HD>;
-  constexpr int kStep = kLdsKeys ? 32 : 64;  // rows per step
-  constexpr int kTile = kStep * L::kRowBytes;
-  __shared__ __align__(1024) char lds[4 * kTile + (kLdsKeys ? kAttnRows * L::kRowBytes : 0)];  // q, dout: two steps
-  char* key_tile = lds + 4 * kTile;
+  constexpr int kStep = C::STEP;
+  constexpr int kTile = kStep * L::kRowBytes, kKeyTile = C::KEYS * L::kRowBytes;
+  // q and dout, two steps of each, then the keys (and values)
+  __shared__ __align__(1024) char lds[4 * kTile + (C::VALUES_IN_LDS ? 2 : 1) * kKeyTile];
+  char *key_tile = lds + 4 * kTile, *val_tile = key_tile + kKeyTile;
   // of the step's rows, as k_attn_dq left them; 0 where there is no row: its q and dout are 0 too, and add nothing
-  __shared__ __align__(16) float stat[2][kStats][kWave];
+  constexpr int kStatRows = kStep < kWave ? kWave : kStep;
+  __shared__ __align__(16) float stat[2][kStats][kStatRows];
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
+  const int kw = wave % C::KW, rw = wave / C::KW;
   const BlockOf blk = block_of(a.hkv, false);
   const int kvh = blk.kvh;
   int s;
   int64_t tile;
   if (a.kv_pad > 0) {
-    const uint32_t per = static_cast<uint32_t>((a.kv_pad + kAttnRows - 1) / kAttnRows);
+    const uint32_t per = static_cast<uint32_t>((a.kv_pad + C::KEYS - 1) / C::KEYS);
     s = static_cast<uint32_t>(blk.tile) / per;
     tile = blk.tile - static_cast<int64_t>(s) * per;
   } else {
-    s = find_seq(a.kv_off, a.seqs, 1, kAttnRows, blk.tile, tile);
+    s = find_seq(a.kv_off, a.seqs, 1, C::KEYS, blk.tile, tile);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int64_t out_rows = a.kv_pad > 0 ? a.kv_pad : ks.len;
-  if (tile * kAttnRows >= out_rows) return;  // block-uniform
+  if (tile * C::KEYS >= out_rows) return;  // block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
 
-  const int j0 = static_cast<int>(tile) * kAttnRows;
-  const int jw = j0 + wave * 32;  // the wave's first key
+  const int j0 = static_cast<int>(tile) * C::KEYS;
+  const int jw = j0 + kw * 32;  // the wave's first key
   const int j = jw + col;         // the lane's key
   const bool live = j < ks.len;
-  F kf[kLdsKeys ? 1 : KS], vf[KS];
-  {
-    const T* k = static_cast<const T*>(a.k.p) + (ks.start + j) * a.k.row + kvh * a.k.head;
+  F vf[C::VALUES_IN_LDS ? 1 : KS];
+  if (!C::VALUES_IN_LDS) {
     const T* v = static_cast<const T*>(a.v.p) + (ks.start + j) * a.v.row + kvh * a.v.head;
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
       const int k0 = t * 16 + half * 8;
-      if (!kLdsKeys) kf[t] = zero_frag<T>();
       vf[t] = zero_frag<T>();
-      if (live && k0 < a.d) {
-        if (!kLdsKeys) load_frag(k + k0, kf[t]);
-        load_frag(v + k0, vf[t]);
-      }
+      if (live && k0 < a.d) load_frag(v + k0, vf[t]);
     }
   }
   const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
@@ -118,34 +137,41 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   if (j0 >= ks.len) first = qs.len;
 
   const RowSteps<kStep> steps(a.group);
-  RowLoader<T, HD, kStep> ql, ol;
+  RowLoader<T, HD, kStep, C::W> ql, ol;
   ql.init(a.q, qs.start, kvh, a.group, a.d);
   ol.init(HeadRows{a.dout, int64_t(a.hq) * a.d, a.d}, qs.start, kvh, a.group, a.d);
   // Step n: token first + n / parts * tokens, head n % parts * kStep of the group.
   const int n_steps = first < qs.len ? (qs.len - first + steps.tokens - 1) / steps.tokens * steps.parts : 0;
-  const bool first_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) == 0;
-  const int stat_up = steps.parts > 1 ? 0 : div_group(lane, a.group);
-  const uint32_t stat_off = static_cast<uint32_t>(stat_up * a.hq + lane - stat_up * a.group) * 4;
+  // the row that the thread loads the statistics of, 64 rows a wave
+  const int stat_row = threadIdx.x;
+  const int stat_up = steps.parts > 1 ? 0 : div_group(stat_row, a.group);
+  const uint32_t stat_off = static_cast<uint32_t>(stat_up * a.hq + stat_row - stat_up * a.group) * 4;
+  const int stat_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   auto fetch = [&](int n, int buf) {
     const int tok = first + (steps.parts > 1 ? n / steps.parts : n * steps.tokens);
     const int head = steps.parts > 1 ? n % steps.parts * kStep : 0;
     const int count = min(min(steps.tokens, qs.len - tok) * a.group - head, kStep);
     ql.load(lds + buf * kTile, tok, head, count);
     ol.load(lds + (2 + buf) * kTile, tok, head, count);
-    if (first_wave) {
+    if (stat_wave < kStatRows / kWave) {
       const int64_t at = (qs.start + tok) * a.hq + kvh * a.group + head;
-      const uint32_t off = lane < count ? stat_off : 0x80000000u;
+      const uint32_t off = stat_row < count ? stat_off : 0x80000000u;
 #pragma unroll
-      for (int k = 0; k < kStats; ++k) load_words(a.stat + k * a.q_rows * a.hq + at, off, stat[buf][k]);
+      for (int k = 0; k < kStats; ++k)
+        load_words(a.stat + k * a.q_rows * a.hq + at, off, stat[buf][k] + stat_wave * kWave);
     }
   };
 
-  if (kLdsKeys && n_steps > 0) {  // a step needs a key: j0 < ks.len
-    TileLoader<T, HD, kAttnRows> kl;
+  if (n_steps > 0) {  // a step needs a key: j0 < ks.len
+    TileLoader<T, HD, C::KEYS, C::W> kl;
     kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
     kl.load(key_tile, j0);
+    if (C::VALUES_IN_LDS) {
+      kl.init(a.v.p, ks.start, a.v.row, kvh * a.v.head, a.d, ks.len);
+      kl.load(val_tile, j0);
+    }
+    fetch(0, 0);
   }
-  if (n_steps > 0) fetch(0, 0);
   for (int n = 0; n < n_steps; ++n) {
     const int buf = n & 1;
     wait_tiles();  // this step's rows are there, the other step's have been read
@@ -157,23 +183,23 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     const bool masked = min(jw + 32, ks.len) > least;
     const char* qt = lds + buf * kTile;
     const char* dt = lds + (2 + buf) * kTile;
+    const int rb = rw;  // the wave's 32 rows of the step
     // wave-uniform: some row of the step sees the wave's keys
-    if (jw < most)
-#pragma unroll
-    for (int rb = 0; rb < kStep / 32; ++rb) {
+    if (jw < most) {
       f32x16 sc = {}, dp = {};
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
-        F f;
+        F f, g;
         row_frag<HD>(qt, rb * 32 + col, t * 16 + half * 8, f);
-        if (kLdsKeys) row_frag<HD>(key_tile, wave * 32 + col, t * 16 + half * 8, kf[0]);
-        sc = mma(f, kf[kLdsKeys ? 0 : t], sc);
+        row_frag<HD>(key_tile, kw * 32 + col, t * 16 + half * 8, g);
+        sc = mma(f, g, sc);
       }
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
         F f;
         row_frag<HD>(dt, rb * 32 + col, t * 16 + half * 8, f);
-        dp = mma(f, vf[t], dp);
+        if (C::VALUES_IN_LDS) row_frag<HD>(val_tile, kw * 32 + col, t * 16 + half * 8, vf[0]);
+        dp = mma(f, vf[C::VALUES_IN_LDS ? 0 : t], dp);
       }
       // registers 4 g .. 4 g + 3 are rows r, r + 1, r + 2, r + 3
       float p[16], ds[16];
@@ -235,11 +261,42 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     }
   }
 
-  typedef RowWriter<T, HD> S;
-  constexpr int kShare = sizeof(lds) / kAttnWaves;
-  static_assert(S::kBytes <= kShare, "a wave's rows fit its share of the tiles");
   __syncthreads();  // the tiles have been read
-  char* mine = lds + wave * kShare;
+  if (C::RW > 1) {
+    // the row parts' gradients, added to the first part's in order
+    constexpr int kPart = DT * 16 * kWave * sizeof(float);
+    static_assert(sizeof(lds) >= C::KW * kPart, "a part of every key wave fits");
+    f32x4* mine = reinterpret_cast<f32x4*>(lds + kw * kPart) + lane;
+#pragma unroll
+    for (int part = 1; part < C::RW; ++part) {
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        f32x16(&g)[DT] = which ? dv : dk;
+        if (rw == part)
+#pragma unroll
+          for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              mine[(i * 4 + e) * kWave] = f32x4{g[i][4 * e], g[i][4 * e + 1], g[i][4 * e + 2], g[i][4 * e + 3]};
+        __syncthreads();
+        if (rw == 0)
+#pragma unroll
+          for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const f32x4 x = mine[(i * 4 + e) * kWave];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) g[i][4 * e + q] += x[q];
+            }
+        __syncthreads();
+      }
+    }
+    if (rw > 0) return;
+  }
+  typedef RowWriter<T, HD> S;
+  constexpr int kShare = sizeof(lds) / C::KW / 16 * 16;
+  static_assert(S::kBytes <= kShare, "a wave's rows fit its share of the tiles");
+  char* mine = lds + kw * kShare;
   auto at = [&](void* base, int i) -> T* {
     if (jw + i >= out_rows) return nullptr;
     return static_cast<T*>(base) + ((ks.start + jw + i) * a.hkv + kvh) * a.d;
@@ -499,17 +556,27 @@ __global__ __launch_bounds__(kSlopeThreads) void k_attn_dslopes(const AttnArgs a
   if (threadIdx.x == 0) a.dslopes[blockIdx.x] = static_cast<float>(sh[0]);
 }
 
-int64_t key_tiles(const AttnArgs& a) {
+int64_t key_tiles(const AttnArgs& a, int keys) {
   if (a.seqs == 0) return 0;
-  if (a.kv_pad > 0) return a.seqs * ((a.kv_pad + kAttnRows - 1) / kAttnRows);
-  return a.kv_rows / kAttnRows + a.seqs;
+  if (a.kv_pad > 0) return a.seqs * ((a.kv_pad + keys - 1) / keys);
+  return a.kv_rows / keys + a.seqs;
 }
+
+template <typename T, int HD, bool FEW>
+void run_keys(const AttnArgs& a, hipStream_t s) {
+  typedef KeyShape<T, HD, FEW> C;
+  const int64_t n = key_tiles(a, C::KEYS) * a.hkv;
+  if (n > 0) k_attn_dkdv<T, HD, FEW><<<static_cast<unsigned>(n), C::W * kWave, 0, s>>>(a);
+}
+
+constexpr int64_t kFewKeyBlocks = 1536;  // two to three times what the GPU runs at once
 
 template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
-  const int64_t kt = key_tiles(a), qt = attn_row_tiles(a);
+  const int64_t qt = attn_row_tiles(a);
   if (qt > 0) k_attn_dq<T, HD><<<static_cast<unsigned>(qt * a.hkv), kAttnWaves * kWave, 0, s>>>(a);
-  if (kt > 0) k_attn_dkdv<T, HD><<<static_cast<unsigned>(kt * a.hkv), kAttnWaves * kWave, 0, s>>>(a);
+  if (key_tiles(a, KeyShape<T, HD, false>::KEYS) * a.hkv < kFewKeyBlocks && HD * sizeof(T) <= 256) run_keys<T, HD, true>(a, s);
+  else run_keys<T, HD, false>(a, s);
   if (a.dslopes) k_attn_dslopes<<<a.hq, kSlopeThreads, 0, s>>>(a, qt);
   return hipGetLastError();
 }

@@ -295,10 +295,10 @@ __device__ inline int key_limit(int token, int lq, int lk, bool causal, int pref
 // The lane picks the chunk that belongs at its place, so the tile's chunk
 // order costs nothing.  The buffer's bounds do the masking: rows past the
 // sequence's end and columns past d lie outside and arrive as zeros.
-template <typename T, int HD, int N = kAttnStep>
+template <typename T, int HD, int N = kAttnStep, int W = kAttnWaves>
 struct TileLoader {
   typedef Tile<T, HD> L;
-  static constexpr int kLoads = N * L::kRowBytes / (kAttnWaves * kWave * 16);  // per thread
+  static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);  // per thread of W waves
   uint32_t off[kLoads];  // byte offset of the thread's chunks from the tile's first row
   int64_t row_bytes;
   const char* base;  // the sequence's first row
@@ -348,10 +348,10 @@ struct RowSteps {
   int tokens, parts;  // tokens per step, steps per token (one of them is 1)
   __device__ inline explicit RowSteps(int g) : tokens(g <= N ? N / g : 1), parts(g <= N ? 1 : (g + N - 1) / N) {}
 };
-template <typename T, int HD, int N>
+template <typename T, int HD, int N, int W>
 struct RowLoader {
   typedef Tile<T, HD> L;
-  static constexpr int kLoads = N * L::kRowBytes / (kAttnWaves * kWave * 16);
+  static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);
   uint32_t off[kLoads];
   int64_t row_bytes, head_bytes;
   const char* base;  // the sequence's first token, the group's first head

@@ -40,7 +40,7 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 int64_t attn_blocks(const rs_attn_desc& d) {
   const int64_t group = d.heads_q / d.heads_kv;
   const int64_t q = d.q_pad > 0 ? d.seqs * (d.q_pad * group / 128 + 1) : d.q_rows * group / 128 + d.seqs;
-  const int64_t k = d.kv_pad > 0 ? d.seqs * (d.kv_pad / 128 + 1) : d.kv_rows / 128 + d.seqs;
+  const int64_t k = d.kv_pad > 0 ? d.seqs * (d.kv_pad / 64 + 1) : d.kv_rows / 64 + d.seqs;
   return std::max(q, k) * d.heads_kv;
 }
 
