@@ -65,7 +65,8 @@ struct KeyShape {
   static constexpr int KW = FEW && !kWide ? 2 : 4;
   static constexpr int RW = !FEW || kWide ? 1 : kNarrow ? 2 : 4;
   static constexpr int W = KW * RW;       // waves
-  static constexpr int STEP = 32 * RW;    // rows per step
+  // rows per step: 32 for every row wave, and at least a load of 16 bytes for every thread
+  static constexpr int STEP = 32 * RW * kRow < W * kWave * 16 ? W * kWave * 16 / kRow : 32 * RW;
   static constexpr int KEYS = 32 * KW;    // keys per block
   static constexpr bool VALUES_IN_LDS = kNarrow;
   static constexpr int BLOCKS = kWide ? 1 : kNarrow ? 3 : 8 / W;  // per CU
@@ -183,9 +184,11 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
     const bool masked = min(jw + 32, ks.len) > least;
     const char* qt = lds + buf * kTile;
     const char* dt = lds + (2 + buf) * kTile;
-    const int rb = rw;  // the wave's 32 rows of the step
     // wave-uniform: some row of the step sees the wave's keys
-    if (jw < most) {
+    if (jw < most)
+#pragma unroll
+    for (int part = 0; part < kStep / 32 / C::RW; ++part) {
+      const int rb = part * C::RW + rw;  // 32 rows of the step
       f32x16 sc = {}, dp = {};
 #pragma unroll
       for (int t = 0; t < KS; ++t) {

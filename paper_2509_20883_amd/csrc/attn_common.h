@@ -299,6 +299,7 @@ template <typename T, int HD, int N = kAttnStep, int W = kAttnWaves>
 struct TileLoader {
   typedef Tile<T, HD> L;
   static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);  // per thread of W waves
+  static_assert(kLoads >= 1 && kLoads * W * kWave * 16 == N * L::kRowBytes, "whole loads");
   uint32_t off[kLoads];  // byte offset of the thread's chunks from the tile's first row
   int64_t row_bytes;
   const char* base;  // the sequence's first row
@@ -309,7 +310,7 @@ struct TileLoader {
     base = static_cast<const char*>(p) + (start * row + head_off) * static_cast<int64_t>(sizeof(T));
     len = n;
     d_bytes = d * static_cast<int>(sizeof(T));
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    const int wave = W == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int at = ((wave * kLoads + i) * kWave + lane) * 16;
@@ -330,7 +331,7 @@ struct TileLoader {
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes),
         0x00020000);
-    char* dst = tile + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kLoads * kWave * 16;
+    char* dst = tile + (W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kLoads * kWave * 16);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -352,6 +353,7 @@ template <typename T, int HD, int N, int W>
 struct RowLoader {
   typedef Tile<T, HD> L;
   static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);
+  static_assert(kLoads >= 1 && kLoads * W * kWave * 16 == N * L::kRowBytes, "whole loads");
   uint32_t off[kLoads];
   int64_t row_bytes, head_bytes;
   const char* base;  // the sequence's first token, the group's first head
@@ -392,6 +394,13 @@ struct RowLoader {
 #endif
   }
 };
+
+// All but the wave's last N loads have arrived.
+template <int N>
+__device__ inline void wait_loads() {
+  static_assert(N < 64, "the counter has six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);
+}
 
 // Every load of the wave has arrived, and then every wave's.
 __device__ inline void wait_tiles() {

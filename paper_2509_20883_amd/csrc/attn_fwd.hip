@@ -270,14 +270,246 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     a.lse[(qs.start + me.token) * a.hq + me.head] = none ? -INFINITY : m * kLn2 + logf(l);
 }
 
+// At most 32 rows a sequence and key head (single tokens, a few candidates):
+// bound by reading the keys and values once.  A wave walks over blocks of 32
+// keys of its own, W waves in turn through the block's chunk, with its own
+// place for a block's keys and one for its values in LDS: the next keys are on
+// their way as soon as the scores are taken, the next values as soon as the
+// output is, and no barrier ties the waves together.  The waves' results are
+// joined as those of chunks are.
+template <typename T, int HD>
+struct FewShape {
+  static constexpr int W = 8;
+  static constexpr bool kUsed = HD * sizeof(T) <= 128;
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const AttnArgs a) {
+  typedef FewShape<T, HD> C;
+  typedef Tile<T, HD> L;
+  typedef typename Frag<T>::type F;
+  constexpr int KS = HD / 16, DT = HD / 32;
+  constexpr int kTile = 32 * L::kRowBytes;
+  __shared__ __align__(1024) char k_place[C::W * kTile], v_place[C::W * kTile];
+  __shared__ float2 sh_ml[C::W][32];
+
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int half = lane >> 5, col = lane & 31;
+  const int kvh = blockIdx.y;
+  int s;
+  int64_t ci;
+  if (a.kv_pad > 0) {
+    const uint32_t per = static_cast<uint32_t>(a.kv_pad + a.chunk - 1) / a.chunk;
+    s = blockIdx.x / per;
+    ci = blockIdx.x - s * per;
+  } else {
+    s = find_seq(a.kv_off, a.seqs, 1, a.chunk, blockIdx.x, ci);
+  }
+  if (ci * a.chunk >= int64_t(1) << 31) return;
+  const int c0 = static_cast<int>(ci) * a.chunk;
+  const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
+  const int rows = min(qs.len * a.group, a.part_rows);
+  const int out_rows = a.q_pad > 0 ? a.part_rows : rows;
+  const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
+  const RowOf me = row_of(col, kvh, a.group);
+  const bool live = col < rows;
+  const int limit = live ? key_limit(me.token, qs.len, ks.len, a.causal, prefix) : 0;
+  int end = rows > 0 ? key_limit(div_group(rows - 1, a.group), qs.len, ks.len, a.causal, prefix) : 0;
+  const int least = rows > 0 ? key_limit(0, qs.len, ks.len, a.causal, prefix) : 0;
+  const bool joined = ks.len > a.chunk;
+  if (c0 > 0 && c0 >= end) return;  // block-uniform; the join does not look here
+  end = min(end, c0 + a.chunk);
+
+  // the wave's blocks of 32 keys: first, first + 32 W, ...
+  const int first = c0 + wave * 32;
+  const int n_mine = first < end ? (end - first + 32 * C::W - 1) / (32 * C::W) : 0;
+  char *kt = k_place + wave * kTile, *vt = v_place + wave * kTile;
+  TileLoader<T, HD, 32, 1> kl, vl;
+  kl.init(a.k.p, ks.start, a.k.row, kvh * a.k.head, a.d, ks.len);
+  vl.init(a.v.p, ks.start, a.v.row, kvh * a.v.head, a.d, ks.len);
+  constexpr int kLoads = TileLoader<T, HD, 32, 1>::kLoads;  // of a block of keys, or of values
+  if (n_mine > 0) {
+    kl.load(kt, first);
+    vl.load(vt, first);
+  }
+  F qf[KS];
+  {
+    const T* q = static_cast<const T*>(a.q.p) + (qs.start + me.token) * a.q.row + me.head * a.q.head;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      const int k0 = t * 16 + half * 8;
+      qf[t] = zero_frag<T>();
+      if (live && k0 < a.d) load_frag(q + k0, qf[t]);
+    }
+  }
+  const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
+  const float inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e, scale2 = a.scale * kLog2e;
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
+  float m = 0.0f, move = -INFINITY, l = 0.0f;
+
+  for (int n = 0; n < n_mine; ++n) {
+    const int j0 = first + n * 32 * C::W;
+    const bool more = n + 1 < n_mine;
+    wait_loads<kLoads>();  // the keys have arrived, the values may be on their way
+    asm volatile("" ::: "memory");
+    f32x16 sc = {};
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      F kf;
+      row_frag<HD>(kt, col, t * 16 + half * 8, kf);
+      sc = mma(kf, qf[t], sc);
+    }
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = sc[i];
+    if (more) kl.load(kt, j0 + 32 * C::W);  // the products have read the keys
+    const int j = j0 + half * 4;  // register i is key j + (i / 4) * 8 + i % 4
+    float c = scale2;
+    if (a.cap > 0.0f) {
+      c = cap2;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = tanh_of<T>(p[i] * inv_cap);
+    }
+    if (!a.slopes) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = p[i] * c - m;
+    } else {
+      const float dist = static_cast<float>(j) - pos;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        p[i] = p[i] * c - (slope * fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3))) + m);
+    }
+    if (j0 + 32 > least || j0 + 32 > end) {
+      const int left = min(limit, end) - j;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = (i >> 2) * 8 + (i & 3) < left ? p[i] : -INFINITY;
+    }
+    float top = p[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+    top = other_half_max(top);
+    if (__any(top > move)) {
+      const bool up = top > move;
+      const float by = up ? top : 0.0f;
+      const float alpha = move == -INFINITY ? 0.0f : exp2_hw(-by);
+      m += by;
+      move = up ? 8.0f : move;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[i] *= alpha;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] -= by;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = exp2_hw(p[i]);
+      sum += p[i];
+    }
+    l += sum;
+    if (more) wait_loads<kLoads>();  // the values
+    else wait_loads<0>();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const F pf = to_frag<T>(p, t);
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        F vf;
+        col_frag<HD>(vt, t * 16, i * 32, lane, vf);
+        acc[i] = mma(vf, pf, acc[i]);
+      }
+    }
+    if (more) vl.load(vt, j0 + 32 * C::W);  // the products have read the values
+  }
+
+  // the waves' parts: m = max m_w, acc = sum acc_w 2^(m_w - m), l alike
+  l = other_half_sum(l);
+  if (half == 0) sh_ml[wave][col] = make_float2(m, l);
+  __syncthreads();  // and the rings have been read
+  float m_all = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < C::W; ++w) m_all = fmaxf(m_all, sh_ml[w][col].y == 0.0f ? -INFINITY : sh_ml[w][col].x);
+  const float base = m_all == -INFINITY ? 0.0f : m_all;
+  const float mul = l == 0.0f ? 0.0f : exp2_hw(m - base);
+  constexpr int kPart = DT * 16 * kWave * sizeof(float);
+  static_assert(C::W / 2 * kPart <= static_cast<int>(sizeof(k_place)), "half of the parts fit");
+#pragma unroll
+  for (int i = 0; i < DT; ++i) acc[i] *= mul;
+#pragma unroll
+  for (int w = C::W / 2; w >= 1; w /= 2) {  // the upper half of the waves hand theirs to the lower half
+    f32x4* at = reinterpret_cast<f32x4*>(k_place + wave % w * kPart) + lane;
+    if (wave >= w && wave < 2 * w)
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          at[(i * 4 + e) * kWave] = f32x4{acc[i][4 * e], acc[i][4 * e + 1], acc[i][4 * e + 2], acc[i][4 * e + 3]};
+    __syncthreads();
+    if (wave < w)
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 x = at[(i * 4 + e) * kWave];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[i][4 * e + q] += x[q];
+        }
+    __syncthreads();
+  }
+  if (wave > 0) return;
+  l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < C::W; ++w) {
+    const float2 x = sh_ml[w][col];
+    l += x.y == 0.0f ? 0.0f : x.y * exp2_hw(x.x - base);
+  }
+  m = base;
+  if (col >= out_rows) return;
+  if (joined) {
+    const int64_t slot = (static_cast<int64_t>(blockIdx.x) * a.hkv + kvh) * a.part_rows + col;
+    float* po = a.part_o + slot * a.d;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d0 = i * 32 + g * 8 + half * 4;
+        if (d0 < a.d) store4(po + d0, acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]);
+      }
+    if (half == 0) reinterpret_cast<float2*>(a.part_ml)[slot] = make_float2(m, l);
+    return;
+  }
+  const bool none = !live || l == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / l;
+  const int64_t row = (qs.start + me.token) * a.hq + me.head;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d0 = i * 32 + g * 8 + half * 4;
+      if (d0 >= a.d) continue;
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : acc[i][4 * g + e] * inv;
+      store4(static_cast<T*>(a.out) + row * a.d + d0, x[0], x[1], x[2], x[3]);
+      if (sizeof(T) == 2 && a.rest && live)
+        store4(static_cast<T*>(a.rest) + row * a.d + d0, rest_bf16(x[0]), rest_bf16(x[1]), rest_bf16(x[2]), rest_bf16(x[3]));
+    }
+  if (a.lse && half == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
+}
+
 // Joins the chunks of a row: a block per query token and head, threads four
 // columns and a share of the chunks each.
 //   m = max m_c,  l = sum l_c 2^(m_c - m),  out = sum acc_c 2^(m_c - m) / l
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
-  __shared__ float4 sh_o[kBlock];
-  __shared__ float sh_l[kBlock];
-  __shared__ float sh_m[kBlock / kWave];
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void k_attn_join(const AttnArgs a) {
+  __shared__ float4 sh_o[NT];
+  __shared__ float sh_l[NT];
+  __shared__ float sh_m[NT / kWave];
   const int head = blockIdx.y, kvh = head / a.group;
   int s;
   int64_t token;
@@ -301,7 +533,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
 
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   float m = -INFINITY;
-  for (int c = threadIdx.x; c < chunks; c += kBlock) {
+  for (int c = threadIdx.x; c < chunks; c += NT) {
     const float2 x = ml[slot0 + c * step];
     m = fmaxf(m, x.y == 0.0f ? -INFINITY : x.x);  // a part may see no key
   }
@@ -310,11 +542,11 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(const AttnArgs a) {
   if ((threadIdx.x & (kWave - 1)) == 0) sh_m[threadIdx.x / kWave] = m;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kBlock / kWave; ++w) m = fmaxf(m, sh_m[w]);
+  for (int w = 0; w < NT / kWave; ++w) m = fmaxf(m, sh_m[w]);
   const float base = m == -INFINITY ? 0.0f : m;
 
   const int quads = a.d / 4;  // at most 32
-  const int shares = kBlock / quads, q = threadIdx.x % quads, share = threadIdx.x / quads;
+  const int shares = NT / quads, q = threadIdx.x % quads, share = threadIdx.x / quads;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float l = 0.0f;
   if (share < shares) {
@@ -362,9 +594,16 @@ template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
   if (a.chunk > 0) {
     const dim3 grid(static_cast<unsigned>(key_chunks(a)), a.hkv, a.row_tiles);
-    k_attn_fwd<T, HD, true><<<grid, kAttnWaves * kWave, 0, s>>>(a);
+    if constexpr (FewShape<T, HD>::kUsed) {
+      if (a.few) k_attn_few<T, HD><<<grid, FewShape<T, HD>::W * kWave, 0, s>>>(a);
+      else k_attn_fwd<T, HD, true><<<grid, kAttnWaves * kWave, 0, s>>>(a);
+    } else {
+      k_attn_fwd<T, HD, true><<<grid, kAttnWaves * kWave, 0, s>>>(a);
+    }
     const dim3 jg(static_cast<unsigned>(a.q_pad > 0 ? a.q_rows : a.q_rows + a.seqs), a.hq);
-    k_attn_join<T><<<jg, kBlock, 0, s>>>(a);
+    // threads by the chunks of a row: many rows of few chunks, or few rows of many
+    if (key_chunks(a) / a.seqs > 32) k_attn_join<T, 1024><<<jg, 1024, 0, s>>>(a);
+    else k_attn_join<T, 128><<<jg, 128, 0, s>>>(a);
   } else {
     const unsigned grid = static_cast<unsigned>(attn_row_tiles(a) * a.hkv);
     k_attn_fwd<T, HD, false><<<grid, kAttnWaves * kWave, 0, s>>>(a);
@@ -388,12 +627,28 @@ int64_t attn_row_tiles(const AttnArgs& a) {
 }
 
 // Split where the row tiles alone are fewer blocks than the GPU runs at once
-// twice over, into about kSplitBlocks, of at least kLeastChunk keys.
-constexpr int64_t kFewBlocks = 1024, kSplitBlocks = 2048, kLeastChunk = 256;
+// twice over, into about kSplitBlocks (kFewSplitBlocks of k_attn_few's larger
+// ones), of at least kLeastChunk keys.  More blocks read no faster and leave
+// more parts to join: chunks of 33 to 257 queries over 2000 to 8191 keys, kernel
+// and join 61 + 22 us with 2048, 59 + 19 with 1024, 60 + 18 with 512; one token
+// of 256 users 115 + 9, 116 + 9, 130 + 8; a million keys (k_attn_few) 111 + 20
+// with 2048, 97 + 14 with 1024, 94 + 10 with 512.
+constexpr int64_t kFewBlocks = 1024, kSplitBlocks = 1024, kFewSplitBlocks = 512, kLeastChunk = 256;
+// Where no bound of the queries is known the parts' room follows the largest
+// sequence that the rows allow; past this it is not taken.
+constexpr size_t kMostPartBytes = size_t(256) << 20;
 // Short sequences on the average are not split (nothing to join: 64 sessions of
 // up to 50 keys 7.6 + 3.5 -> 7.6 us) unless the keys are many enough for a long
 // one among them to matter.
 constexpr int64_t kShortKeyRows = 8192;
+
+// Whether k_attn_few takes the split: at most 32 rows, of at most 128 bytes.  (One
+// candidate set over a million keys of 64 bf16: 115 us in 64-key steps of the
+// general kernel, 95 so; one token of 256 users, 128 bf16, 113 and 120.)
+static bool attn_few_rows(const AttnArgs& a, int64_t most_q) {
+  const int width = a.d <= 32 ? 32 : a.d <= 64 ? 64 : 128;
+  return most_q * a.group <= 32 && width * (a.bf16 ? 2 : 4) <= 128;
+}
 
 size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at) {
   a->chunk = 0;
@@ -404,17 +659,19 @@ size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at) {
   int64_t most_q = a->q_pad > 0 ? a->q_pad : a->q_rows;
   if (a->q_pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
   const int64_t tiles = (most_q * a->group + kAttnRows - 1) / kAttnRows;
-  const int64_t chunk = a->kv_rows * a->hkv * tiles / kSplitBlocks;
-  a->chunk = static_cast<int>(std::max(kLeastChunk, (chunk + kAttnStep - 1) / kAttnStep * kAttnStep));
-  if (a->chunk >= most_keys) {
-    a->chunk = 0;
-    return 0;
-  }
+  const int64_t share = a->kv_rows * a->hkv * tiles / (attn_few_rows(*a, most_q) ? kFewSplitBlocks : kSplitBlocks);
+  const int64_t chunk = std::max(kLeastChunk, (share + kAttnStep - 1) / kAttnStep * kAttnStep);
+  if (chunk >= most_keys) return 0;
+  a->chunk = static_cast<int>(chunk);
   a->row_tiles = static_cast<int>(tiles);
+  a->few = attn_few_rows(*a, most_q);
   a->part_rows = static_cast<int>(std::min(most_q * a->group, int64_t(kAttnRows)));
   const size_t slots = static_cast<size_t>(key_chunks(*a)) * a->hkv * a->row_tiles * a->part_rows;
   *ml_at = (slots * a->d * sizeof(float) + 255) / 256 * 256;
-  return *ml_at + slots * 2 * sizeof(float);
+  const size_t bytes = *ml_at + slots * 2 * sizeof(float);
+  if (bytes <= kMostPartBytes) return bytes;
+  a->chunk = 0;
+  return 0;
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, hipStream_t s) {

@@ -89,6 +89,7 @@ AttnArgs attn_args(const rs_attn_desc& d) {
   a.hkv = d.heads_kv;
   a.group = d.heads_q / d.heads_kv;
   a.d = d.head_dim;
+  a.bf16 = d.dtype == RS_BF16;
   a.causal = d.causal != 0;
   a.scale = static_cast<float>(d.scale);
   a.cap = static_cast<float>(d.softcap);

@@ -61,6 +61,7 @@ struct AttnArgs {
   const float* slopes;
   int64_t q_rows, kv_rows, q_pad, kv_pad;
   int seqs, hq, hkv, group, d, causal;
+  bool bf16;
   float scale, cap;
   // outputs (and the backward's inputs): contiguous [rows][heads][d]
   void* out;
@@ -69,6 +70,7 @@ struct AttnArgs {
   // forward split along the keys (chunk > 0): chunks of that many keys, partial
   // results of up to part_rows rows of each block
   int chunk, row_tiles, part_rows;
+  bool few;  // at most 32 narrow rows a sequence and key head
   float *part_o, *part_ml;
   // backward
   const void *o, *o_rest, *dout;

@@ -234,6 +234,28 @@ def test_many_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_enough_sequences_for_whole_key_tiles(dtype, d):
+    """The backward takes larger key tiles where there are many of them: packed and padded, one and several heads a key head."""
+    print("tiles", dtype, d, flush=True)
+    g = torch.Generator().manual_seed(d)
+    lens = torch.randint(0, 30, (400,), generator=g)
+    lens[7], lens[200] = 300, 129
+    _case(dtype, 4, 4, d, lens.tolist(), slopes=True, cap=6.0, seed=1)
+    _case(dtype, 8, 4, d, lens.clamp(max=40).tolist(), q_pad=40, kv_pad=40, causal=False, seed=2, poison=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv", [(33, 1), (65, 1), (200, 1), (130, 2)])
+def test_many_heads_on_a_key_head(dtype, hq, hkv):
+    """More query heads on a key head than a step of the backward holds rows."""
+    print("groups", dtype, hq, hkv, flush=True)
+    _case(dtype, hq, hkv, 32, [3, 0, 1, 40, 70], slopes=True, seed=hq)
+    _case(dtype, hq, hkv, 64, [5, 1], [90, 700], max_q=5, cap=3.0, seed=hq + 1)
+    _case(dtype, hq, hkv, 128, [2, 9], causal=False, seed=hq + 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_values(dtype):
     """Large scores (one key takes all), equal scores, a scale of one's own."""
     print("values", dtype, flush=True)
