@@ -572,7 +572,14 @@ void run_keys(const AttnArgs& a, hipStream_t s) {
   if (n > 0) k_attn_dkdv<T, HD, FEW><<<static_cast<unsigned>(n), C::W * kWave, 0, s>>>(a);
 }
 
-constexpr int64_t kFewKeyBlocks = 1536;  // two to three times what the GPU runs at once
+// Where the larger tiles make fewer blocks than this, two to three times what the
+// GPU runs at once, the longest of them bounds the pass, and the small shape is
+// taken.  dk and dv with small / large tiles, us: 128 bf16, 128 large tiles (one
+// sequence of 8000, two heads) 233 / 572, 660 (24 documents, four query heads a
+// key head) 542 / 668, 2256 (32 sequences, eight heads) 524 / 435; 64 bf16, 314
+// (eight query heads a key head) 162 / 295, 1410 110 / 117, 24576 1238 / 938; 32
+// fp32, 128 lists 114 / 137.
+constexpr int64_t kFewKeyBlocks = 1536;
 
 template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {

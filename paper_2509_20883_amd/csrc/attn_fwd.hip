@@ -626,14 +626,19 @@ int64_t attn_row_tiles(const AttnArgs& a) {
   return a.q_rows * a.group / kAttnRows + a.seqs;
 }
 
-// Split where the row tiles alone are fewer blocks than the GPU runs at once
-// twice over, into about kSplitBlocks (kFewSplitBlocks of k_attn_few's larger
-// ones), of at least kLeastChunk keys.  More blocks read no faster and leave
-// more parts to join: chunks of 33 to 257 queries over 2000 to 8191 keys, kernel
-// and join 61 + 22 us with 2048, 59 + 19 with 1024, 60 + 18 with 512; one token
-// of 256 users 115 + 9, 116 + 9, 130 + 8; a million keys (k_attn_few) 111 + 20
-// with 2048, 97 + 14 with 1024, 94 + 10 with 512.
-constexpr int64_t kFewBlocks = 1024, kSplitBlocks = 1024, kFewSplitBlocks = 512, kLeastChunk = 256;
+// Split where the row tiles alone leave CUs without a block: fewer than
+// kFewBlocks, or for at most 32 rows a sequence and key head, whose parts are
+// small next to the keys, kFewRowBlocks.  (Kernel and join against one pass, 128
+// bf16: 88 row tiles, chunks of 33 to 257 queries over 2000 to 8191 keys, 59 + 19
+// and 174 us; 376 tiles, 200 to 300 queries over 2000 to 4000, 58 + 44 and 78; 512
+// tiles, four sequences of 4000, 104 + 80 and 127.)
+// About kSplitBlocks blocks (kFewSplitBlocks of k_attn_few's larger ones) of at
+// least kLeastChunk keys: more read no faster and leave more parts to join (that
+// chunk case 61 + 22 with 2048, 59 + 19 with 1024, 60 + 18 with 512; one token
+// of 256 users 115 + 9, 116 + 9, 130 + 8; a million keys (k_attn_few) 111 + 20 with
+// 2048, 97 + 14 with 1024, 94 + 10 with 512).
+constexpr int64_t kFewBlocks = 256, kFewRowBlocks = 1024;
+constexpr int64_t kSplitBlocks = 1024, kFewSplitBlocks = 512, kLeastChunk = 256;
 // Where no bound of the queries is known the parts' room follows the largest
 // sequence that the rows allow; past this it is not taken.
 constexpr size_t kMostPartBytes = size_t(256) << 20;
@@ -653,11 +658,12 @@ static bool attn_few_rows(const AttnArgs& a, int64_t most_q) {
 size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at) {
   a->chunk = 0;
   *ml_at = 0;
-  if (a->seqs == 0 || a->q_rows == 0 || attn_row_tiles(*a) * a->hkv >= kFewBlocks) return 0;
-  const int64_t most_keys = a->kv_pad > 0 ? a->kv_pad : a->kv_rows;  // of one sequence
-  if (most_keys < 2 * kLeastChunk || (a->kv_rows < kShortKeyRows && a->kv_rows / a->seqs < kLeastChunk)) return 0;
+  if (a->seqs == 0 || a->q_rows == 0) return 0;
   int64_t most_q = a->q_pad > 0 ? a->q_pad : a->q_rows;
   if (a->q_pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
+  if (attn_row_tiles(*a) * a->hkv >= (most_q * a->group <= 32 ? kFewRowBlocks : kFewBlocks)) return 0;
+  const int64_t most_keys = a->kv_pad > 0 ? a->kv_pad : a->kv_rows;  // of one sequence
+  if (most_keys < 2 * kLeastChunk || (a->kv_rows < kShortKeyRows && a->kv_rows / a->seqs < kLeastChunk)) return 0;
   const int64_t tiles = (most_q * a->group + kAttnRows - 1) / kAttnRows;
   const int64_t share = a->kv_rows * a->hkv * tiles / (attn_few_rows(*a, most_q) ? kFewSplitBlocks : kSplitBlocks);
   const int64_t chunk = std::max(kLeastChunk, (share + kAttnStep - 1) / kAttnStep * kAttnStep);

@@ -195,6 +195,22 @@ def test_other_keys_than_queries(dtype, causal):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (8, 1, 128), (3, 1, 32)])
+def test_chunks_over_long_keys(dtype, hq, hkv, d):
+    """Several row tiles over keys long enough to be split, chunks that no row sees, a padded side."""
+    print("long chunks", dtype, hq, hkv, d, flush=True)
+    ql, kl = [70, 0, 129, 1], [3000, 2000, 257, 5001]
+    for causal in (True, False):
+        for bound in (129, 0):
+            _case(dtype, hq, hkv, d, ql, kl, causal=causal, max_q=bound, seed=d, train=False)
+        _case(dtype, hq, hkv, d, ql, kl, causal=causal, slopes=True, cap=5.0, prefix=[100, 3, 300, 2600], max_q=129, seed=1,
+              train=False)
+    _case(dtype, hq, hkv, d, ql, kl, q_pad=130, kv_pad=5001, seed=2, train=False, poison=True)
+    # more queries than keys: the first rows of the sequence see nothing
+    _case(dtype, hq, hkv, d, [90, 700], [4000, 600], seed=3, train=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 257, 1000])
 def test_lengths_around_the_tiles(dtype, n):
     print("length", dtype, n, flush=True)
