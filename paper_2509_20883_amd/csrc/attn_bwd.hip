@@ -8,7 +8,15 @@
 // Two passes, each owning its outputs, so no sum is taken by atomics and
 // repeated calls agree bit for bit: one over key tiles for dk and dv, walking
 // over the packed rows (all query heads of the key head, so their gradients
-// add up in registers), one over row tiles for dq, walking over the keys.
+// add up in registers), one over row tiles for dq, walking over the keys.  The
+// scores and dP are computed in both, seven products instead of five; a single
+// pass would need atomics into one of the gradients.
+//
+// What bounds them: vector instructions and the waits between them, with two or
+// three blocks a CU (the gradients' registers allow no more).  1536 padded
+// sequences of 100 to 1024, 2 heads of 64, distances weighed and their slopes'
+// gradient taken: dq 800 us, dk and dv 921; 24 documents of 17 to 1500, 16 heads of
+// 128 over 4, capped: 287 and 535.  The matrix unit is 13 to 25% busy.
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"
