@@ -26,10 +26,12 @@
 namespace rs {
 namespace {
 
-// What the pass over keys needs of a row, four arrays of q_rows * heads_q words
+// What the pass over keys needs of a row, arrays of q_rows * heads_q words
 // written by k_attn_dq: -lse in base 2 (-infinity: no key seen, P = 0), delta,
-// the position (an integer), the slope in base 2 (where there are slopes).
-enum : int { kStatLse = 0, kStatDelta = 1, kStatPos = 2, kStatSlope = 3, kStats = 4 };
+// the position as an integer (for the mask), the slope in base 2 and the position
+// as a number (for the distance).
+enum : int { kStatLse = 0, kStatDelta = 1, kStatPos = 2, kStatSlope = 3, kStatPosF = 4, kStats = 5 };
+static_assert(kStats == kAttnStats, "the workspace holds them");
 
 // A word per lane from p + off (bytes; past 2^31: 0) to 64 consecutive words of LDS.
 __device__ inline void load_words(const float* p, uint32_t off, float* dst) {
@@ -233,9 +235,9 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
       if (a.slopes) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 pos = four(stat[buf][kStatPos], r + g * 8), slope = four(stat[buf][kStatSlope], r + g * 8);
+          const f32x4 pos = four(stat[buf][kStatPosF], r + g * 8), slope = four(stat[buf][kStatSlope], r + g * 8);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - static_cast<float>(__float_as_int(pos[e])));
+          for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - pos[e]);
         }
       }
 #pragma unroll
@@ -251,11 +253,14 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
       for (int g = 0; g < 4; ++g) {
         const f32x4 delta = four(stat[buf][kStatDelta], r + g * 8);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * g + e;
-          const float x = p[i] * (dp[i] - delta[e]);
-          ds[i] = a.cap > 0.0f ? x * ds[i] : x;
-        }
+        for (int e = 0; e < 4; ++e) dp[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - delta[e]);
+      }
+      if (a.cap > 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] *= dp[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = dp[i];
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -421,17 +426,18 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
     lse = INFINITY;
     delta = 0.0f;
   }
+  const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
+  const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
+  const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
   if (live && half == 0) {
     const int64_t n = a.q_rows * a.hq;
     a.stat[kStatLse * n + row] = -lse;
     a.stat[kStatDelta * n + row] = delta;
     a.stat[kStatPos * n + row] = __int_as_float(me.token + ks.len - qs.len);
-    a.stat[kStatSlope * n + row] = a.slopes ? a.slopes[me.head] * kLog2e : 0.0f;
+    a.stat[kStatSlope * n + row] = slope;
+    a.stat[kStatPosF * n + row] = pos;
   }
-  const float pos = static_cast<float>(me.token + ks.len - qs.len);
-  const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
-  const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
-  const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
   const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
 
   f32x16 acc[DT];
@@ -497,20 +503,23 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[i] = (i >> 2) * 8 + (i & 3) < left ? p[i] : 0.0f;
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dp[i] = p[i] * (dp[i] - delta);
       if (a.slope_part) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float t = fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3)));
-          const float x = p[i] * (dp[i] - delta);
           sum_pt += p[i] * t;
-          sum_x += x;
-          sum_xt += x * t;
+          sum_x += dp[i];
+          sum_xt += dp[i] * t;
         }
       }
+      if (a.cap > 0.0f) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = p[i] * (dp[i] - delta);
-        ds[i] = a.cap > 0.0f ? x * ds[i] : x;
+        for (int i = 0; i < 16; ++i) ds[i] *= dp[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = dp[i];
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {

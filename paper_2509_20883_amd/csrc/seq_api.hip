@@ -123,7 +123,7 @@ struct BwdWork {
 };
 BwdWork bwd_work(const AttnArgs& a) {
   BwdWork w{};
-  w.slope_part = align_up(4 * sizeof(float) * static_cast<size_t>(a.q_rows) * static_cast<size_t>(a.hq));
+  w.slope_part = align_up(kAttnStats * sizeof(float) * static_cast<size_t>(a.q_rows) * static_cast<size_t>(a.hq));
   w.total = w.slope_part + align_up(sizeof(float) * static_cast<size_t>(attn_row_tiles(a)) * static_cast<size_t>(a.hq));
   return w;
 }
