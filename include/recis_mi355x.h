@@ -474,8 +474,10 @@ rs_status layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x, int64
  * and strides multiples of 16 bytes, strides below 2^23 elements, 64 rows and
  * a group of q's heads within 2^31 bytes.  out and the gradients are contiguous.
  * q_offsets, kv_offsets: device int64 [seqs + 1], CSR (off[0] = 0,
- * nondecreasing).  q_pad = 0: packed, sequence s is rows off[s] .. off[s + 1];
- * rows outside every sequence are neither read nor written.  q_pad > 0: padded,
+ * nondecreasing, off[seqs] = the rows; validate checks it).  q_pad = 0: packed,
+ * sequence s is rows off[s] .. off[s + 1]; offsets that leave rows outside every
+ * sequence are accepted unless validated, and those rows neither read nor
+ * written.  q_pad > 0: padded,
  * q_rows = seqs * q_pad, sequence s is the first min(off[s+1] - off[s], q_pad)
  * rows from s * q_pad; the rows after them are never read (they may hold
  * anything), and their out and gradients are 0 and their lse -infinity.  kv_pad
@@ -491,7 +493,7 @@ typedef struct {
   int32_t head_dim;  /* a multiple of 8 in [8, 128]                               */
   int32_t causal;
   int32_t reserved;  /* 0 */
-  int64_t seqs, q_rows, kv_rows; /* q_rows * heads_q, kv_rows < 2^31              */
+  int64_t seqs, q_rows, kv_rows; /* seqs < 2^24; q_rows * heads_q, kv_rows < 2^31 - 1024 */
   int64_t q_pad, kv_pad;         /* rows per sequence of a padded layout; 0: packed */
   int64_t max_q;     /* the caller's bound of every Lq (0: none known); the launch
                         shape goes by it, and a longer sequence's rows past it may

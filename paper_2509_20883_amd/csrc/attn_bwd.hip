@@ -115,7 +115,7 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int64_t out_rows = a.kv_pad > 0 ? a.kv_pad : ks.len;
-  if (tile * C::KEYS >= out_rows) return;  // block-uniform
+  if (tile < 0 || tile * C::KEYS >= out_rows) return;  // block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
 
   const int j0 = static_cast<int>(tile) * C::KEYS;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
 
   // int arithmetic below is for tiles inside the sequence; another tile has no row
-  const bool none = tile * kAttnRows >= out_rows;
+  const bool none = tile < 0 || tile * kAttnRows >= out_rows;
   const int r0 = none ? 0 : static_cast<int>(tile) * kAttnRows;
   const int r = r0 + wave * 32 + col;
   const RowOf me = row_of(r, kvh, a.group);

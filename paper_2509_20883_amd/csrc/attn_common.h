@@ -226,7 +226,8 @@ __device__ inline SeqSpan seq_span(const int64_t* __restrict__ off, int s, int64
 // ceil(len * mul / per) tiles (floor((o + n) / per) - floor(o / per) + 1 >=
 // ceil(n / per)), strictly increasing in s, and end below
 // off[seqs] * mul / per + seqs.  Returns the sequence of block b, found by the
-// wave in steps of 64 sequences at a time, and the tile inside it.
+// wave in steps of 64 sequences at a time, and the tile inside it: below 0 for
+// a block before the first sequence (off[0] > 0, or offsets that fall).
 __device__ inline int64_t tile_base(const int64_t* __restrict__ off, int s, int mul, int per) {
   return max(off[s], int64_t(0)) * mul / per + s;
 }

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
       s = find_seq(a.kv_off, a.seqs, 1, a.chunk, blockIdx.x, c);
     }
     tile = blockIdx.z;
-    if (c * a.chunk >= int64_t(1) << 31) return;
+    if (c < 0 || c * a.chunk >= int64_t(1) << 31) return;
     c0 = static_cast<int>(c) * a.chunk;
   } else if (a.q_pad > 0) {
     const uint32_t per = static_cast<uint32_t>((a.q_pad * a.group + kAttnRows - 1) / kAttnRows);
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int rows = qs.len * a.group;  // the others of a padded sequence have no key
   const int64_t out_rows = a.q_pad > 0 ? a.q_pad * a.group : rows;
-  if (tile * kAttnRows >= out_rows) return;  // block-uniform
+  if (tile < 0 || tile * kAttnRows >= out_rows) return;  // block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
 
   const int r0 = static_cast<int>(tile) * kAttnRows;
@@ -317,7 +317,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
   } else {
     s = find_seq(a.kv_off, a.seqs, 1, a.chunk, blockIdx.x, ci);
   }
-  if (ci * a.chunk >= int64_t(1) << 31) return;
+  if (ci < 0 || ci * a.chunk >= int64_t(1) << 31) return;
   const int c0 = static_cast<int>(ci) * a.chunk;
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
   const int rows = min(qs.len * a.group, a.part_rows);
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(NT) void k_attn_join(const AttnArgs a) {
     s = find_seq(a.q_off, a.seqs, 1, 1, blockIdx.x, token);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
-  if (ks.len <= a.chunk || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // written, or no row; block-uniform
+  if (token < 0 || ks.len <= a.chunk || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // written, or no row; block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
   const int limit = token < qs.len ? key_limit(static_cast<int>(token), qs.len, ks.len, a.causal, prefix) : 0;
   const int chunks = (limit + a.chunk - 1) / a.chunk;

@@ -53,11 +53,11 @@ const char* check_attn(const rs_attn_desc* d) {
     return "heads_q must be a multiple of heads_kv, at most 8192";
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8 != 0) return "head_dim must be a multiple of 8 in [8, 128]";
   if (d->reserved != 0) return "reserved must be 0";
-  constexpr int64_t kMost = int64_t(1) << 31;
+  constexpr int64_t kMost = (int64_t(1) << 31) - 1024;  // a tile past the last row still counts in 32 bits
   if (d->seqs < 0 || d->seqs >= (int64_t(1) << 24)) return "seqs must be in [0, 2^24)";
-  if (d->q_rows < 0 || d->q_rows >= kMost || d->q_rows * d->heads_q >= kMost) return "q_rows * heads_q must be below 2^31";
-  if (d->kv_rows < 0 || d->kv_rows >= kMost) return "kv_rows must be in [0, 2^31)";
-  if (d->q_pad < 0 || d->q_pad >= kMost || d->kv_pad < 0 || d->kv_pad >= kMost) return "pad lengths must be in [0, 2^31)";
+  if (d->q_rows < 0 || d->q_rows >= kMost || d->q_rows * d->heads_q >= kMost) return "q_rows * heads_q must be below 2^31 - 1024";
+  if (d->kv_rows < 0 || d->kv_rows >= kMost) return "kv_rows must be in [0, 2^31 - 1024)";
+  if (d->q_pad < 0 || d->q_pad >= kMost || d->kv_pad < 0 || d->kv_pad >= kMost) return "pad lengths must be in [0, 2^31 - 1024)";
   if (d->q_pad > 0 && d->seqs * d->q_pad != d->q_rows) return "padded: q_rows must be seqs * q_pad";
   if (d->kv_pad > 0 && d->seqs * d->kv_pad != d->kv_rows) return "padded: kv_rows must be seqs * kv_pad";
   if (d->max_q < 0) return "max_q must be >= 0";

@@ -362,6 +362,34 @@ def test_repeats_streams_and_workspace():
         assert all(torch.equal(a, b) for a, b in zip(first, second))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_outside_every_sequence(dtype):
+    """Offsets that start past 0 and end before the last row: the rows outside are neither read nor written."""
+    print("outside", dtype, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    op = R.SeqAttention()
+    for q_lens, k_lens in (([40, 130], [40, 130]), ([1, 2], [700, 9000])):
+        nq, nk, lead = sum(q_lens), sum(k_lens), 300
+        q, do = (torch.randn(lead + nq + 9, 4, 64, generator=g, device="cuda").to(dtype) for _ in range(2))
+        k, v = (torch.randn(lead + nk + 9, 2, 64, generator=g, device="cuda").to(dtype) for _ in range(2))
+        in_q, in_k = slice(lead, lead + nq), slice(lead, lead + nk)
+        ref = op.forward(q[in_q], k[in_k], v[in_k], _offsets(q_lens), kv_offsets=_offsets(k_lens), max_q=max(q_lens))
+        want = (ref[0],) + op.backward(do[in_q], q[in_q], k[in_k], v[in_k], *ref, _offsets(q_lens),
+                                       kv_offsets=_offsets(k_lens))[:3]
+        for t, inside in ((q, in_q), (do, in_q), (k, in_k), (v, in_k)):
+            t[:lead], t[inside.stop:] = float("nan"), float("nan")
+        out = torch.full_like(q, 7.0)
+        qo, ko = _offsets(q_lens) + lead, _offsets(k_lens) + lead
+        _, stats = op.forward(q, k, v, qo, kv_offsets=ko, max_q=max(q_lens), out=out)
+        assert (out[:lead] == 7.0).all() and (out[in_q.stop:] == 7.0).all()
+        dq, dk, dv, _ = op.backward(do, q, k, v, out, stats, qo, kv_offsets=ko)
+        got = (out[in_q], dq[in_q], dk[in_k], dv[in_k])
+        for name, a, b in zip(("out", "dq", "dk", "dv"), got, want):
+            # the key chunks of a split start elsewhere: equal up to the order of the fp32 sums
+            tol = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -18
+            assert (a.double() - b.double()).norm() <= tol * b.double().norm(), name
+
+
 def test_offsets_past_32_bits():
     """A history whose keys lie more than 2^32 bytes into the tensor, in rows 2 KiB apart."""
     print("far keys", flush=True)
