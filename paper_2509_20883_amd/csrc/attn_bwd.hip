@@ -15,8 +15,8 @@
 // What bounds them: vector instructions and the waits between them, with two or
 // three blocks a CU (the gradients' registers allow no more).  1536 padded
 // sequences of 100 to 1024, 2 heads of 64, distances weighed and their slopes'
-// gradient taken: dq 800 us, dk and dv 921; 24 documents of 17 to 1500, 16 heads of
-// 128 over 4, capped: 287 and 535.  The matrix unit is 13 to 25% busy.
+// gradient taken: dq 820 us, dk and dv 905; 24 documents of 17 to 1500, 16 heads of
+// 128 over 4, capped: 290 and 527.  The matrix unit is 13 to 25% busy.
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"
@@ -215,22 +215,22 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
         dp = mma(f, vf[C::VALUES_IN_LDS ? 0 : t], dp);
       }
       // registers 4 g .. 4 g + 3 are rows r, r + 1, r + 2, r + 3
-      float p[16], ds[16];
+      float p[16], ds[16], sv[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sv[i] = sc[i];
       const int r = rb * 32 + half * 4;
       float c = scale2;
       if (a.cap > 0.0f) {
         c = cap2;
+        tanh_scores<T>(sv, inv_cap);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[i] = tanh_of<T>(sc[i] * inv_cap);
-          ds[i] = 1.0f - sc[i] * sc[i];
-        }
+        for (int i = 0; i < 16; ++i) ds[i] = 1.0f - sv[i] * sv[i];
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 lse = four(stat[buf][kStatLse], r + g * 8);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[4 * g + e] = sc[4 * g + e] * c + lse[e];
+        for (int e = 0; e < 4; ++e) p[4 * g + e] = sv[4 * g + e] * c + lse[e];
       }
       if (a.slopes) {
 #pragma unroll
@@ -346,8 +346,12 @@ __device__ inline float dot8(const f32x8s& x, const f32x8s& y) {
 // sequences of 100 to 1024 keys with distances weighed).
 //
 // The slopes' gradient is taken per row, with x_j = P (dP - delta) and t = |p -
-// j|, as sum_j x t - (sum_j x) (sum_j P t): the sum of x is 0 but for delta's
-// own error, which would else be weighed by every distance.
+// j|, as (sum_j x t - (sum_j x) (sum_j P t) / sum_j P) / sum_j P: the sum of x
+// is 0 but for delta's own error, which would else be weighed by every
+// distance, and the sum of P is 1 but for the rounding of lse.  Without the
+// latter and the sums of 16 keys at a time it was off by up to 2.3e-6 of its
+// norm, now by 2e-7 to 9e-7 (fp32 matrix products of the same inputs 3e-7 to
+// 2.2e-6), for 8% of this kernel's time where slopes are learnt.
 template <typename T, int HD>
 __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) void k_attn_dq(const AttnArgs a) {
   typedef Tile<T, HD> L;
@@ -443,7 +447,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
   f32x16 acc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-  float sum_pt = 0.0f, sum_x = 0.0f, sum_xt = 0.0f;
+  float sum_p = 0.0f, sum_pt = 0.0f, sum_x = 0.0f, sum_xt = 0.0f;
 
   int buf = 0;
   for (int j0 = 0; j0 < end; j0 += kAttnStep, buf ^= 1) {
@@ -474,27 +478,27 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
       }
       const int j = j0 + kb * 32 + half * 4;  // register i is key j + (i / 4) * 8 + i % 4
       const float dist = static_cast<float>(j) - pos;
-      float p[16], ds[16];
+      float p[16], ds[16], sv[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sv[i] = sc[i];
       float c = scale2;
       if (a.cap > 0.0f) {
         c = cap2;
+        tanh_scores<T>(sv, inv_cap);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[i] = tanh_of<T>(sc[i] * inv_cap);
-          ds[i] = 1.0f - sc[i] * sc[i];
-        }
+        for (int i = 0; i < 16; ++i) ds[i] = 1.0f - sv[i] * sv[i];
       }
       if (!a.slopes) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = sc[i] * c - lse;
+        for (int i = 0; i < 16; ++i) p[i] = sv[i] * c - lse;
       } else if (sign != 0) {
         const float e = sign > 0 ? slope : -slope, b = dist * e - lse;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = sc[i] * c + (e * static_cast<float>((i >> 2) * 8 + (i & 3)) + b);
+        for (int i = 0; i < 16; ++i) p[i] = sv[i] * c + (e * static_cast<float>((i >> 2) * 8 + (i & 3)) + b);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          p[i] = sc[i] * c - (slope * fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3))) + lse);
+          p[i] = sv[i] * c - (slope * fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3))) + lse);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exp2_hw(p[i]);
@@ -505,14 +509,35 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) dp[i] = p[i] * (dp[i] - delta);
-      if (a.slope_part) {
+      if (a.slope_part) {  // the 16 keys' sums first: shorter chains, less rounding
+        float sp = 0.0f, x = 0.0f, pt = 0.0f, xt = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float t = fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3)));
-          sum_pt += p[i] * t;
-          sum_x += dp[i];
-          sum_xt += dp[i] * t;
+          sp += p[i];
+          x += dp[i];
         }
+        if (sign != 0) {  // one side of the row: |dist + c| = -sign (dist + c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float c = static_cast<float>((i >> 2) * 8 + (i & 3));
+            pt += p[i] * c;
+            xt += dp[i] * c;
+          }
+          const float e = sign > 0 ? -1.0f : 1.0f;
+          pt = e * (dist * sp + pt);
+          xt = e * (dist * x + xt);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float t = fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3)));
+            pt += p[i] * t;
+            xt += dp[i] * t;
+          }
+        }
+        sum_p += sp;
+        sum_x += x;
+        sum_pt += pt;
+        sum_xt += xt;
       }
       if (a.cap > 0.0f) {
 #pragma unroll
@@ -549,8 +574,8 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
   if (a.slope_part) {
     __syncthreads();  // the rows have been read
     float* per_row = reinterpret_cast<float*>(lds);
-    const float pt = other_half_sum(sum_pt), sx = other_half_sum(sum_x), sxt = other_half_sum(sum_xt);
-    if (half == 0) per_row[wave * 32 + col] = live ? sx * pt - sxt : 0.0f;
+    const float sp = other_half_sum(sum_p), pt = other_half_sum(sum_pt), sx = other_half_sum(sum_x), sxt = other_half_sum(sum_xt);
+    if (half == 0) per_row[wave * 32 + col] = live && sp != 0.0f ? (sx * (pt / sp) - sxt) / sp : 0.0f;
     __syncthreads();
     // rows of one head are `group` apart; every block's first row is head r0 % group
     for (int g = threadIdx.x; g < a.group; g += kAttnWaves * kWave) {

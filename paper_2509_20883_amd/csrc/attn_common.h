@@ -185,18 +185,42 @@ __device__ inline float other_half_sum(float x) {
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh.  bf16: 1 - 2 / (e^2x + 1) on the hardware's exp2 and reciprocal, off
-// by about 1e-7 whatever x; fp32 scores keep the relative accuracy near 0
-// that the library function has.
+// x = tanh(scale x) of 16 scores.  fp32 has the library's function.  bf16, by
+// |scale x|: up to 1/2, x + x^3 P(x^2) with P fitted to the least largest error,
+// off by 7e-8 of the value; above, 1 - 2 / (e^2x + 1) on the hardware's exp2 and
+// reciprocal, off by 1e-7.  A score's value goes by itself alone, so that the
+// passes agree on it; a wave whose scores are all small, as caps are used,
+// leaves out the exponents.
 template <typename T>
-__device__ inline float tanh_of(float x);
+__device__ inline void tanh_scores(float (&x)[16], float scale);
 template <>
-__device__ inline float tanh_of<uint16_t>(float x) {
-  return 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_hw(x * (2.0f * kLog2e)) + 1.0f);
+__device__ inline void tanh_scores<float>(float (&x)[16], float scale) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = tanhf(x[i] * scale);
+}
+__device__ inline float tanh_small(float x) {
+  const float u = x * x;
+  const float p = -0.3333314955f + u * (0.1332598776f + u * (-0.0530529357f + u * 0.0172569603f));
+  return x + x * (u * p);
 }
 template <>
-__device__ inline float tanh_of<float>(float x) {
-  return tanhf(x);
+__device__ inline void tanh_scores<uint16_t>(float (&x)[16], float scale) {
+  float most = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    x[i] *= scale;
+    most = fmaxf(most, fabsf(x[i]));
+  }
+  if (__all(most <= 0.5f)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = tanh_small(x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float big = 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_hw(x[i] * (2.0f * kLog2e)) + 1.0f);
+      x[i] = fabsf(x[i]) <= 0.5f ? tanh_small(x[i]) : big;
+    }
+  }
 }
 
 // First row and length of sequence s among `rows` rows: packed, rows

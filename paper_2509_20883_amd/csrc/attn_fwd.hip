@@ -159,9 +159,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
     if (a.cap > 0.0f) {
       c = cap2;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[kb][i] = tanh_of<T>(p[kb][i] * inv_cap);
+      for (int kb = 0; kb < 2; ++kb) tanh_scores<T>(p[kb], inv_cap);
     }
     if (!a.slopes) {
 #pragma unroll
@@ -383,8 +381,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
     float c = scale2;
     if (a.cap > 0.0f) {
       c = cap2;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = tanh_of<T>(p[i] * inv_cap);
+      tanh_scores<T>(p, inv_cap);
     }
     if (!a.slopes) {
 #pragma unroll

@@ -390,6 +390,14 @@ def test_rows_outside_every_sequence(dtype):
             assert (a.double() - b.double()).norm() <= tol * b.double().norm(), name
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cap, spread", [(100.0, 1.0), (2.0, 1.0), (2.0, 6.0)])
+def test_small_and_saturated_caps(dtype, cap, spread):
+    """All scores below half the cap, on both sides of it, and far past it."""
+    print("caps", dtype, cap, spread, flush=True)
+    _case(dtype, 4, 2, 64, [33, 1, 0, 150, 64], cap=cap, spread=spread, slopes=True, causal=False, seed=9)
+
+
 def test_offsets_past_32_bits():
     """A history whose keys lie more than 2^32 bytes into the tensor, in rows 2 KiB apart."""
     print("far keys", flush=True)
