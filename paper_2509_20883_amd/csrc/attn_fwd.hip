@@ -15,12 +15,12 @@
 // What bounds it.  Per score the products take 4 HD operations, which the matrix
 // unit does in HD / 256 cycles a lane column, and the softmax 5 to 8 vector
 // instructions (scale, maximum, exponent, sum, rounding; 3 more for a distance
-// term, 5 and two more transcendental ones for a cap): at HD = 128 the two are
+// term, 8 for a cap, and two transcendental ones where a score passes its half): at HD = 128 the two are
 // even, below it the vector unit bounds.  One causal sequence of 16384, 8 heads
 // of 128 bf16: 587 us, 936 TFLOP/s of the scores it needs (a large library
 // product reaches 1329); matrix unit 37% busy, vector unit 44%.  1536 padded
-// sequences of 100 to 1024, 2 heads of 64, distances weighed: 460 us, vector unit
-// 61% busy.  One token for each of 256 users, 8 heads of 128 over 2: 4.9 TB/s.
+// sequences of 100 to 1024, 2 heads of 64, distances weighed: 467 us, vector unit
+// 61% busy.  One token for each of 256 users, 8 heads of 128 over 2: 117 us, 4.5 TB/s with the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
