@@ -319,35 +319,39 @@ __device__ inline int key_limit(int token, int lq, int lk, bool causal, int pref
 // no registers hold them and the wave goes on; wait_tiles() before their use.
 // The lane picks the chunk that belongs at its place, so the tile's chunk
 // order costs nothing.  The buffer's bounds do the masking: rows past the
-// sequence's end and columns past d lie outside and arrive as zeros.
+// sequence's end and columns past d lie outside and arrive as zeros.  A wave's
+// rows are consecutive (at most 32) and its buffer starts at the first of them:
+// their offsets stay below 2^31, where the bounds end, up to the largest stride.
 template <typename T, int HD, int N = kAttnStep, int W = kAttnWaves>
 struct TileLoader {
   typedef Tile<T, HD> L;
   static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);  // per thread of W waves
   static_assert(kLoads >= 1 && kLoads * W * kWave * 16 == N * L::kRowBytes, "whole loads");
-  uint32_t off[kLoads];  // byte offset of the thread's chunks from the tile's first row
+  static constexpr int kRows = N / W;  // a wave's share
+  static_assert(kRows * W == N && kRows <= 32, "32 rows of 2^23 fp32 elements span 2^30 bytes");
+  uint32_t off[kLoads];  // byte offset of the thread's chunks from the wave's first row
   int64_t row_bytes;
-  const char* base;  // the sequence's first row
-  int len, d_bytes;
+  const char* base;  // the wave's first row of the sequence's first tile
+  int len, d_bytes;  // rows from there to the sequence's end
 
   __device__ inline void init(const void* p, int64_t start, int64_t row, int64_t head_off, int d, int n) {
+    const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
     row_bytes = row * static_cast<int64_t>(sizeof(T));
-    base = static_cast<const char*>(p) + (start * row + head_off) * static_cast<int64_t>(sizeof(T));
-    len = n;
+    base = static_cast<const char*>(p) + ((start + wave * kRows) * row + head_off) * static_cast<int64_t>(sizeof(T));
+    len = n - wave * kRows;
     d_bytes = d * static_cast<int>(sizeof(T));
-    const int wave = W == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = ((wave * kLoads + i) * kWave + lane) * 16;
-      const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(r);
+      const int at = (i * kWave + lane) * 16;
+      const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(wave * kRows + r);
       off[i] = c * 16 < d_bytes ? r * static_cast<uint32_t>(row_bytes) + c * 16 : 0x80000000u;
     }
   }
-  // Rows j0 .. j0 + N - 1 of the sequence (j0 < len).
+  // Rows j0 .. j0 + N - 1 of the sequence (j0 < its length).
   __device__ inline void load(char* tile, int j0) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass has no buffer descriptors
-    const int rows = min(N, len - j0);
-    const int bytes = max(rows - 1, 0) * static_cast<int>(row_bytes) + d_bytes;
+    const int rows = min(kRows, len - j0);
+    const int bytes = rows > 0 ? (rows - 1) * static_cast<int>(row_bytes) + d_bytes : 0;
     const char* p = base + j0 * row_bytes;
     const uint64_t u = reinterpret_cast<uint64_t>(p);
     // readfirstlane gives a signed int: no sign may reach the upper word
@@ -379,22 +383,26 @@ struct RowLoader {
   typedef Tile<T, HD> L;
   static constexpr int kLoads = N * L::kRowBytes / (W * kWave * 16);
   static_assert(kLoads >= 1 && kLoads * W * kWave * 16 == N * L::kRowBytes, "whole loads");
+  static constexpr int kRows = N / W;  // a wave's share
+  static_assert(kRows * W == N && kRows <= 16, "at most 16 tokens and a group of heads: below 2^31 bytes");
   uint32_t off[kLoads];
   int64_t row_bytes, head_bytes;
-  const char* base;  // the sequence's first token, the group's first head
+  const char* base;  // the sequence's first token (of the wave's rows), the group's first head
 
   __device__ inline void init(const HeadRows& t, int64_t start, int kvh, int group, int d) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
+    const int tok0 = group <= N ? div_group(wave * kRows, group) : 0;  // of the wave's first row
     row_bytes = t.row * static_cast<int64_t>(sizeof(T));
     head_bytes = t.head * static_cast<int64_t>(sizeof(T));
-    base = static_cast<const char*>(t.p) + start * row_bytes + static_cast<int64_t>(kvh) * group * head_bytes;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    base = static_cast<const char*>(t.p) + (start + tok0) * row_bytes + static_cast<int64_t>(kvh) * group * head_bytes;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int at = ((wave * kLoads + i) * kWave + lane) * 16;
       const int r = at / L::kRowBytes, c = ((at % L::kRowBytes) >> 4) ^ L::key(r);
       const int tok = group <= N ? div_group(r, group) : 0;
       off[i] = c * 16 < d * static_cast<int>(sizeof(T))
-                   ? tok * static_cast<uint32_t>(row_bytes) + (r - tok * group) * static_cast<uint32_t>(head_bytes) + c * 16
+                   ? (tok - tok0) * static_cast<uint32_t>(row_bytes) +
+                         (r - tok * group) * static_cast<uint32_t>(head_bytes) + c * 16
                    : 0x80000000u;
     }
   }

@@ -65,7 +65,7 @@ const char* check_attn(const rs_attn_desc* d) {
   for (const int64_t st : {d->q_stride, d->q_head_stride, d->k_stride, d->k_head_stride, d->v_stride, d->v_head_stride})
     if (st < 0 || st >= (int64_t(1) << 23) || st % unit != 0)
       return "strides must be multiples of 16 bytes in [0, 2^23) elements";
-  // a step of 64 packed rows is addressed with 32 bits
+  // a wave's share of a step of packed rows, at most 16 tokens and a group of heads, is addressed with 31 bits
   const int64_t es = d->dtype == RS_BF16 ? 2 : 4;
   if ((64 * d->q_stride + d->heads_q / d->heads_kv * d->q_head_stride) * es >= kMost)
     return "64 rows and a group of heads of q must span less than 2^31 bytes";
