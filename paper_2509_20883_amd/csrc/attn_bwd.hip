@@ -28,9 +28,8 @@ namespace {
 
 // What the pass over keys needs of a row, arrays of q_rows * heads_q words
 // written by k_attn_dq: -lse in base 2 (-infinity: no key seen, P = 0), delta,
-// the position as an integer (for the mask), the slope in base 2 and the position
-// as a number (for the distance).
-enum : int { kStatLse = 0, kStatDelta = 1, kStatPos = 2, kStatSlope = 3, kStatPosF = 4, kStats = 5 };
+// the position as an integer (for the mask) and the slope in base 2.
+enum : int { kStatLse = 0, kStatDelta = 1, kStatPos = 2, kStatSlope = 3, kStats = 4 };
 static_assert(kStats == kAttnStats, "the workspace holds them");
 
 // A word per lane from p + off (bytes; past 2^31: 0) to 64 consecutive words of LDS.
@@ -97,7 +96,10 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
   char *key_tile = lds + 4 * kTile, *val_tile = key_tile + kKeyTile;
   // of the step's rows, as k_attn_dq left them; 0 where there is no row: its q and dout are 0 too, and add nothing
   constexpr int kStatRows = kStep < kWave ? kWave : kStep;
-  __shared__ __align__(16) float stat[2][kStats][kStatRows];
+  // and the row's position from the step's first token on, the same in every step:
+  // fp32 then holds the distances of near keys however long the sequence is
+  constexpr int kStepPos = kStats;
+  __shared__ __align__(16) float stat[2][kStats + 1][kStatRows];
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
@@ -133,7 +135,6 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
     }
   }
   const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
-  const float key = static_cast<float>(j);
   const int see_all = a.causal ? prefix : ks.len;  // keys that every row sees
 
   f32x16 dk[DT], dv[DT];
@@ -157,6 +158,7 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
   const int stat_row = threadIdx.x;
   const int stat_up = steps.parts > 1 ? 0 : div_group(stat_row, a.group);
   const uint32_t stat_off = static_cast<uint32_t>(stat_up * a.hq + stat_row - stat_up * a.group) * 4;
+  if (stat_row < kStep) stat[0][kStepPos][stat_row] = stat[1][kStepPos][stat_row] = static_cast<float>(stat_up);
   const int stat_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   auto fetch = [&](int n, int buf) {
     const int tok = first + (steps.parts > 1 ? n / steps.parts : n * steps.tokens);
@@ -233,9 +235,10 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
         for (int e = 0; e < 4; ++e) p[4 * g + e] = sv[4 * g + e] * c + lse[e];
       }
       if (a.slopes) {
+        const float key = static_cast<float>(j - (tok + ks.len - qs.len));
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 pos = four(stat[buf][kStatPosF], r + g * 8), slope = four(stat[buf][kStatSlope], r + g * 8);
+          const f32x4 pos = four(stat[buf][kStepPos], r + g * 8), slope = four(stat[buf][kStatSlope], r + g * 8);
 #pragma unroll
           for (int e = 0; e < 4; ++e) p[4 * g + e] -= slope[e] * fabsf(key - pos[e]);
         }
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
     lse = INFINITY;
     delta = 0.0f;
   }
-  const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int pos = me.token + ks.len - qs.len;
   const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
   const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
@@ -438,9 +441,8 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
     const int64_t n = a.q_rows * a.hq;
     a.stat[kStatLse * n + row] = -lse;
     a.stat[kStatDelta * n + row] = delta;
-    a.stat[kStatPos * n + row] = __int_as_float(me.token + ks.len - qs.len);
+    a.stat[kStatPos * n + row] = __int_as_float(pos);
     a.stat[kStatSlope * n + row] = slope;
-    a.stat[kStatPosF * n + row] = pos;
   }
   const float scale2 = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
 
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
         dp = mma(f, of[t], dp);
       }
       const int j = j0 + kb * 32 + half * 4;  // register i is key j + (i / 4) * 8 + i % 4
-      const float dist = static_cast<float>(j) - pos;
+      const float dist = static_cast<float>(j - pos);
       float p[16], ds[16], sv[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) sv[i] = sc[i];

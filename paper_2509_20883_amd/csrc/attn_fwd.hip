@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
       if (live && k0 < a.d) load_frag(q + k0, qf[t]);
     }
   }
-  const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int pos = me.token + ks.len - qs.len;
   const int wave_pos0 = div_group(w0, a.group) + ks.len - qs.len;
   const int wave_pos1 = div_group(max(w1, w0), a.group) + ks.len - qs.len;
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[kb][i] = p[kb][i] * c - m;
     } else {
-      const float dist = static_cast<float>(j) - pos;
+      const float dist = static_cast<float>(j - pos);
       const int sign = dist_sign(j0, j0 + kAttnStep - 1, wave_pos0, wave_pos1);
       if (sign != 0) {
         const float e = sign > 0 ? slope : -slope, b = dist * e - m;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
       if (live && k0 < a.d) load_frag(q + k0, qf[t]);
     }
   }
-  const float pos = static_cast<float>(me.token + ks.len - qs.len);
+  const int pos = me.token + ks.len - qs.len;
   const float slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
   const float inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e, scale2 = a.scale * kLog2e;
 
@@ -387,7 +387,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = p[i] * c - m;
     } else {
-      const float dist = static_cast<float>(j) - pos;
+      const float dist = static_cast<float>(j - pos);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         p[i] = p[i] * c - (slope * fabsf(dist + static_cast<float>((i >> 2) * 8 + (i & 3))) + m);

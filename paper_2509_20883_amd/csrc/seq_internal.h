@@ -85,7 +85,7 @@ struct AttnArgs {
 size_t plan_attn_split(AttnArgs* a, int64_t max_q, size_t* ml_at);
 hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, hipStream_t s);
 // Words per query row and head that the backward's first pass leaves for its second.
-constexpr int kAttnStats = 5;
+constexpr int kAttnStats = 4;
 hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, hipStream_t s);
 // Blocks of the pass over query rows (each leaves one partial sum per head
 // of the slopes' gradient).
