@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   const bool joined = SPLIT && ks.len > a.chunk;  // other blocks hold parts of these rows
   if (SPLIT) {
     if (c0 > 0 && c0 >= end) return;  // block-uniform; the join does not look here
-    end = min(end, c0 + a.chunk);
+    end = c0 + min(end - c0, a.chunk);  // c0 + chunk may pass 2^31
   }
   const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows) - 1;
   const int wave_least = w0 < rows ? key_limit(div_group(w0, a.group), qs.len, ks.len, a.causal, prefix) : 0;
@@ -328,7 +328,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
   const int least = rows > 0 ? key_limit(0, qs.len, ks.len, a.causal, prefix) : 0;
   const bool joined = ks.len > a.chunk;
   if (c0 > 0 && c0 >= end) return;  // block-uniform; the join does not look here
-  end = min(end, c0 + a.chunk);
+  end = c0 + min(end - c0, a.chunk);  // c0 + chunk may pass 2^31
 
   // the wave's blocks of 32 keys: first, first + 32 W, ...
   const int first = c0 + wave * 32;
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(NT) void k_attn_join(const AttnArgs a) {
   if (token < 0 || ks.len <= a.chunk || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // written, or no row; block-uniform
   const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
   const int limit = token < qs.len ? key_limit(static_cast<int>(token), qs.len, ks.len, a.causal, prefix) : 0;
-  const int chunks = (limit + a.chunk - 1) / a.chunk;
+  const int chunks = static_cast<int>((static_cast<uint32_t>(limit) + a.chunk - 1) / a.chunk);
   const int64_t first = a.kv_pad > 0 ? s * ((a.kv_pad + a.chunk - 1) / a.chunk) : tile_base(a.kv_off, s, 1, a.chunk);
   const int r = static_cast<int>(token) * a.group + head - kvh * a.group;
   const int64_t tile = r / kAttnRows, at = r % kAttnRows;

@@ -55,3 +55,26 @@ def test_distances_past_2_24_keys(dtype, hq, hkv, d, causal):
         _close(t, *want[0][name], name)
     _close(dm, wm, em, "dslopes")
     assert not dk[:-w].any() and not dv[:-w].any()
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 8), (torch.float32, 64)])
+def test_last_chunk_of_the_longest_history(dtype, d):
+    """One row over nearly 2^31 keys, all of them one row of memory, scores falling by 0.01 a key: the last keys carry
+    the sum, and the last chunk of the split ends past the 32-bit whole numbers."""
+    print("longest", dtype, d, flush=True)
+    n, slope = (1 << 31) - 2048, 0.01
+    g = torch.Generator(device="cuda").manual_seed(d)
+    row = torch.randn(1, 1, d, generator=g, device="cuda").to(dtype)
+    q = torch.randn(1, 1, d, generator=g, device="cuda").to(dtype)
+    keys = row.expand(n, -1, -1)
+    m = torch.full((1,), slope, device="cuda")
+    out, stats = R.SeqAttention().forward(q, keys, keys, _offsets([1]), kv_offsets=_offsets([n]), slopes=m, max_q=1)
+    u = 2.0 ** -24
+    s = float((q.double() * row.double()).sum()) * d ** -0.5
+    want = s - float(torch.log(-torch.expm1(-m.double())))  # sum over t >= 0 of e^(-slope t)
+    # the keys that count (e^(-slope t) > u) lie within 1700; their scores and distance terms are at most 17 + |s|, and a
+    # lane adds up at most 64 of them in a row before the lanes and the parts are added in trees
+    assert abs(float(stats.lse) - want) <= (8 * (17 + abs(s)) + (d + 8) * float((q.double() * row.double()).abs().sum()) + 512) * u
+    # probabilities that sum to one over equal rows: v, off by their rounding to bf16 and the result's
+    r = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    _close(out, row.double(), row.double().abs() * (r + 600 * u), "out")
