@@ -104,7 +104,7 @@ __global__ __launch_bounds__((KeyShape<T, HD, FEW>::W * kWave), (KeyShape<T, HD,
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
   const int kw = wave % C::KW, rw = wave / C::KW;
-  const BlockOf blk = block_of(a.hkv, false);
+  const BlockOf blk = block_of(a, false);
   const int kvh = blk.kvh;
   int s;
   int64_t tile;
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentRowBlocks<T, HD>)) voi
 
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int half = lane >> 5, col = lane & 31;
-  const BlockOf blk = block_of(a.hkv, true);
+  const BlockOf blk = block_of(a, true);
   const int kvh = blk.kvh;
   int s;
   int64_t tile;
@@ -612,8 +612,7 @@ int64_t key_tiles(const AttnArgs& a, int keys) {
 template <typename T, int HD, bool FEW>
 void run_keys(const AttnArgs& a, hipStream_t s) {
   typedef KeyShape<T, HD, FEW> C;
-  const int64_t n = key_tiles(a, C::KEYS) * a.hkv;
-  if (n > 0) k_attn_dkdv<T, HD, FEW><<<static_cast<unsigned>(n), C::W * kWave, 0, s>>>(a);
+  launch_blocks<C::W * kWave>(k_attn_dkdv<T, HD, FEW>, a, key_tiles(a, C::KEYS) * a.hkv, s);
 }
 
 // Where the larger tiles make fewer blocks than this, two to three times what the
@@ -628,7 +627,7 @@ constexpr int64_t kFewKeyBlocks = 1536;
 template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
   const int64_t qt = attn_row_tiles(a);
-  if (qt > 0) k_attn_dq<T, HD><<<static_cast<unsigned>(qt * a.hkv), kAttnWaves * kWave, 0, s>>>(a);
+  launch_blocks<kAttnWaves * kWave>(k_attn_dq<T, HD>, a, qt * a.hkv, s);
   if (key_tiles(a, KeyShape<T, HD, false>::KEYS) * a.hkv < kFewKeyBlocks && HD * sizeof(T) <= 256) run_keys<T, HD, true>(a, s);
   else run_keys<T, HD, false>(a, s);
   if (a.dslopes) k_attn_dslopes<<<a.hq, kSlopeThreads, 0, s>>>(a, qt);

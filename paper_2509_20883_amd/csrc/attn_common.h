@@ -287,14 +287,27 @@ struct BlockOf {
   int64_t tile;
   int kvh;
 };
-__device__ inline BlockOf block_of(int hkv, bool back) {
-  const uint32_t tiles = gridDim.x / hkv;
-  uint32_t b = xcd_runs<kTileRun>(blockIdx.x, gridDim.x);
-  if (back) b = gridDim.x - 1 - b;
+__device__ inline BlockOf block_of(const AttnArgs& a, bool back) {
+  const uint32_t tiles = a.blocks / a.hkv;
+  uint32_t b = xcd_runs<kTileRun>(a.block0 + blockIdx.x, a.blocks);
+  if (back) b = a.blocks - 1 - b;
   BlockOf x;
   x.kvh = b / tiles;
   x.tile = b - x.kvh * tiles;
   return x;
+}
+
+// The kernel over so many blocks, in launches of at most 2^22 of them, whole sets
+// of tile runs.
+template <int THREADS, typename K>
+inline void launch_blocks(K* kernel, AttnArgs a, int64_t blocks, hipStream_t s) {
+  constexpr int64_t kMost = int64_t(1) << 22;
+  static_assert(kMost * THREADS < int64_t(1) << 32 && kMost % (8 * kTileRun) == 0, "a launch's threads");
+  a.blocks = static_cast<uint32_t>(blocks);
+  for (int64_t b = 0; b < blocks; b += kMost) {
+    a.block0 = static_cast<uint32_t>(b);
+    kernel<<<static_cast<unsigned>(blocks - b < kMost ? blocks - b : kMost), THREADS, 0, s>>>(a);
+  }
 }
 
 // Rows of a sequence are packed head by head: row r is token r / group, query

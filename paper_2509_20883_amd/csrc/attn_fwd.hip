@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
   int c0 = 0;  // the block's first key
   BlockOf blk{};
   if (!SPLIT) {
-    blk = block_of(a.hkv, true);
+    blk = block_of(a, true);
     kvh = blk.kvh;
   }
   if (SPLIT) {
@@ -615,8 +615,7 @@ hipError_t run(const AttnArgs& a, hipStream_t s) {
     if (key_chunks(a) / a.seqs > 32) k_attn_join<T, 1024><<<jg, 1024, 0, s>>>(a);
     else k_attn_join<T, 128><<<jg, 128, 0, s>>>(a);
   } else {
-    const unsigned grid = static_cast<unsigned>(attn_row_tiles(a) * a.hkv);
-    k_attn_fwd<T, HD, false><<<grid, kAttnWaves * kWave, 0, s>>>(a);
+    launch_blocks<kAttnWaves * kWave>(k_attn_fwd<T, HD, false>, a, attn_row_tiles(a) * a.hkv, s);
   }
   return hipGetLastError();
 }

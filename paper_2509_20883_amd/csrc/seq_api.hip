@@ -69,7 +69,7 @@ const char* check_attn(const rs_attn_desc* d) {
   const int64_t es = d->dtype == RS_BF16 ? 2 : 4;
   if ((64 * d->q_stride + d->heads_q / d->heads_kv * d->q_head_stride) * es >= kMost)
     return "64 rows and a group of heads of q must span less than 2^31 bytes";
-  if (attn_blocks(*d) >= kMost) return "too many sequences and rows for one launch";
+  if (attn_blocks(*d) >= kMost) return "too many sequences, rows and key heads: below 2^31 blocks";
   if (!(d->scale > 0.0) || !std::isfinite(d->scale)) return "scale must be finite and > 0";
   if (!(d->softcap >= 0.0) || !std::isfinite(d->softcap)) return "softcap must be finite and >= 0";
   return nullptr;

@@ -57,6 +57,8 @@ struct HeadRows {
 
 struct AttnArgs {
   HeadRows q, k, v;
+  // the launch's first block of all: HIP takes fewer than 2^32 threads along an axis
+  uint32_t block0, blocks;
   const int64_t *q_off, *kv_off, *prefix;
   const float* slopes;
   int64_t q_rows, kv_rows, q_pad, kv_pad;

@@ -78,3 +78,23 @@ def test_last_chunk_of_the_longest_history(dtype, d):
     # probabilities that sum to one over equal rows: v, off by their rounding to bf16 and the result's
     r = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
     _close(out, row.double(), row.double().abs() * (r + 600 * u), "out")
+
+
+def test_more_blocks_than_one_launch_takes():
+    """Three million sequences of one row, eight key heads: 24 million blocks, and HIP takes fewer than 2^32 threads."""
+    print("many blocks", flush=True)
+    n, h, d = 3000000, 8, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, do = (torch.randn(n, h, d, generator=g, device="cuda").bfloat16() for _ in range(4))
+    off = torch.arange(n + 1, device="cuda")
+    op = R.SeqAttention()
+    out, stats = op.forward(q, k, v, off)
+    dq, dk, dv, _ = op.backward(do, q, k, v, out, stats, off)
+    assert torch.equal(out, v) and torch.equal(dv, do)  # one key: probability 1
+    x = (q.float() * k.float()).sum(2) * d ** -0.5
+    u = 2.0 ** -24
+    lim = (d + 8) * u * (q.float() * k.float()).abs().sum(2) * d ** -0.5 + 8 * u * x.abs() + 1e-6
+    assert ((stats.lse - x).abs() <= 2 * lim).all()
+    # ds = dP - delta: the same sum of d products taken twice, each off by (d + 8) u of its magnitudes
+    ds = 2 * (d + 8) * u * (do.float() * v.float()).abs().sum(2, keepdim=True) * d ** -0.5 * (1 + 2.0 ** -6)
+    assert (dq.float().abs() <= ds * k.float().abs() + 1e-30).all() and (dk.float().abs() <= ds * q.float().abs() + 1e-30).all()
