@@ -602,8 +602,9 @@ __global__ __launch_bounds__(kBlock) void k_ln_bwd(const NormArgs a) {
 
 template <typename T, int VEC, int NV, int G, int R>
 void fwd_rows(const NormArgs& a, hipStream_t s) {
-  // one pass per block; element-wise parameter loads are shared by more rows
-  const unsigned grid = grid_for(a.rows, kBlock / G * R, VEC > 1 ? 1ll << 31 : 1 << 13);
+  // one pass per block, up to the 2^32 threads that a launch stays below; element-wise
+  // parameter loads are shared by more rows
+  const unsigned grid = grid_for(a.rows, kBlock / G * R, VEC > 1 ? 1 << 23 : 1 << 13);
   if (VEC > 1 && a.stream) k_ln_fwd<T, VEC, NV, G, R, (VEC > 1)><<<grid, kBlock, 0, s>>>(a);
   else k_ln_fwd<T, VEC, NV, G, R, false><<<grid, kBlock, 0, s>>>(a);
 }

@@ -98,3 +98,20 @@ def test_more_blocks_than_one_launch_takes():
     # ds = dP - delta: the same sum of d products taken twice, each off by (d + 8) u of its magnitudes
     ds = 2 * (d + 8) * u * (do.float() * v.float()).abs().sum(2, keepdim=True) * d ** -0.5 * (1 + 2.0 ** -6)
     assert (dq.float().abs() <= ds * k.float().abs() + 1e-30).all() and (dk.float().abs() <= ds * q.float().abs() + 1e-30).all()
+
+
+def test_more_rows_than_one_launch_takes():
+    """Narrow rows, 64 to a block of the layer norm: past 2^30 of them the threads would be more than HIP's 2^32."""
+    print("many rows", flush=True)
+    rows, dim, part = (1 << 30) + 300, 8, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(1)
+    block = torch.randn(part, dim, generator=g, device="cuda").bfloat16()
+    x = torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda")
+    whole = rows // part * part
+    x[:whole].view(-1, part, dim).copy_(block)
+    x[whole:] = block[:rows - whole]
+    op = R.LayerNorm()
+    want, mean, rstd = op.forward(block)
+    y, m, s = op.forward(x)
+    for got, ref in ((y, want), (m, mean), (s, rstd)):
+        assert (got[:whole].view(-1, *ref.shape) == ref).all() and torch.equal(got[whole:], ref[:rows - whole])
