@@ -495,9 +495,12 @@ typedef struct {
   int32_t reserved;  /* 0 */
   int64_t seqs, q_rows, kv_rows; /* seqs < 2^24; q_rows * heads_q, kv_rows < 2^31 - 1024 */
   int64_t q_pad, kv_pad;         /* rows per sequence of a padded layout; 0: packed */
-  int64_t max_q;     /* the caller's bound of every Lq (0: none known); the launch
-                        shape goes by it, and a longer sequence's rows past it may
-                        be left out                                               */
+  int64_t max_q;     /* the caller's bound of every Lq (0: none known).  It only
+                        shapes the launches: a longer sequence's rows past it are
+                        right too, but slow (a block a row and head over all its
+                        keys).  Packed queries without a bound are planned as if one
+                        sequence held them all, and many short ones over long keys
+                        may then not be split along the keys at all              */
   int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
   double scale;      /* > 0                                                       */
   double softcap;    /* >= 0                                                      */

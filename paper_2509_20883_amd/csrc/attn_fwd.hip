@@ -511,6 +511,72 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
   if (a.lse && half == 0) a.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
 }
 
+// Two consecutive elements, as floats and from them.
+__device__ inline float2 load2(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ inline float2 load2(const uint16_t* p) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ inline void store2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ inline void store2(uint16_t* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(a, b); }
+
+// A row of the split that no part holds, since its sequence has more queries than
+// the caller's bound: a block takes it over all its keys, a wave a key at a time,
+// a lane two columns.  Slow, but such rows are a caller's mistake.
+template <typename T, int NT>
+__device__ __forceinline__ void whole_row(const AttnArgs& a, const SeqSpan& qs, const SeqSpan& ks, int token, int head, int kvh,
+                                 int limit, float2* sh_o, float2* sh_ml) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = 2 * lane;
+  const bool in = c < a.d;
+  const T* q = static_cast<const T*>(a.q.p) + (qs.start + token) * a.q.row + head * a.q.head + c;
+  const float2 none = make_float2(0.0f, 0.0f), qv = in ? load2(q) : none;
+  const int pos = token + ks.len - qs.len;
+  const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  float2 o = none;
+  for (int j = wave; j < limit; j += NT / kWave) {
+    const T* k = static_cast<const T*>(a.k.p) + (ks.start + j) * a.k.row + kvh * a.k.head + c;
+    const T* v = static_cast<const T*>(a.v.p) + (ks.start + j) * a.v.row + kvh * a.v.head + c;
+    const float2 kv = in ? load2(k) : none, vv = in ? load2(v) : none;
+    float x = qv.x * kv.x + qv.y * kv.y;
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) x += __shfl_xor(x, d, kWave);
+    x = a.cap > 0.0f ? a.cap * kLog2e * tanhf(x * (a.scale / a.cap)) : x * (a.scale * kLog2e);
+    x -= slope * fabsf(static_cast<float>(j - pos));
+    const float top = fmaxf(m, x), base = top == -INFINITY ? 0.0f : top;
+    const float alpha = exp2_hw(m - base), p = exp2_hw(x - base);
+    m = top;
+    l = l * alpha + p;
+    o.x = o.x * alpha + p * vv.x;
+    o.y = o.y * alpha + p * vv.y;
+  }
+  sh_o[threadIdx.x] = o;
+  if (lane == 0) sh_ml[wave] = make_float2(m, l);
+  __syncthreads();
+  if (wave > 0) return;
+  m = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) m = fmaxf(m, sh_ml[w].x);
+  l = 0.0f;
+  o = none;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) {
+    const float mul = sh_ml[w].y == 0.0f ? 0.0f : exp2_hw(sh_ml[w].x - m);
+    const float2 x = sh_o[w * kWave + lane];
+    l += mul * sh_ml[w].y;
+    o.x += mul * x.x;
+    o.y += mul * x.y;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int64_t row = (qs.start + token) * a.hq + head;
+  if (in) {
+    store2(static_cast<T*>(a.out) + row * a.d + c, o.x * inv, o.y * inv);
+    if (sizeof(T) == 2 && a.rest)
+      store2(static_cast<T*>(a.rest) + row * a.d + c, rest_bf16(o.x * inv), rest_bf16(o.y * inv));
+  }
+  if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
+}
+
 // Joins the chunks of a row: a block per query token and head, threads four
 // columns and a share of the chunks each.  Bound by the latency of its two trips
 // (maxima, then parts): 9 us for 2048 rows of few chunks, 10 for 16 rows of 245.
@@ -518,7 +584,7 @@ __global__ __launch_bounds__((FewShape<T, HD>::W * kWave)) void k_attn_few(const
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void k_attn_join(const AttnArgs a) {
   __shared__ float4 sh_o[NT];
-  __shared__ float sh_l[NT];
+  __shared__ __align__(8) float sh_l[NT];
   __shared__ float sh_m[NT / kWave];
   const int head = blockIdx.y, kvh = head / a.group;
   int s;
@@ -530,14 +596,25 @@ __global__ __launch_bounds__(NT) void k_attn_join(const AttnArgs a) {
     s = find_seq(a.q_off, a.seqs, 1, 1, blockIdx.x, token);
   }
   const SeqSpan qs = seq_span(a.q_off, s, a.q_pad, a.q_rows), ks = seq_span(a.kv_off, s, a.kv_pad, a.kv_rows);
-  if (token < 0 || ks.len <= a.chunk || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // written, or no row; block-uniform
-  const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
-  const int limit = token < qs.len ? key_limit(static_cast<int>(token), qs.len, ks.len, a.causal, prefix) : 0;
-  const int chunks = static_cast<int>((static_cast<uint32_t>(limit) + a.chunk - 1) / a.chunk);
-  const int64_t first = a.kv_pad > 0 ? s * ((a.kv_pad + a.chunk - 1) / a.chunk) : tile_base(a.kv_off, s, 1, a.chunk);
+  if (token < 0 || token >= (a.q_pad > 0 ? a.q_pad : int64_t(qs.len))) return;  // no row; block-uniform, as below
   const int r = static_cast<int>(token) * a.group + head - kvh * a.group;
   const int64_t tile = r / kAttnRows, at = r % kAttnRows;
-  if (tile >= a.row_tiles || at >= a.part_rows) return;  // past the caller's bound of the queries
+  const bool past = tile >= a.row_tiles || at >= a.part_rows;  // of the caller's bound of the queries
+  if (!past && ks.len <= a.chunk) return;                      // written
+  const int prefix = a.prefix ? static_cast<int>(min(max(a.prefix[s], int64_t(0)), int64_t(ks.len))) : 0;
+  const int limit = token < qs.len ? key_limit(static_cast<int>(token), qs.len, ks.len, a.causal, prefix) : 0;
+  if (__builtin_expect(past, 0)) {
+    // the arguments again, by an address that is not known before: the compiler else
+    // loads q, k and v ahead of the branch, and every row waits for a further line of
+    // the arguments (9.0 -> 10.0 us)
+    uint64_t args = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+    asm volatile("" : "+s"(args));
+    whole_row<T, NT>(*reinterpret_cast<const AttnArgs*>(args), qs, ks, static_cast<int>(token), head, kvh, limit, reinterpret_cast<float2*>(sh_o),
+                     reinterpret_cast<float2*>(sh_l));
+    return;
+  }
+  const int chunks = static_cast<int>((static_cast<uint32_t>(limit) + a.chunk - 1) / a.chunk);
+  const int64_t first = a.kv_pad > 0 ? s * ((a.kv_pad + a.chunk - 1) / a.chunk) : tile_base(a.kv_off, s, 1, a.chunk);
   const int64_t slot0 = ((first * a.hkv + kvh) * a.row_tiles + tile) * a.part_rows + at;
   const int64_t step = static_cast<int64_t>(a.hkv) * a.row_tiles * a.part_rows;
 

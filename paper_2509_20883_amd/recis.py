@@ -472,8 +472,11 @@ class SeqAttention:
     prefix[s] (int64 [seqs]); softcap: scores capped by softcap * tanh(x /
     softcap); slopes (float32 [heads_q]): the score falls by slope * |i + Lk -
     Lq - j|, and the backward returns their gradient.  max_q: a bound of the
-    query lengths where the caller knows one (0: none): it only shapes the
-    launches, so that few queries over long keys are split along the keys.
+    query lengths where the caller knows one (0: none).  It only shapes the
+    launches; rows past a bound that does not hold are right, but slow.  Give
+    it for single tokens and short chunks: packed queries without it are
+    planned as if one sequence held them all, which takes up to 256 MiB of
+    workspace, and past that the keys are not split.
     Calls of one object share its workspace: issue them on one stream, or
     order the streams.
     """

@@ -115,3 +115,27 @@ def test_more_rows_than_one_launch_takes():
     y, m, s = op.forward(x)
     for got, ref in ((y, want), (m, mean), (s, rstd)):
         assert (got[:whole].view(-1, *ref.shape) == ref).all() and torch.equal(got[whole:], ref[:rows - whole])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv,d", [(2, 1, 64), (8, 2, 128), (3, 3, 40)])
+@pytest.mark.parametrize("bound", [1, 4, 50])
+def test_a_bound_of_the_queries_that_does_not_hold(dtype, hq, hkv, d, bound):
+    """max_q shapes the launches, the results hold without it: rows past a bound that is too small, over keys that are
+    split and keys that are not, masked and not, and padding of the row tiles between them."""
+    print("bound", dtype, hq, hkv, d, bound, flush=True)
+    ql, kl = [1, 9, 200, 0, 3, 60], [3000, 5000, 900, 40, 100, 20]
+    qo, ko = _offsets(ql), _offsets(kl)
+    g = torch.Generator(device="cuda").manual_seed(d + bound)
+    q = torch.randn(sum(ql), hq, d, generator=g, device="cuda").to(dtype)
+    k, v = (torch.randn(sum(kl), hkv, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+    m = torch.rand(hq, generator=g, device="cuda") * 0.1
+    pre = torch.tensor([5, 0, 950, 1, 50, 3], device="cuda")
+    for causal, cap, slopes, prefix in ((True, 0.0, None, None), (False, 4.0, m, None), (True, 0.0, m, pre)):
+        op = R.SeqAttention(causal=causal, softcap=cap)
+        out = torch.full_like(q, float("nan"))
+        _, stats = op.forward(q, k, v, qo, kv_offsets=ko, slopes=slopes, prefix=prefix, max_q=bound, out=out)
+        want, _ = _reference(q, k, v, q, qo, ko, causal, cap, prefix, slopes, d ** -0.5, dtype == torch.bfloat16)
+        for b, (lo, hi) in enumerate(zip(qo.tolist(), qo.tolist()[1:])):
+            _close(out[lo:hi], *want[b]["out"], f"out of sequence {b}")
+            _close(stats.lse[lo:hi], *want[b]["lse"], f"lse of sequence {b}")
