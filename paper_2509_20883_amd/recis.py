@@ -344,13 +344,21 @@ def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     return t, t.shape[-1]
 
 
-def _bytes(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
-    """The workspace, replaced if it is too small or on another device.  One
-    that other streams may still read goes back to the caching allocator,
-    which holds a block for the stream it was allocated on."""
-    if ws is None or ws.numel() < need or ws.device != like.device:
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
-    return ws
+class _Workspace:
+    """A buffer that grows with the calls of an object.  One that a larger call
+    replaces goes back to the caching allocator, for use once the current stream
+    is past the calls so far."""
+
+    def __init__(self):
+        self.ws: Optional[torch.Tensor] = None
+
+    def _take(self, need: int, like: torch.Tensor) -> torch.Tensor:
+        ws = self.ws
+        if ws is None or ws.numel() < need or ws.device != like.device:
+            if ws is not None:
+                ws.record_stream(torch.cuda.current_stream(ws.device))
+            self.ws = ws = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+        return ws
 
 
 def _like(t: torch.Tensor) -> torch.Tensor:
@@ -364,7 +372,7 @@ def _packed(t: torch.Tensor) -> torch.Tensor:
     return t.clone() if t.data_ptr() % 16 else t
 
 
-class LayerNorm:
+class LayerNorm(_Workspace):
     """Layer norm over the last axis, with a reusable backward workspace.
 
     ``forward(x, weight, bias, mask)`` returns (y, mean, rstd); ``backward``
@@ -376,8 +384,8 @@ class LayerNorm:
     """
 
     def __init__(self, eps: float = 1e-5):
+        super().__init__()
         self.eps = float(eps)
-        self.ws: Optional[torch.Tensor] = None
 
     @staticmethod
     def _params(x, weight, bias):
@@ -442,10 +450,10 @@ class LayerNorm:
         dx = _like(x)
         dw = x.new_empty((dim,), dtype=torch.bfloat16 if pt == BF16 else torch.float32)
         db = torch.empty_like(dw)
-        self.ws = _bytes(self.ws, lib().layer_norm_bwd_workspace_bytes(rows, dim), x)
+        ws = self._take(lib().layer_norm_bwd_workspace_bytes(rows, dim), x)
         _check(lib().layer_norm_bwd(gr.data_ptr(), gs, xr.data_ptr(), rows, dim, xs, dt, _ptr(weight), pt, _ptr(m),
                                     mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dim, dw.data_ptr(),
-                                    db.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream()))
+                                    db.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
         return dx, dw, db
 
 
@@ -457,7 +465,7 @@ class AttnStats(NamedTuple):
     rest: Optional[torch.Tensor]
 
 
-class SeqAttention:
+class SeqAttention(_Workspace):
     """Attention over ragged sequences, with a reusable workspace.
 
     q [rows, heads_q, d] packed with q_offsets (int64 [seqs + 1]), or the
@@ -482,8 +490,8 @@ class SeqAttention:
     """
 
     def __init__(self, scale: Optional[float] = None, softcap: float = 0.0, causal: bool = True):
+        super().__init__()
         self.scale, self.softcap, self.causal = scale, float(softcap), bool(causal)
-        self.ws: Optional[torch.Tensor] = None
 
     @staticmethod
     def _layout(t: torch.Tensor, what: str):
@@ -544,12 +552,11 @@ class SeqAttention:
         stats = AttnStats(q.new_empty(shape[:-1], dtype=torch.float32),
                           torch.empty_like(out) if desc.dtype == BF16 else None)
         need = lib().seq_attention_workspace_bytes(C.byref(desc), 0)
-        if need:
-            self.ws = _bytes(self.ws, need, q)
+        ws = self._take(need, q) if need else None
         _check(lib().seq_attention_fwd(C.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), qo.data_ptr(),
                                        ko.data_ptr(), _ptr(prefix), _ptr(slopes), out.data_ptr(), _ptr(stats.rest),
-                                       stats.lse.data_ptr(), _ptr(self.ws) if need else None,
-                                       self.ws.numel() if need else 0, int(validate), _stream()))
+                                       stats.lse.data_ptr(), _ptr(ws), ws.numel() if need else 0, int(validate),
+                                       _stream()))
         return out, stats
 
     def backward(self, grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -567,12 +574,11 @@ class SeqAttention:
         grad_out, out, lse = _packed(grad_out), _packed(out), lse.contiguous()
         rest = None if rest is None else _packed(rest)
         dslopes = None if slopes is None else torch.empty_like(slopes)
-        need = lib().seq_attention_workspace_bytes(C.byref(desc), 1)
-        self.ws = _bytes(self.ws, need, q)
+        ws = self._take(lib().seq_attention_workspace_bytes(C.byref(desc), 1), q)
         _check(lib().seq_attention_bwd(C.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                        _ptr(rest), lse.data_ptr(), grad_out.data_ptr(), qo.data_ptr(), ko.data_ptr(),
                                        _ptr(prefix), _ptr(slopes), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                       _ptr(dslopes), self.ws.data_ptr(), self.ws.numel(), int(validate), _stream()))
+                                       _ptr(dslopes), ws.data_ptr(), ws.numel(), int(validate), _stream()))
         return dq, dk, dv, dslopes
 
 

@@ -139,3 +139,42 @@ def test_a_bound_of_the_queries_that_does_not_hold(dtype, hq, hkv, d, bound):
         for b, (lo, hi) in enumerate(zip(qo.tolist(), qo.tolist()[1:])):
             _close(out[lo:hi], *want[b]["out"], f"out of sequence {b}")
             _close(stats.lse[lo:hi], *want[b]["lse"], f"lse of sequence {b}")
+
+
+def _inputs(n):
+    g = torch.Generator(device="cuda").manual_seed(n)
+    q, do = (torch.randn(n, 2, 64, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(n, 2, 64, generator=g, device="cuda").bfloat16() for _ in range(2))
+    return q, k, v, do, _offsets([n])
+
+
+def _gradients(op, q, k, v, do, off):
+    out, stats = op.forward(q, k, v, off)
+    return op.backward(do, q, k, v, out, stats, off)[:3]
+
+
+def test_a_workspace_that_another_stream_works_on_is_not_handed_out():
+    """A call that needs a larger workspace replaces it: the old one, which came from this stream, is not used again while
+    the other stream, ordered after this one, still works on it."""
+    print("workspace, streams", flush=True)
+    small, large = _inputs(300), _inputs(30000)
+    want = _gradients(R.SeqAttention(), *small)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        _gradients(R.SeqAttention(), *large)  # memory of that stream's own for the calls below
+    torch.cuda.synchronize()
+    op = R.SeqAttention()
+    _gradients(op, *small)
+    first, size = op.ws.data_ptr(), op.ws.numel()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200000000)
+        got = _gradients(op, *small)
+        _gradients(op, *large)
+        done = torch.cuda.Event()
+        done.record()
+    others = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(500)]
+    assert not done.query()  # the other stream is still at work
+    assert not any(t.data_ptr() < first + size and first < t.data_ptr() + size for t in others)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
