@@ -345,12 +345,14 @@ def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
 
 
 class _Workspace:
-    """A buffer that grows with the calls of an object.  One that a larger call
-    replaces goes back to the caching allocator, for use once the current stream
-    is past the calls so far."""
+    """A buffer that grows with the calls of an object.  What a captured graph
+    works on stays with the object when a larger call replaces it; any other
+    goes back to the caching allocator, for use once the current stream is past
+    the calls so far."""
 
     def __init__(self):
         self.ws: Optional[torch.Tensor] = None
+        self._captured: list = []
 
     def _take(self, need: int, like: torch.Tensor) -> torch.Tensor:
         ws = self.ws
@@ -358,6 +360,8 @@ class _Workspace:
             if ws is not None:
                 ws.record_stream(torch.cuda.current_stream(ws.device))
             self.ws = ws = torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+        if torch.cuda.is_current_stream_capturing() and not any(t is ws for t in self._captured):
+            self._captured.append(ws)
         return ws
 
 
@@ -380,7 +384,8 @@ class LayerNorm(_Workspace):
     dweight, dbias).  x: float32 or bfloat16 [..., dim]; weight, bias [dim] in
     either type or None (1 and 0); mask: uint8 or bool [...], rows of mask 0
     are never read and give y = dx = 0.  Calls of one object share its
-    workspace: issue them on one stream, or order the streams.
+    workspace: issue them on one stream, or order the streams, and keep the
+    object as long as a graph that captured its calls.
     """
 
     def __init__(self, eps: float = 1e-5):
@@ -486,7 +491,8 @@ class SeqAttention(_Workspace):
     planned as if one sequence held them all, which takes up to 256 MiB of
     workspace, and past that the keys are not split.
     Calls of one object share its workspace: issue them on one stream, or
-    order the streams.
+    order the streams, and keep the object as long as a graph that captured its
+    calls.
     """
 
     def __init__(self, scale: Optional[float] = None, softcap: float = 0.0, causal: bool = True):

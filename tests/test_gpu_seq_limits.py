@@ -178,3 +178,31 @@ def test_a_workspace_that_another_stream_works_on_is_not_handed_out():
     assert not any(t.data_ptr() < first + size and first < t.data_ptr() + size for t in others)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_workspace_that_a_graph_was_captured_with_is_kept():
+    """A larger call after the capture takes another workspace, and the graph's own holds nobody else's values."""
+    print("workspace, graph", flush=True)
+    small, large = _inputs(300), _inputs(30000)
+    want = _gradients(R.SeqAttention(), *small)
+    side = torch.cuda.Stream()
+    op = R.SeqAttention()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _gradients(op, *small)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _gradients(op, *small)
+    size = op.ws.numel()
+    _gradients(op, *large)
+    assert op.ws.numel() > size
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):  # the stream that the first workspace came from
+        others = [torch.full((size,), 77, dtype=torch.uint8, device="cuda") for _ in range(500)]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((t == 77).all() for t in others)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
