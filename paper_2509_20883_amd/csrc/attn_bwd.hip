@@ -71,8 +71,9 @@ template <typename T, int HD, bool FEW>
 struct KeyShape {
   static constexpr int kRow = HD * sizeof(T);
   static constexpr bool kNarrow = kRow <= 128, kWide = kRow > 256;
-  static constexpr int KW = FEW && !kWide ? 2 : 4;
-  static constexpr int RW = !FEW || kWide ? 1 : kNarrow ? 2 : 4;
+  static_assert(!FEW || !kWide, "fp32 rows of 128 have one shape");
+  static constexpr int KW = FEW ? 2 : 4;
+  static constexpr int RW = !FEW ? 1 : kNarrow ? 2 : 4;
   static constexpr int W = KW * RW;       // waves
   // rows per step: 32 for every row wave, and at least a load of 16 bytes for every thread
   static constexpr int STEP = 32 * RW * kRow < W * kWave * 16 ? W * kWave * 16 / kRow : 32 * RW;
@@ -628,8 +629,12 @@ template <typename T, int HD>
 hipError_t run(const AttnArgs& a, hipStream_t s) {
   const int64_t qt = attn_row_tiles(a);
   launch_blocks<kAttnWaves * kWave>(k_attn_dq<T, HD>, a, qt * a.hkv, s);
-  if (key_tiles(a, KeyShape<T, HD, false>::KEYS) * a.hkv < kFewKeyBlocks && HD * sizeof(T) <= 256) run_keys<T, HD, true>(a, s);
-  else run_keys<T, HD, false>(a, s);
+  bool few = false;
+  if constexpr (HD * sizeof(T) <= 256) {
+    few = key_tiles(a, KeyShape<T, HD, false>::KEYS) * a.hkv < kFewKeyBlocks;
+    if (few) run_keys<T, HD, true>(a, s);
+  }
+  if (!few) run_keys<T, HD, false>(a, s);
   if (a.dslopes) k_attn_dslopes<<<a.hq, kSlopeThreads, 0, s>>>(a, qt);
   return hipGetLastError();
 }
