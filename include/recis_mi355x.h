@@ -502,8 +502,9 @@ typedef struct {
                         sequence held them all, and many short ones over long keys
                         may then not be split along the keys at all              */
   int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
-  double scale;      /* > 0                                                       */
-  double softcap;    /* >= 0                                                      */
+  double scale;      /* > 0, below 2^127                                          */
+  double softcap;    /* >= 0; a cap, and scale / softcap, within fp32's range (a
+                        cap of 2^100 or more changes no score)                    */
 } rs_attn_desc;
 
 /* Workspace bytes of seq_attention_fwd (backward = 0) or seq_attention_bwd

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -70,8 +71,12 @@ const char* check_attn(const rs_attn_desc* d) {
   if ((64 * d->q_stride + d->heads_q / d->heads_kv * d->q_head_stride) * es >= kMost)
     return "64 rows and a group of heads of q must span less than 2^31 bytes";
   if (attn_blocks(*d) >= kMost) return "too many sequences, rows and key heads: below 2^31 blocks";
-  if (!(d->scale > 0.0) || !std::isfinite(d->scale)) return "scale must be finite and > 0";
+  // the kernels hold both, and their quotient, in fp32
+  const float scale = static_cast<float>(d->scale), cap = static_cast<float>(d->softcap);
+  if (!(d->scale > 0.0) || !(d->scale < 0x1p127)) return "scale must be > 0 and below 2^127";
   if (!(d->softcap >= 0.0) || !std::isfinite(d->softcap)) return "softcap must be finite and >= 0";
+  if (d->softcap > 0.0 && (cap < FLT_MIN || !std::isfinite(scale / cap)))
+    return "softcap and scale / softcap must be within fp32's range";
   return nullptr;
 }
 
@@ -92,7 +97,9 @@ AttnArgs attn_args(const rs_attn_desc& d) {
   a.bf16 = d.dtype == RS_BF16;
   a.causal = d.causal != 0;
   a.scale = static_cast<float>(d.scale);
-  a.cap = static_cast<float>(d.softcap);
+  // A score below 2^-13 of the cap is cap(x) to within fp32's rounding: past 2^100
+  // every score is, and the cap's own products would leave fp32's range.
+  a.cap = d.softcap < 0x1p100 ? static_cast<float>(d.softcap) : 0.0f;
   return a;
 }
 

@@ -206,3 +206,19 @@ def test_a_workspace_that_a_graph_was_captured_with_is_kept():
         torch.cuda.synchronize()
         assert all((t == 77).all() for t in others)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cap", [1e31, 1e38, 1e39, 1e300])
+def test_a_cap_past_every_score(dtype, cap):
+    """The cap's products with the scores would leave fp32: the same results as without a cap."""
+    print("cap", dtype, cap, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    off = _offsets([40, 3, 100])
+    q, do = (torch.randn(143, 2, 64, generator=g, device="cuda").to(dtype) for _ in range(2))
+    k, v = (torch.randn(143, 2, 64, generator=g, device="cuda").to(dtype) for _ in range(2))
+    got = []
+    for op in (R.SeqAttention(softcap=cap), R.SeqAttention()):
+        out, stats = op.forward(q, k, v, off)
+        got.append((out, stats.lse) + op.backward(do, q, k, v, out, stats, off)[:3])
+    assert all(torch.equal(a, b) for a, b in zip(*got))

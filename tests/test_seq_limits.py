@@ -1,5 +1,8 @@
 """The sequence operators' limits without a GPU: what their descriptor refuses, and the kernels that are compiled (CPU only)."""
+import ctypes as C
 import subprocess
+
+import pytest
 
 from paper_2509_20883_amd import recis as R
 from paper_2509_20883_amd.build import LIB
@@ -12,3 +15,16 @@ def test_every_compiled_shape_of_the_key_pass_is_launched():
     shapes = {n.split("k_attn_dkdv<")[1].split(">")[0] for n in names.splitlines() if "k_attn_dkdv<" in n}
     want = {f"{t}, {d}, {few}" for t in ("float", "unsigned short") for d in (32, 64, 128) for few in ("true", "false")}
     assert shapes == want - {"float, 128, true"}
+
+
+@pytest.mark.parametrize("scale,softcap,ok", [
+    (0.125, 0.0, True), (0.125, 1e-30, True), (1e-30, 1e-37, True), (0.125, 1e300, True), (1e38, 0.0, True), (1e-300, 5.0, True),
+    (3e38, 0.0, False), (1e39, 0.0, False), (1e300, 5.0, False),  # not finite in fp32, in base 2
+    (0.125, 1e-46, False), (0.125, 1e-39, False),  # no cap, or half of one, in fp32
+    (1e5, 1e-37, False),  # their quotient is not
+])
+def test_scale_and_cap_hold_in_fp32(scale, softcap, ok):
+    d = R.AttnDesc(dtype=R.BF16, heads_q=8, heads_kv=2, head_dim=64, causal=1, reserved=0, seqs=3, q_rows=100, kv_rows=100,
+                   q_pad=0, kv_pad=0, max_q=0, q_stride=512, q_head_stride=64, k_stride=128, k_head_stride=64, v_stride=128,
+                   v_head_stride=64, scale=scale, softcap=softcap)
+    assert (R.lib().seq_attention_workspace_bytes(C.byref(d), 1) > 0) == ok
