@@ -222,3 +222,92 @@ def test_a_cap_past_every_score(dtype, cap):
         out, stats = op.forward(q, k, v, off)
         got.append((out, stats.lse) + op.backward(do, q, k, v, out, stats, off)[:3])
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lengths_above_the_pad_length_are_cut(dtype):
+    """A padded sequence longer than its block is its first pad rows, on either side; its positions go by the cut lengths."""
+    print("cut", dtype, flush=True)
+    hq, hkv, d, ql, kl = 4, 2, 64, [90, 64, 3, 200], [41, 500, 7, 40]
+    for q_pad, kv_pad in ((64, 40), (64, 300), (130, 40)):
+        for causal in (True, False):
+            g = torch.Generator(device="cuda").manual_seed(q_pad)
+            q, do = (torch.randn(4, q_pad, hq, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+            k, v = (torch.randn(4, kv_pad, hkv, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+            op = R.SeqAttention(causal=causal)
+            kw = dict(kv_offsets=_offsets(kl))
+            out, stats = op.forward(q, k, v, _offsets(ql), **kw)
+            got = dict(zip(("out", "lse", "dq", "dk", "dv"),
+                           (out, stats.lse) + op.backward(do, q, k, v, out, stats, _offsets(ql), **kw)[:3]))
+            want, _ = _reference(q, k, v, do, _offsets(ql), _offsets(kl), causal, 0.0, None, None, d ** -0.5,
+                                 dtype == torch.bfloat16)
+            for name, t in got.items():
+                for b in range(4):
+                    n = want[b][name][0].shape[0]
+                    assert n == (min(kl[b], kv_pad) if name in ("dk", "dv") else min(ql[b], q_pad))
+                    _close(t[b, :n], *want[b][name], f"{name} of sequence {b}")
+                    assert (t[b, n:] == (-float("inf") if name == "lse" else 0)).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,ql,kl,max_q", [
+    (4, 2, 64, [300, 5, 64], [300, 5, 64], 0),  # one pass over the keys
+    (8, 2, 128, [1, 1, 1], [9000, 3, 700], 1),  # split and joined
+    (4, 2, 64, [4, 1, 2], [20000, 3, 700], 4),  # few narrow rows, joined by waves and chunks
+])
+def test_rest_is_what_rounding_took(hq, hkv, d, ql, kl, max_q):
+    """out + rest is the output before its rounding, and the backward takes delta from both.  Scores are next to 0, so P is
+    1 / Lk with nothing lost as an operand, and v lies around 4: out's rounding is then the largest error of the forward,
+    and of dq and dk, whose terms are differences of dP that the 4 does not change."""
+    print("rest", hq, d, ql, flush=True)
+    qo, ko = _offsets(ql), _offsets(kl)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    q, do = (torch.randn(sum(ql), hq, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(sum(kl), hkv, d, generator=g, device="cuda") for _ in range(2))
+    k, v = (2 + k).bfloat16(), (4 + 0.1 * v).bfloat16()
+    scale = 1e-8
+    op = R.SeqAttention(causal=False, scale=scale)
+    kw = dict(kv_offsets=ko, max_q=max_q)
+    out, stats = op.forward(q, k, v, qo, **kw)
+    want, _ = _reference(q, k, v, do, qo, ko, False, 0.0, None, None, scale, True)
+    full = torch.cat([want[b]["out"][0] for b in range(len(ql))])
+    # rest's own rounding, the sums over the keys and the scores' 1e-7 in P
+    lim = (2.0 ** -16 + (max(kl) + 64) * 2.0 ** -24 + 1e-6) * 5
+    assert float((out.double() + stats.rest.double() - full).abs().max()) <= lim
+    assert float((out.double() - full).abs().max()) > 2 * lim  # without rest it is not
+    with_rest = op.backward(do, q, k, v, out, stats, qo, **kw)
+    without = op.backward(do, q, k, v, out, R.AttnStats(stats.lse, None), qo, **kw)
+    for at, name in ((0, "dq"), (1, "dk")):
+        ref = torch.cat([want[b][name][0] for b in range(len(ql))])
+        a, b = (float((t[at].double() - ref).norm() / ref.norm()) for t in (with_rest, without))
+        assert a < 0.5 * b, (name, a, b)
+
+
+def test_backward_past_2_31_bytes():
+    """A sequence whose q, k and v lie more than 2^32 bytes into their tensors: the gradients of the same sequence alone,
+    and zero for the keys of a sequence without queries before it."""
+    print("far backward", flush=True)
+    lead, n, h, d = 20000000, 300, 1, 128
+    g = torch.Generator(device="cuda").manual_seed(4)
+    t = [torch.randn(n, h, d, generator=g, device="cuda").bfloat16() for _ in range(4)]
+    far = [torch.empty(lead + n, h, d, dtype=torch.bfloat16, device="cuda") for _ in t]
+    for a, b in zip(far, t):
+        a[:lead], a[lead:] = 0.5, b
+    off, alone = _offsets([lead, n]), _offsets([n])
+    op = R.SeqAttention()
+    m = torch.full((h,), 0.05, device="cuda")
+    # the first sequence's queries see no key: it has none
+    empty = torch.tensor([0, 0, n], device="cuda")
+    out, stats = op.forward(far[0], t[1], t[2], off, kv_offsets=empty, slopes=m)
+    ref, rstats = op.forward(t[0], t[1], t[2], alone, slopes=m)
+    assert torch.equal(out[lead:], ref) and not out[:lead].any()
+    got = op.backward(far[3], far[0], t[1], t[2], out, stats, off, kv_offsets=empty, slopes=m)
+    want = op.backward(t[3], t[0], t[1], t[2], ref, rstats, alone, slopes=m)
+    assert torch.equal(got[0][lead:], want[0]) and not got[0][:lead].any()
+    # and the keys far into theirs, the first sequence without a query
+    out, stats = op.forward(t[0], far[1], far[2], empty, kv_offsets=off, slopes=m)
+    far_k = op.backward(t[3], t[0], far[1], far[2], out, stats, empty, kv_offsets=off, slopes=m)
+    for name, a, b in (("dk", far_k[1], want[1]), ("dv", far_k[2], want[2])):
+        # larger key tiles, since there are many: the fp32 sums in another order, rounded once
+        assert (a[lead:].double() - b.double()).norm() <= 2.0 ** -8 * b.double().norm() and not a[:lead].any(), name
+    for name, a, b in (("dk", got[1], want[1]), ("dv", got[2], want[2])):
+        assert torch.equal(a, b), name
