@@ -12,11 +12,16 @@
 // scores and dP are computed in both, seven products instead of five; a single
 // pass would need atomics into one of the gradients.
 //
-// What bounds them: vector instructions and the waits between them, with two or
-// three blocks a CU (the gradients' registers allow no more).  1536 padded
-// sequences of 100 to 1024, 2 heads of 64, distances weighed and their slopes'
-// gradient taken: dq 820 us, dk and dv 905; 24 documents of 17 to 1500, 16 heads of
-// 128 over 4, capped: 290 and 527.  The matrix unit is 13 to 25% busy.
+// What bounds them: waits, half of the waves' cycles and more in bf16, with two or
+// three blocks a CU (the gradients' registers allow no more; one of the small
+// shape for rows of 256 bytes, whose tiles take 152 KB).  A step's loads are
+// requested a step ahead, but the compiler waits for every load that writes LDS:
+// in dk and dv before the step's first read, so that each step pays a trip to
+// memory, in dq (bf16) before its first transposed read.  1536 padded sequences
+// of 100 to 1024, 2 heads of 64, distances weighed and their slopes' gradient
+// taken: dq 727 us, dk and dv 849; 24 documents of 17 to 1500, 16 heads of 128
+// over 4, capped: 259 and 469.  The matrix unit is 15 to 20% busy, the vector unit
+// 25 to 49%; in fp32 (128 lists of 0 to 400, 4 heads of 32) 32 to 45% and 15%.
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"

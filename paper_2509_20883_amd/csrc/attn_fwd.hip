@@ -8,8 +8,9 @@
 // in base 2.  A block takes 128 packed rows (tokens times the query heads of
 // one key head) and walks over the keys 64 at a time; a wave owns 32 rows, one
 // per lane column: its maximum, sum and rescaling are the lane's own scalars.
-// The next step's keys and values are on their way to LDS while a step is
-// computed.  Where the rows alone make too few blocks (single tokens, short
+// The next step's keys and values are requested before a step is computed; fp32
+// runs beside them to the step's end, bf16 to its first transposed read of the
+// values, before which the compiler waits for every load that writes LDS.  Where the rows alone make too few blocks (single tokens, short
 // chunks), a block takes a chunk of the keys and a second kernel joins them.
 //
 // What bounds it.  Per score the products take 4 HD operations, which the matrix
@@ -17,10 +18,10 @@
 // instructions (scale, maximum, exponent, sum, rounding; 3 more for a distance
 // term, 8 for a cap, and two transcendental ones where a score passes its half): at HD = 128 the two are
 // even, below it the vector unit bounds.  One causal sequence of 16384, 8 heads
-// of 128 bf16: 587 us, 936 TFLOP/s of the scores it needs (a large library
-// product reaches 1329); matrix unit 37% busy, vector unit 44%.  1536 padded
-// sequences of 100 to 1024, 2 heads of 64, distances weighed: 467 us, vector unit
-// 61% busy.  One token for each of 256 users, 8 heads of 128 over 2: 117 us, 4.5 TB/s with the join.
+// of 128 bf16: 561 to 594 us, 925 to 980 TFLOP/s of the scores it needs (a large
+// library product reaches 1329); matrix unit 45% busy, vector unit 41%.  1536 padded
+// sequences of 100 to 1024, 2 heads of 64, distances weighed: 426 us, vector unit
+// 63% busy.  One token for each of 256 users, 8 heads of 128 over 2: 114 us, 4.5 TB/s with the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(kAttnWaves* kWave, (kResidentBlocks<T, HD>)) void k
 // their way as soon as the scores are taken, the next values as soon as the
 // output is, and no barrier ties the waves together.  The waves' results are
 // joined as those of chunks are.  Four candidates over 1,000,003 keys, two key
-// heads of 64 bf16: 92 us, 5.5 TB/s (reads alone reach 6.8).
+// heads of 64 bf16: 90 us, 5.7 TB/s (reads alone reach 6.8).
 template <typename T, int HD>
 struct FewShape {
   static constexpr int W = 8;
