@@ -28,3 +28,17 @@ def test_scale_and_cap_hold_in_fp32(scale, softcap, ok):
                    q_pad=0, kv_pad=0, max_q=0, q_stride=512, q_head_stride=64, k_stride=128, k_head_stride=64, v_stride=128,
                    v_head_stride=64, scale=scale, softcap=softcap)
     assert (R.lib().seq_attention_workspace_bytes(C.byref(d), 1) > 0) == ok
+
+
+@pytest.mark.parametrize("dtype,field,value,ok", [
+    (R.F32, "k_stride", (1 << 23) - 4, True), (R.F32, "k_stride", 1 << 23, False), (R.BF16, "v_stride", (1 << 23) - 8, True),
+    (R.F32, "k_head_stride", (1 << 23) - 4, True), (R.BF16, "q_stride", (1 << 23) - 8, True),
+    (R.F32, "q_stride", 5000000, True), (R.F32, "q_stride", (1 << 23) - 4, False),  # 64 rows of q and its heads
+    (R.F32, "q_head_stride", (1 << 23) - 4, True), (R.BF16, "q_stride", 12, False), (R.F32, "q_stride", 0, True),
+])
+def test_strides(dtype, field, value, ok):
+    """Rows and heads as far apart as the kernels address them, and no further."""
+    d = dict(dtype=dtype, heads_q=2, heads_kv=1, head_dim=64, causal=1, reserved=0, seqs=3, q_rows=200, kv_rows=200, q_pad=0,
+             kv_pad=0, max_q=0, q_stride=128, q_head_stride=64, k_stride=64, k_head_stride=64, v_stride=64, v_head_stride=64,
+             scale=0.125, softcap=0.0)
+    assert (R.lib().seq_attention_workspace_bytes(C.byref(R.AttnDesc(**dict(d, **{field: value}))), 1) > 0) == ok
