@@ -231,6 +231,7 @@ def prepare(case, seed):
         s["q"], s["k"], s["v"] = y.split([hq, hkv, hkv], 1)
         s["start"] = kl // P * P
         s["back"] = _offsets(torch.where(ql > 0, held - s["start"], 0))
+        s["back_rows"] = int(s["back"][-1])
     else:
         # histories drift: the keys of a page share a direction, and a query looks for some page's
         step = max(1, int(1e8 / (hkv * P * W)))
@@ -285,7 +286,7 @@ def _run_own(s):
     case, c = s["case"], s["cache"]
     if case["kind"] == "append":
         lens, q = c.append(s["k"], s["v"], s["off"], s["lens"], s["table"], q=s["q"], slots=s["slots"])
-        k, v = c.read(s["back"], lens, s["table"], start=s["start"], slots=s["slots"])
+        k, v = c.read(s["back"], lens, s["table"], s["back_rows"], start=s["start"], slots=s["slots"])
         got = dict(q=q, k=k, v=v, lens=lens)
         if case["bounds"]:
             got["bounds"] = (c.bounds * c.units[..., None, None]).to(torch.bfloat16)
@@ -319,7 +320,7 @@ def _plain_append(s):
     case = s["case"]
     n, hkv, d, P, codes, dt = case["seqs"], case["hkv"], case["d"], case["page"], case["codes"], s["q"].dtype
     off, lens, back = s["off"], s["lens"], s["back"]
-    rows, total = s["q"].shape[0], int(back[-1])
+    rows, total = s["q"].shape[0], s["back_rows"]
     seq = torch.searchsorted(off, torch.arange(rows, device=DEV), right=True) - 1
     pos = lens[seq] + torch.arange(rows, device=DEV) - off[seq]
     q, k = _turn(s["q"], pos, case), _turn(s["k"], pos, case)
