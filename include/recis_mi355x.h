@@ -15,7 +15,8 @@
  * ids partition (dedup + split by owner shard), the bucketize / mod
  * feature transforms fused over columns, and the sequence operators that
  * follow the step in a model: layer norm and attention over ragged sequences,
- * each with its backward.
+ * each with its backward, and for serving a paged cache of the sequences' keys
+ * and values in 8 bits.
  *
  * Conventions shared by every entry point
  *  - All array arguments are DEVICE pointers owned by the caller, unless a
@@ -534,6 +535,152 @@ rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k,
                             const int64_t* kv_offsets, const int64_t* prefix, const float* slopes, void* dq,
                             void* dk, void* dv, float* dslopes, void* workspace, size_t workspace_bytes,
                             int32_t validate, rs_stream stream);
+
+/* A paged cache of the keys and values of sequences, for serving: histories
+ * that grow by a few tokens a call and are read whole, or page by page, by the
+ * queries of the newest.
+ *
+ * A page is page_len consecutive tokens of a sequence, every key head, keys and
+ * values.  A full page is held in 8 bits with one scale for its keys and one for
+ * its values of each head; the page still being filled, the open page, in the
+ * model's type.  A page is coded once, from the tokens in the model's type, when
+ * its last token comes: the cache does not depend on how the tokens were cut
+ * into calls.
+ *   RS_CACHE_I8:   scale = max |x| / 127 (fp32), code = round(x / scale), ties
+ *                  to even
+ *   RS_CACHE_E4M3: scale = the least power of two with max |x| <= 448 scale,
+ *                  code = x / scale in OCP e4m3, ties to even
+ * Scales are at least 2^-126.  A page that holds an infinity or NaN reads as NaN
+ * throughout (and may reach every query of its sequence).
+ *
+ * Memory (device, the caller's; W = 32, 64 or 128, the least that head_dim fits;
+ * nothing has to be cleared):
+ *   data   [pages][heads_kv][2][page_len * W] bytes: keys as [W / 16][page_len]
+ *          [16 columns], then values as [page_len / 16][W][16 tokens]; columns
+ *          past head_dim are 0
+ *   scales fp32 [pages][heads_kv][2]
+ *   open   `dtype` [slots][2][heads_kv][2][page_len][head_dim]: a sequence's
+ *          slot holds two open pages, page n at n % 2.  After a call only the
+ *          open page's own tokens mean anything.  A call can be repeated on the
+ *          same lens unless it began and ended inside pages an even number (not
+ *          zero) apart
+ *   bounds int8 [pages][heads_kv][2][W]: each column's maximum and minimum over
+ *          the page's keys in units of `units` fp32 [pages][heads_kv], the least
+ *          power of two with max |k| <= 127 units, rounded outward.  Both NULL
+ *          where pages are never selected
+ * Pages and slots are the caller's to hand out.  Pages may be shared by
+ * sequences that only read them. */
+typedef enum { RS_CACHE_I8 = 0, RS_CACHE_E4M3 = 1 } rs_cache_codes;
+typedef struct {
+  int32_t codes;     /* rs_cache_codes                                          */
+  int32_t dtype;     /* rs_dtype of the model: q, k, v, out and the open pages  */
+  int32_t heads_kv;  /* 1 .. 1024                                               */
+  int32_t head_dim;  /* a multiple of 8 in [8, 128]                             */
+  int32_t page_len;  /* 32, 64, 128 or 256                                      */
+  int32_t reserved;  /* 0                                                       */
+  int64_t pages, slots; /* below 2^31 - 1024                                    */
+  void* data;
+  float* scales;
+  void* open;
+  int8_t* bounds;
+  float* units;
+} rs_seq_cache;
+
+/* The sequences of a call and their rows (new tokens, queries, or rows read),
+ * laid out as for seq_attention: offsets int64 [seqs + 1], CSR; pad = 0: packed,
+ * pad > 0: rows = seqs * pad, sequence s the first min(off[s+1] - off[s], pad)
+ * rows of its block, the others never read.  lens int64 [seqs]: the tokens that
+ * each sequence holds.  table int32 [seqs][table_width]: the page of each page
+ * number; entries past a sequence's pages are not read.  slots int32 [seqs]
+ * (NULL: slot s for sequence s).
+ * Entries outside the cache are passed over: their tokens are neither written
+ * nor seen, and read as 0.  validate != 0 in the calls below checks offsets,
+ * lens, the table's entries in use and the slots on the host (and, where tokens
+ * are written, that no page or slot is written twice); it copies them back:
+ * synchronizing. */
+typedef struct {
+  int64_t seqs, rows, pad; /* seqs < 2^24, rows < 2^31 - 1024                   */
+  int64_t table_width;     /* at most 2^26                                      */
+  const int64_t* offsets;
+  const int64_t* lens;
+  const int32_t* table;
+  const int32_t* slots;
+} rs_cache_batch;
+
+/* New tokens, at positions lens[s], lens[s] + 1, ...: keys and queries turn by
+ * their position, column pairs (i, i + rotary / 2), or (2 i, 2 i + 1) interleaved,
+ * by position * frequency_i, in the model's type afterwards; columns from rotary
+ * on stay.  `turns`: device copy of rs_rotation_turns' result. */
+typedef struct {
+  const void *k, *v; /* [rows][heads_kv][head_dim]; both NULL: only q is turned */
+  const void* q;     /* [rows][heads_q][head_dim], or NULL                      */
+  void* q_out;       /* q turned, contiguous; rows past a padded sequence's end 0 */
+  int64_t k_stride, k_head_stride, v_stride, v_head_stride, q_stride, q_head_stride;
+  int32_t heads_q, rotary, interleaved, reserved;
+  const uint64_t* turns; /* [rotary / 2]                                        */
+  int64_t* new_lens;     /* [seqs], lens after the call, or NULL; not lens itself */
+} rs_cache_rows;
+
+/* turns (host, [rotary / 2]): the frequencies (radians a position: freqs, host, or
+ * where NULL base^(-2 i / rotary)) as 64-bit fractions of a turn, so that an angle
+ * is exact at any position.  Errors: RS_EINVAL. */
+rs_status rs_rotation_turns(const double* freqs, double base, int32_t rotary, uint64_t* turns);
+
+/* Writes the rows of k and v as the sequences' next tokens (one launch).  All
+ * pointers and strides are multiples of 16 bytes.  Errors: RS_EINVAL, RS_ENOMEM
+ * (validate), RS_EHIP. */
+rs_status seq_cache_append(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_rows* r, int32_t validate,
+                           rs_stream stream);
+
+/* Tokens start[s] .. start[s] + (off[s+1] - off[s]) - 1 (start NULL: from 0) of
+ * each sequence as rows k, v [rows][heads_kv][head_dim] of `out_dtype`, as the
+ * cache stands for them; tokens past a sequence's end are 0.  Packed only. */
+rs_status seq_cache_read(const rs_seq_cache* c, const rs_cache_batch* b, const int64_t* start, void* k, void* v,
+                         int32_t out_dtype, int32_t validate, rs_stream stream);
+
+/* Attention of query rows over the cache, as seq_attention_fwd with the tokens
+ * held (lens, the queries' own included where they have been appended) as keys:
+ * query i of Lq stands at p_i = i + lens - Lq, and
+ *   s_ij = cap(scale * q_i.k_j) - slope_h * |p_i - j|
+ *   out_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij)
+ * over all keys (causal = 0) or j <= p_i.  With pages (int32 [rows][heads_kv]
+ * [count], page numbers of the sequence), row i of a key head sees only the keys
+ * of those full pages and of the open page; entries that name no full page are
+ * passed over, a page named twice counts twice.  A query without a key gets 0.
+ * q may not be rotated any more; out is contiguous.  Scores, statistics and sums
+ * are fp32; bf16 probabilities are rounded as operands of the matrix
+ * instructions, fp32 ones keep 24 bits.
+ * Workspace: seq_cache_attention_workspace_bytes(...), 256-byte aligned, free for
+ * the next call once this one has completed in stream order; 0 for arguments the
+ * call refuses, or where none is needed. */
+typedef struct {
+  int32_t heads_q;   /* a multiple of heads_kv, at most 8192; rows * heads_q < 2^31 - 1024 */
+  int32_t causal;
+  int32_t count;     /* pages of a row, 0: all; at most 65536                   */
+  int32_t reserved;  /* 0                                                       */
+  int64_t max_q, max_len; /* the caller's bounds of a sequence's queries and
+                        tokens (0: none known): they only shape the launches    */
+  int64_t q_stride, q_head_stride;
+  double scale, softcap; /* as rs_attn_desc                                     */
+} rs_cache_query;
+size_t seq_cache_attention_workspace_bytes(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_query* q);
+rs_status seq_cache_attention(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_query* q, const void* rows,
+                              const int32_t* pages, const float* slopes, void* out, void* workspace,
+                              size_t workspace_bytes, int32_t validate, rs_stream stream);
+
+/* The pages that a query row looks at: for each row and key head the numbers of
+ * the `count` full pages with the highest score among those it sees any key of,
+ * ascending, then -1; pages int32 [rows][heads_kv][count].  The score is a cheap
+ * bound of the keys' products with the query, from the page's bounds:
+ *   units * max_h sq_h sum_c max(q8_c maximum_c, q8_c minimum_c)
+ * over the query heads h of the key head, with q8 = round(q / sq_h), ties to
+ * even, and sq_h the least power of two with max |q_h| <= 127 sq_h.  Whole numbers
+ * and powers of two: the choice is exact, equal scores go to the lower page.  A
+ * query that is not finite counts as 0, a page that is not finite comes first, one
+ * outside the cache last.  Workspace as above. */
+size_t seq_cache_select_workspace_bytes(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_query* q);
+rs_status seq_cache_select(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_query* q, const void* rows,
+                           int32_t* pages, void* workspace, size_t workspace_bytes, int32_t validate, rs_stream stream);
 
 /* Kernel timing hook: from now on, hipEvent_t `start` / `stop` time every
  * launch of the named kernel (NULL, NULL clears it).  For RS_K_POOL,

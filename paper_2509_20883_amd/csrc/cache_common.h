@@ -1,0 +1,97 @@
+// Device helpers of the paged sequence cache (gfx950): where things lie, and
+// 8-bit codes as operands of the matrix instructions.
+#pragma once
+
+#include "attn_common.h"
+#include "cache_internal.h"
+
+namespace rs {
+
+struct CacheSeq {
+  int64_t start;  // the sequence's first row
+  int rows, len, slot;
+};
+
+// Tokens that sequence s holds: lens[s], cut to what its table can name.
+__device__ inline int cache_len(const CacheArgs& c, int s) {
+  return static_cast<int>(min(max(c.lens[s], int64_t(0)), min(c.width << c.plog, int64_t(0x7FFFFF00))));
+}
+// The slot of its open pages, or -1.
+__device__ inline int cache_slot(const CacheArgs& c, int s) {
+  const int64_t x = c.slot_of ? static_cast<int64_t>(c.slot_of[s]) : s;
+  return x >= 0 && x < c.slots ? static_cast<int>(x) : -1;
+}
+// The page that holds page number n of sequence s, or -1.
+__device__ inline int cache_page(const CacheArgs& c, int s, int64_t n) {
+  if (n < 0 || n >= c.width) return -1;
+  const int32_t p = c.table[s * c.width + n];
+  return p >= 0 && p < c.pages ? p : -1;
+}
+// First byte of a page's keys (side 0) or values (side 1).
+__device__ inline int64_t cache_at(const CacheArgs& c, int page, int kvh, int side, int W) {
+  return ((static_cast<int64_t>(page) * c.hkv + kvh) * 2 + side) * (static_cast<int64_t>(W) << c.plog);
+}
+// First element of the open page of page number n.
+__device__ inline int64_t open_at(const CacheArgs& c, int slot, int64_t n, int kvh, int side) {
+  return ((((static_cast<int64_t>(slot) * 2 + (n & 1)) * c.hkv + kvh) * 2 + side) << c.plog) * c.d;
+}
+
+// Block numbers over the pages that a sequence's rows touch: off[s] / P + 2 s on,
+// enough for rows that start anywhere in a page (n rows touch at most n / P + 2).
+__device__ inline int find_pages(const int64_t* __restrict__ off, int seqs, int plog, int64_t b, int64_t& tile) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave;
+    const int s = lane * step;
+    const bool below = s < n && (max(off[lo + s], int64_t(0)) >> plog) + 2 * int64_t(lo + s) <= b;
+    const int c = max(1, static_cast<int>(__popcll(__ballot(below))));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  tile = b - ((max(off[lo], int64_t(0)) >> plog) + 2 * int64_t(lo));
+  return lo;
+}
+
+__device__ inline float bits_f32(uint32_t b) { return __uint_as_float(b); }
+
+// The exponent k, from -126 on, of the least power of two with top <= most 2^k,
+// for most = mant 2^exp2 (1 <= mant < 2).
+__device__ inline int unit_exp(float top, float mant, int exp2) {
+  const uint32_t b = __float_as_uint(top);
+  const float m = __uint_as_float((b & 0x007FFFFFu) | 0x3F800000u);
+  const int e = static_cast<int>(b >> 23) - 127;
+  return max(-126, m <= mant ? e - exp2 : e - exp2 + 1);
+}
+__device__ inline float exp2_int(int k) { return __uint_as_float(static_cast<uint32_t>(k + 127) << 23); }
+
+// Eight codes as bf16: both kinds are exact there.
+template <bool E4M3>
+__device__ inline bf16x8 codes8(uint32_t lo, uint32_t hi) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 w;
+  if (E4M3) {
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = (i < 2 ? lo : hi) >> (i & 1) * 16;
+      const float a = static_cast<float>(static_cast<int8_t>(x)), b = static_cast<float>(static_cast<int8_t>(x >> 8));
+      w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // whole numbers: no rounding
+    }
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// One code's value.
+template <bool E4M3>
+__device__ inline float code_value(uint8_t c) {
+  if (!E4M3) return static_cast<float>(static_cast<int8_t>(c));
+  return __builtin_amdgcn_cvt_f32_fp8(c, 0);
+}
+
+}  // namespace rs

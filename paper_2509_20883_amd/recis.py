@@ -7,7 +7,8 @@ fallback: if the library is not built, or no GPU is present, calls raise.
 Names follow the C ABI (include/recis_mi355x.h): ht_create, ht_find_or_insert,
 lookup_pool_fwd, lookup_pool_bwd, sparse_opt_step, lookup_pool_bwd_opt,
 ids_partition, fused_bucketize, fused_mod, layer_norm_fwd, layer_norm_bwd,
-seq_attention_fwd, seq_attention_bwd.
+seq_attention_fwd, seq_attention_bwd, seq_cache_append, seq_cache_read,
+seq_cache_attention, seq_cache_select.
 """
 from __future__ import annotations
 
@@ -108,6 +109,32 @@ class AttnDesc(C.Structure):
                 ("scale", C.c_double), ("softcap", C.c_double)]
 
 
+class CacheDesc(C.Structure):
+    _fields_ = [("codes", C.c_int32), ("dtype", C.c_int32), ("heads_kv", C.c_int32), ("head_dim", C.c_int32),
+                ("page_len", C.c_int32), ("reserved", C.c_int32), ("pages", C.c_int64), ("slots", C.c_int64),
+                ("data", C.c_void_p), ("scales", C.c_void_p), ("open", C.c_void_p), ("bounds", C.c_void_p),
+                ("units", C.c_void_p)]
+
+
+class CacheBatch(C.Structure):
+    _fields_ = [("seqs", C.c_int64), ("rows", C.c_int64), ("pad", C.c_int64), ("table_width", C.c_int64),
+                ("offsets", C.c_void_p), ("lens", C.c_void_p), ("table", C.c_void_p), ("slots", C.c_void_p)]
+
+
+class CacheRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("v_head_stride", C.c_int64), ("q_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("heads_q", C.c_int32), ("rotary", C.c_int32), ("interleaved", C.c_int32), ("reserved", C.c_int32),
+                ("turns", C.c_void_p), ("new_lens", C.c_void_p)]
+
+
+class CacheQuery(C.Structure):
+    _fields_ = [("heads_q", C.c_int32), ("causal", C.c_int32), ("count", C.c_int32), ("reserved", C.c_int32),
+                ("max_q", C.c_int64), ("max_len", C.c_int64), ("q_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("scale", C.c_double), ("softcap", C.c_double)]
+
+
 _lib = None
 
 
@@ -155,6 +182,17 @@ def lib() -> C.CDLL:
         "seq_attention_workspace_bytes": (C.c_size_t, [C.POINTER(AttnDesc), i32]),
         "seq_attention_fwd": (C.c_int, [C.POINTER(AttnDesc)] + [p] * 11 + [C.c_size_t, i32, p]),
         "seq_attention_bwd": (C.c_int, [C.POINTER(AttnDesc)] + [p] * 16 + [C.c_size_t, i32, p]),
+        "rs_rotation_turns": (C.c_int, [p, C.c_double, i32, p]),
+        "seq_cache_append": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CacheBatch), C.POINTER(CacheRows), i32, p]),
+        "seq_cache_read": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CacheBatch), p, p, p, i32, i32, p]),
+        "seq_cache_attention_workspace_bytes": (C.c_size_t, [C.POINTER(CacheDesc), C.POINTER(CacheBatch),
+                                                             C.POINTER(CacheQuery)]),
+        "seq_cache_attention": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CacheBatch), C.POINTER(CacheQuery)] + [p] * 5
+                                + [C.c_size_t, i32, p]),
+        "seq_cache_select_workspace_bytes": (C.c_size_t, [C.POINTER(CacheDesc), C.POINTER(CacheBatch),
+                                                          C.POINTER(CacheQuery)]),
+        "seq_cache_select": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CacheBatch), C.POINTER(CacheQuery)] + [p] * 3
+                             + [C.c_size_t, i32, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -589,6 +627,226 @@ class SeqAttention(_Workspace):
                                        _ptr(prefix), _ptr(slopes), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
                                        _ptr(dslopes), ws.data_ptr(), ws.numel(), int(validate), _stream()))
         return dq, dk, dv, dslopes
+
+
+class SeqCache(_Workspace):
+    """A paged cache of the keys and values of sequences, full pages in 8 bits.
+
+    pages of `page` tokens (32, 64, 128 or 256) and `slots` sequences' open
+    pages are allocated on the current GPU; which sequence has which pages and
+    slot is the caller's: table int32 [seqs, width] names the page of each of a
+    sequence's page numbers, slots int32 [seqs] its slot (default: its index),
+    lens int64 [seqs] the tokens it holds.  codes "i8" (scale max / 127 of a
+    page and head, the more exact for values without outliers) or "e4m3"
+    (power-of-two scale).  bounds: keep what ``select`` needs.
+
+    rotary columns of keys and queries are turned by their position when they
+    are appended, with frequencies base^(-2 i / rotary) or `freqs` (radians a
+    position, rotary / 2 of them), pairs (i, i + rotary / 2) or, interleaved,
+    (2 i, 2 i + 1).
+
+    ``append(k, v, offsets, lens, table, q=...)`` writes new tokens (packed
+    [rows, heads_kv, d] with CSR offsets, or padded [seqs, pad, heads_kv, d])
+    and returns (lens afterwards, q turned).  ``attend`` is SeqAttention over
+    the tokens held (inference only), with `pages` over the listed ones;
+    ``select`` lists the pages of the highest score for each row and key head;
+    ``read`` returns tokens as rows.  scale, softcap, causal and slopes are
+    SeqAttention's.  max_q and max_len bound a sequence's queries and tokens
+    where the caller knows: they only shape the launches.
+
+    Calls of one object share its workspace: issue them on one stream, or order
+    the streams, and keep the object as long as a graph that captured its calls.
+    """
+
+    def __init__(self, pages: int, slots: int, heads_kv: int, head_dim: int, page: int = 64, codes: str = "i8",
+                 dtype: torch.dtype = torch.bfloat16, bounds: bool = False, rotary: int = 0, base: float = 10000.0,
+                 freqs=None, interleaved: bool = False, scale: Optional[float] = None, softcap: float = 0.0,
+                 causal: bool = True):
+        super().__init__()
+        if codes not in ("i8", "e4m3"):
+            raise RecisError(EINVAL, "codes must be 'i8' or 'e4m3'")
+        if dtype not in _SEQ_TYPES:
+            raise RecisError(EINVAL, f"dtype must be float32 or bfloat16, got {dtype}")
+        if page not in (32, 64, 128, 256):
+            raise RecisError(EINVAL, "page must be 32, 64, 128 or 256")
+        if not 1 <= heads_kv <= 1024 or not 8 <= head_dim <= 128 or head_dim % 8:
+            raise RecisError(EINVAL, "heads_kv must be in [1, 1024] and head_dim a multiple of 8 in [8, 128]")
+        if pages < 0 or slots < 0:
+            raise RecisError(EINVAL, "pages and slots must be >= 0")
+        if rotary < 0 or rotary > head_dim or rotary % 2:
+            raise RecisError(EINVAL, "rotary must be even and at most head_dim")
+        host = (C.c_uint64 * max(rotary // 2, 1))()
+        own = None
+        if freqs is not None:
+            freqs = [float(f) for f in freqs]
+            if len(freqs) != rotary // 2:
+                raise RecisError(EINVAL, "freqs must have rotary / 2 values")
+            own = (C.c_double * max(len(freqs), 1))(*freqs)
+        _check(lib().rs_rotation_turns(own, base, rotary, host))
+        dev = torch.device("cuda", torch.cuda.current_device())
+        self.heads_kv, self.head_dim, self.page, self.dtype = heads_kv, head_dim, page, dtype
+        self.rotary, self.interleaved = rotary, bool(interleaved)
+        self.scale, self.softcap, self.causal = scale, float(softcap), bool(causal)
+        width = 32 if head_dim <= 32 else 64 if head_dim <= 64 else 128
+        self.codes = torch.empty(pages, heads_kv, 2, page * width, dtype=torch.uint8, device=dev)
+        self.scales = torch.empty(pages, heads_kv, 2, dtype=torch.float32, device=dev)
+        self.open = torch.empty(slots, 2, heads_kv, 2, page, head_dim, dtype=dtype, device=dev)
+        self.bounds = torch.empty(pages, heads_kv, 2, width, dtype=torch.int8, device=dev) if bounds else None
+        self.units = torch.empty(pages, heads_kv, dtype=torch.float32, device=dev) if bounds else None
+        # 64-bit fractions as signed words of the same bits
+        turns = [t - (1 << 64) if t >> 63 else t for t in host[:rotary // 2]]
+        self.turns = torch.tensor(turns, dtype=torch.int64, device=dev) if rotary else None
+        self._desc = CacheDesc(1 if codes == "e4m3" else 0, _SEQ_TYPES[dtype], heads_kv, head_dim, page, 0, pages, slots,
+                               self.codes.data_ptr(), self.scales.data_ptr(), self.open.data_ptr(), _ptr(self.bounds),
+                               _ptr(self.units))
+
+    def _layout(self, t: torch.Tensor, what: str, heads: int = 0):
+        """The tensor (copied if its strides do not serve), rows, pad, row and head strides."""
+        if not t.is_cuda or t.device != self.codes.device:
+            raise RecisError(EINVAL, "tensors must be on the GPU, the cache's")
+        if t.dtype != self.dtype:
+            raise RecisError(EINVAL, f"{what} must be {self.dtype}, got {t.dtype}")
+        if t.dim() not in (3, 4) or t.shape[-1] != self.head_dim or (heads and t.shape[-2] != heads):
+            raise RecisError(EINVAL, f"{what} must be [rows, heads, {self.head_dim}] or [seqs, pad, heads, {self.head_dim}]"
+                             + (f" with {heads} heads" if heads else ""))
+        unit = 16 // t.element_size()
+        st = t.stride()
+        if (st[-1] != 1 or st[-2] % unit or st[-3] % unit or max(st[-2], st[-3]) >= 1 << 31 or
+                (t.dim() == 4 and st[0] != t.shape[1] * st[1]) or t.data_ptr() % 16):
+            t = _packed(t)
+            st = t.stride()
+        if t.dim() == 4:
+            return t, t.shape[0] * t.shape[1], t.shape[1], st[1], st[2]
+        return t, t.shape[0], 0, st[0], st[1]
+
+    def _same(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
+        if t.device != self.codes.device or t.dtype != dtype:
+            raise RecisError(EINVAL, f"{what} must be {dtype} on the cache's GPU")
+        return t if t.is_contiguous() else t.contiguous()
+
+    def _batch(self, rows, pad, padded, offsets, lens, table, slots, own_slots=True):
+        if torch.cuda.current_device() != self.codes.device.index:
+            raise RecisError(EINVAL, "the cache's GPU must be the current one")
+        offsets = self._same(offsets, torch.int64, "offsets")
+        lens = self._same(lens, torch.int64, "lens")
+        table = self._same(table, torch.int32, "table")
+        seqs = offsets.numel() - 1
+        if seqs < 0 or lens.numel() != seqs or table.dim() != 2 or table.shape[0] != seqs:
+            raise RecisError(EINVAL, "offsets must be [seqs + 1], lens [seqs] and table [seqs, width]")
+        if padded is not None and padded != seqs:
+            raise RecisError(EINVAL, "a padded tensor must have one block per sequence")
+        if slots is not None:
+            slots = self._same(slots, torch.int32, "slots")
+            if slots.numel() != seqs:
+                raise RecisError(EINVAL, "slots must have one slot per sequence")
+        elif own_slots and self.open.shape[0] < seqs:
+            raise RecisError(EINVAL, "more sequences than slots")
+        return CacheBatch(seqs, rows, pad, table.shape[1], offsets.data_ptr(), lens.data_ptr(), table.data_ptr(),
+                          _ptr(slots)), (offsets, lens, table, slots)
+
+    def append(self, k: Optional[torch.Tensor], v: Optional[torch.Tensor], offsets: torch.Tensor, lens: torch.Tensor,
+               table: torch.Tensor, q: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+               validate: bool = False):
+        """Writes k and v as the sequences' tokens from lens on; returns (lens afterwards, q turned by the same
+        positions or None).  k = v = None turns q alone (candidates that are not kept): lens then come back as they
+        would be with the rows kept, and nothing is written."""
+        if (k is None) != (v is None) or (k is None and q is None):
+            raise RecisError(EINVAL, "append takes k and v, q, or all three")
+        shape, r, q_out = None, CacheRows(rotary=self.rotary, interleaved=int(self.interleaved), turns=_ptr(self.turns)), None
+        if k is not None:
+            k, rows, pad, r.k_stride, r.k_head_stride = self._layout(k, "k", self.heads_kv)
+            v, _, _, r.v_stride, r.v_head_stride = self._layout(v, "v", self.heads_kv)
+            if k.shape != v.shape:
+                raise RecisError(EINVAL, "k and v must have one shape")
+            r.k, r.v, shape = k.data_ptr(), v.data_ptr(), k.shape
+        if q is not None:
+            q, rows, pad, r.q_stride, r.q_head_stride = self._layout(q, "q")
+            if shape is not None and q.shape[:-2] != shape[:-2]:
+                raise RecisError(EINVAL, "q must have the rows of k")
+            q_out, shape = _like(q), q.shape
+            r.q, r.q_out, r.heads_q = q.data_ptr(), q_out.data_ptr(), q.shape[-2]
+        if k is not None and k.numel() == 0:
+            r.k = r.v = None
+        if q is not None and q.numel() == 0:
+            r.q = r.q_out = None
+        b, keep = self._batch(rows, pad, shape[0] if len(shape) == 4 else None, offsets, lens, table, slots)
+        new_lens = torch.empty_like(keep[1])
+        r.new_lens = new_lens.data_ptr()
+        _check(lib().seq_cache_append(C.byref(self._desc), C.byref(b), C.byref(r), int(validate), _stream()))
+        return new_lens, q_out
+
+    def read(self, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, rows: Optional[int] = None,
+             start: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+             dtype: Optional[torch.dtype] = None, validate: bool = False):
+        """(k, v) [rows, heads_kv, d] of `dtype` (default: the model's): tokens start[s] (default 0) on, offsets[s + 1] -
+        offsets[s] of each sequence.  rows: their number, offsets[seqs], where the caller knows it (else it is read from
+        the GPU, which waits for it)."""
+        dtype = self.dtype if dtype is None else dtype
+        if dtype not in _SEQ_TYPES:
+            raise RecisError(EINVAL, f"dtype must be float32 or bfloat16, got {dtype}")
+        if rows is None:
+            rows = int(offsets[-1])
+        b, keep = self._batch(rows, 0, None, offsets, lens, table, slots)
+        if start is not None:
+            start = self._same(start, torch.int64, "start")
+            if start.numel() != b.seqs:
+                raise RecisError(EINVAL, "start must have one position per sequence")
+        k = torch.empty(rows, self.heads_kv, self.head_dim, dtype=dtype, device=self.codes.device)
+        v = torch.empty_like(k)
+        _check(lib().seq_cache_read(C.byref(self._desc), C.byref(b), _ptr(start), k.data_ptr(), v.data_ptr(),
+                                    _SEQ_TYPES[dtype], int(validate), _stream()))
+        return k, v
+
+    def _query(self, q, offsets, lens, table, slots, count, max_q, max_len, own_slots=True):
+        q, rows, pad, qs, qh = self._layout(q, "q")
+        if q.shape[-2] < self.heads_kv or q.shape[-2] % self.heads_kv:
+            raise RecisError(EINVAL, "q's heads must be a multiple of heads_kv")
+        b, keep = self._batch(rows, pad, q.shape[0] if q.dim() == 4 else None, offsets, lens, table, slots,
+                              own_slots)
+        scale = self.scale if self.scale is not None else self.head_dim ** -0.5
+        return q, b, keep, CacheQuery(q.shape[-2], int(self.causal), count, 0, max_q, max_len, qs, qh, scale, self.softcap)
+
+    def attend(self, q: torch.Tensor, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
+               pages: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
+               slots: Optional[torch.Tensor] = None, max_q: int = 0, max_len: int = 0,
+               out: Optional[torch.Tensor] = None, validate: bool = False) -> torch.Tensor:
+        shape = q.shape
+        count = 0 if pages is None else pages.shape[-1]
+        q, b, keep, d = self._query(q, offsets, lens, table, slots, count, max_q, max_len)
+        if pages is not None:
+            pages = self._same(pages, torch.int32, "pages")
+            if pages.shape != (*shape[:-2], self.heads_kv, count) or count < 1:
+                raise RecisError(EINVAL, "pages must be [rows, heads_kv, count] of q's rows")
+        if slopes is not None:
+            slopes = self._same(slopes, torch.float32, "slopes")
+            if slopes.numel() != shape[-2]:
+                raise RecisError(EINVAL, "slopes must have one value per query head")
+        if out is None:
+            out = _like(q)
+        elif out.shape != shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
+            raise RecisError(EINVAL, "out must be a contiguous GPU tensor of q's shape and type")
+        need = lib().seq_cache_attention_workspace_bytes(C.byref(self._desc), C.byref(b), C.byref(d))
+        ws = self._take(need, q) if need else None
+        _check(lib().seq_cache_attention(C.byref(self._desc), C.byref(b), C.byref(d), q.data_ptr(), _ptr(pages), _ptr(slopes),
+                                         out.data_ptr(), _ptr(ws), ws.numel() if need else 0, int(validate), _stream()))
+        return out
+
+    def select(self, q: torch.Tensor, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, count: int,
+               max_q: int = 0, max_len: int = 0, validate: bool = False) -> torch.Tensor:
+        """int32 [rows, heads_kv, count] (or [seqs, pad, heads_kv, count]): the numbers of the full pages of the highest
+        score, ascending, then -1."""
+        if self.bounds is None:
+            raise RecisError(EINVAL, "the cache keeps no bounds")
+        if count < 1:
+            raise RecisError(EINVAL, "count must be >= 1")
+        shape = q.shape
+        q, b, keep, d = self._query(q, offsets, lens, table, None, count, max_q, max_len, False)
+        pages = torch.empty(*shape[:-2], self.heads_kv, count, dtype=torch.int32, device=q.device)
+        need = lib().seq_cache_select_workspace_bytes(C.byref(self._desc), C.byref(b), C.byref(d))
+        ws = self._take(need, q) if need else None
+        _check(lib().seq_cache_select(C.byref(self._desc), C.byref(b), C.byref(d), q.data_ptr(), pages.data_ptr(), _ptr(ws),
+                                      ws.numel() if need else 0, int(validate), _stream()))
+        return pages
 
 
 PROBES = {"read": 0, "write": 1, "copy": 2, "gather": 3, "rmw": 4}
