@@ -56,16 +56,43 @@ __device__ inline void split(const float (&x)[8], bf16x8 (&f)[N]) {
   }
 }
 
+// The matrix instruction of M x M results: M = 32 for many rows, 16 where a tile
+// has at most 16, which leaves half the registers. A lane's group (lane / M) holds
+// slots 8 group .. 8 group + 7 of the product and, of a result, 4 consecutive rows
+// of column lane % M at a time.
+template <int M>
+struct Shape;
+template <>
+struct Shape<32> {
+  typedef f32x16 acc;
+  __device__ static inline acc mma(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  __device__ static inline float column_max(float x) { return other_half_max(x); }
+  __device__ static inline float column_sum(float x) { return other_half_sum(x); }
+};
+template <>
+struct Shape<16> {
+  typedef f32x4 acc;
+  __device__ static inline acc mma(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  __device__ static inline float column_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return other_half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  }
+  __device__ static inline float column_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return other_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+  }
+};
+
 // The sum of the products of two sets of pieces, the smallest (below 2^-24 of
 // the whole) left out.
-template <int NA, int NB>
-__device__ inline f32x16 mma_pieces(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x16 c) {
+template <int M, int NA, int NB>
+__device__ inline typename Shape<M>::acc mma_pieces(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], typename Shape<M>::acc c) {
   constexpr int kMost = NA > NB ? NA : NB;
 #pragma unroll
   for (int i = NA - 1; i >= 0; --i)
 #pragma unroll
     for (int j = NB - 1; j >= 0; --j)
-      if (i + j < kMost) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], c, 0, 0, 0);
+      if (i + j < kMost) c = Shape<M>::mma(a[i], b[j], c);
   return c;
 }
 
@@ -97,17 +124,19 @@ __device__ inline void pieces_of(const uint16_t (&x)[8], bf16x8 (&f)[1]) {
 }
 __device__ inline void pieces_of(const float (&x)[8], bf16x8 (&f)[3]) { split(x, f); }
 
+constexpr int kPartBlocks = 8;
+
 // Where a row tile stands and which blocks of 32 keys its sequence has for it.
 struct TileAt {
   int s, token0, row0;  // row0: the tile's first row (of the sequence, or of the token's heads where pages are listed)
   int rows, lk, lq;     // rows: of the sequence (of the token)
   int64_t start;
   int closed, end;      // tokens in full pages, tokens that any row of the tile sees
-  int full_blocks, blocks, per;  // blocks: of 32 keys, those of full pages first; per: of a split
+  int blocks, per, parts;  // blocks of 32 keys in full pages; per: of a part
 };
 
 // False: no such tile.
-__device__ inline bool tile_at(const CacheAttn& a, int64_t unit, int tile_rows, int waves, TileAt& t) {
+__device__ inline bool tile_at(const CacheAttn& a, int64_t unit, int tile_rows, TileAt& t) {
   const CacheArgs& c = a.c;
   int64_t tile;
   if (a.list) {
@@ -149,19 +178,21 @@ __device__ inline bool tile_at(const CacheAttn& a, int64_t unit, int tile_rows, 
     last = t.row0 < t.rows ? div_group(min(t.row0 + tile_rows, t.rows) - 1, a.group) : -1;
   }
   t.end = last < 0 || t.rows == 0 ? 0 : a.causal ? max(0, min(t.lk, last + t.lk - t.lq + 1)) : t.lk;
-  if (t.end == 0) t.full_blocks = 0;
-  else if (a.list) t.full_blocks = a.count << (c.plog - 5);
-  else t.full_blocks = (min(t.end, t.closed) + kCacheBlock - 1) / kCacheBlock;
-  t.blocks = t.full_blocks + (t.end > t.closed ? (t.end - t.closed + kCacheBlock - 1) / kCacheBlock : 0);
+  if (t.end == 0) t.blocks = 0;
+  else if (a.list) t.blocks = a.count << (c.plog - 5);
+  else t.blocks = (min(t.end, t.closed) + kCacheBlock - 1) / kCacheBlock;
+  // at least eight blocks to a part: fewer are not worth its way through memory
   const int share = (t.blocks + a.splits - 1) / a.splits;
-  // at least eight blocks to a split: fewer are not worth their part's way through memory
-  t.per = max(8, (share + waves - 1) / waves * waves);
+  t.per = max(kPartBlocks, (share + kPartBlocks - 1) / kPartBlocks * kPartBlocks);
+  t.parts = max(1, (t.blocks + t.per - 1) / t.per);
   return true;
 }
 
-template <typename T, int HD>
+// A lane's output columns and its row's running maximum, the height above it at
+// which it moves, and sum of the softmax, in base 2.
+template <int M, int HD>
 struct AttnState {
-  f32x16 acc[HD / 32];
+  typename Shape<M>::acc acc[HD / M];
   float m, move, l;
 };
 
@@ -170,12 +201,12 @@ struct RowParams {
   float slope, scale, cap;
 };
 
-// 32 keys from position j0 on into the softmax: p comes as the products of the
-// codes and leaves as probabilities times vs.
-template <typename T, int HD>
-__device__ __forceinline__ void soften(AttnState<T, HD>& st, float (&p)[16], const RowParams& r, bool capped, bool sloped,
-                                       float ks, float vs, int j0, int half) {
-  const int j = j0 + half * 16;  // register i is key j + i
+// The lane's 16 keys from position j on into the softmax: p comes as the products
+// of the codes and leaves as probabilities times vs. masked: some lane's row may
+// not see some key of the step.
+template <typename T, int M, int HD>
+__device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[16], const RowParams& r, bool capped, bool sloped,
+                                       float ks, float vs, int j, bool masked) {
   float c = r.scale * kLog2e * ks;
   if (capped) {
     c = r.cap * kLog2e;
@@ -189,7 +220,7 @@ __device__ __forceinline__ void soften(AttnState<T, HD>& st, float (&p)[16], con
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = p[i] * c - (r.slope * fabsf(dist + static_cast<float>(i)) + st.m);
   }
-  if (j0 + kCacheBlock > r.least) {
+  if (masked) {
     const int left = r.limit - j;
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = i < left ? p[i] : -INFINITY;
@@ -197,7 +228,7 @@ __device__ __forceinline__ void soften(AttnState<T, HD>& st, float (&p)[16], con
   float top = p[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
-  top = other_half_max(top);
+  top = Shape<M>::column_max(top);
   // the running maximum moves only when a score passes it by 2^8
   if (__any(top > st.move)) {
     const bool up = top > st.move;
@@ -207,7 +238,7 @@ __device__ __forceinline__ void soften(AttnState<T, HD>& st, float (&p)[16], con
     st.move = up ? 8.0f : st.move;
     st.l *= alpha;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) st.acc[i] *= alpha;
+    for (int i = 0; i < HD / M; ++i) st.acc[i] *= alpha;
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] -= by;
   }
@@ -221,29 +252,33 @@ __device__ __forceinline__ void soften(AttnState<T, HD>& st, float (&p)[16], con
   st.l += sum;
 }
 
-__device__ inline void halves(const float (&p)[16], int t, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = p[8 * t + e];
-}
+// Waves of a SIMD that the registers are kept down for.
+template <typename T, int HD, int M>
+constexpr int kResident = HD <= 32 ? 3 : HD <= 64 && (M == 16 || sizeof(T) == 2) ? 3 : HD * sizeof(T) <= 256 || M == 16 ? 2 : 1;
 
-// WR waves along the rows, WK along the keys.
-template <typename T, bool E4M3, int HD, int WR, int WK>
-__global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a) {
-  constexpr int KS = HD / 32, DT = HD / 32, NP = Pieces<T>::N, kRows = 32 * WR;
+// Tiles of WR M rows: WR waves along the rows, WK along the keys, each taking steps
+// of 1024 / M keys.
+template <typename T, bool E4M3, int HD, int M, int WR, int WK>
+__global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_attn(const CacheAttn a) {
+  typedef Shape<M> S;
+  constexpr int G = kWave / M;                       // lane groups
+  constexpr int B = 16 * G / kCacheBlock;            // blocks of a step
+  constexpr int KT = 16 * G / M;                     // key tiles of a step
+  constexpr int KC = HD < 16 * G ? 1 : HD / (16 * G);  // 16-column chunks of a key per lane
+  constexpr int DT = HD / M, NP = Pieces<T>::N, kRows = M * WR;
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int wr = wave % WR, wk = wave / WR, half = lane >> 5, col = lane & 31;
+  const int wr = wave % WR, wk = wave / WR, grp = lane / M, col = lane % M;
   const int64_t b = a.block0 + blockIdx.x;
-  const int split_at = static_cast<int>(b % a.splits);
+  const int part = static_cast<int>(b % a.splits);
   const int kvh = static_cast<int>(b / a.splits % c.hkv);
   const int64_t unit = b / a.splits / c.hkv;
   TileAt t;
-  if (!tile_at(a, unit, kRows, WK, t)) return;  // block-uniform
-  const int b0 = split_at * t.per, b1 = min(b0 + t.per, t.blocks);
-  if (split_at > 0 && b0 >= t.blocks) return;
-  const bool joined = t.blocks > t.per;
+  if (!tile_at(a, unit, kRows, t) || part >= t.parts) return;  // block-uniform
+  const int b0 = part * t.per, b1 = min(b0 + t.per, t.blocks);
+  const bool joined = t.parts > 1;
 
-  const int r = t.row0 + wr * 32 + col;
+  const int r = t.row0 + wr * M + col;
   const bool live = r < t.rows;
   RowOf me;
   if (a.list) {
@@ -255,161 +290,184 @@ __global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a)
   RowParams rp;
   rp.limit = !live ? 0 : a.causal ? max(0, min(t.lk, me.token + t.lk - t.lq + 1)) : t.lk;
   rp.pos = me.token + t.lk - t.lq;
-  const int w0 = t.row0 + wr * 32;
-  rp.least = !a.causal ? t.lk : a.list ? rp.limit : w0 < t.rows ? max(0, min(t.lk, div_group(w0, a.group) + t.lk - t.lq + 1)) : 0;
-  rp.least = __builtin_amdgcn_readfirstlane(rp.least);
+  // keys that every row of the wave sees: limits do not fall along the rows
+  const int least = __builtin_amdgcn_readfirstlane(rp.limit);
   rp.slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
   rp.scale = a.scale;
   rp.cap = a.cap;
   const bool capped = a.cap > 0.0f, sloped = a.slopes != nullptr;
 
-  bf16x8 qf[2 * KS][NP];
+  bf16x8 qf[2 * KC][NP];
   {
     const T* q = static_cast<const T*>(a.q.p) + (t.start + me.token) * a.q.row + me.head * a.q.head;
 #pragma unroll
-    for (int i = 0; i < 2 * KS; ++i) {
-      const int d0 = i / 2 * 32 + half * 16 + (i & 1) * 8;
+    for (int i = 0; i < 2 * KC; ++i) {
+      const int d0 = i / 2 * 16 * G + grp * 16 + (i & 1) * 8;
       load8(q + d0, live && d0 < c.d, qf[i]);
     }
   }
-  AttnState<T, HD> st;
+  AttnState<M, HD> st;
 #pragma unroll
-  for (int i = 0; i < DT; ++i) st.acc[i] = f32x16{};
+  for (int i = 0; i < DT; ++i) st.acc[i] = typename S::acc{};
   st.m = 0.0f;
   st.move = -INFINITY;
   st.l = 0.0f;
 
-  // a lane's key of the scores' rows: register i of half h then holds key 16 h + i
-  const int key = ((col >> 2) & 1) * 16 + (col >> 3) * 4 + (col & 3);
-  const int sub_mask = (1 << (c.plog - 5)) - 1;
+  // the lane's row of a key tile, so that scores 0 .. 15 of group g are keys 16 g ..
+  auto key_of = [&](int tile) { return M == 32 ? ((col >> 2) & 1) * 16 + (col >> 3) * 4 + (col & 3) : (col >> 2) * 16 + tile * 4 + (col & 3); };
   const int64_t page_bytes = static_cast<int64_t>(HD) << c.plog;
-  const int full_end = min(b1, t.full_blocks);
-  struct Codes {
-    u32x4 k[KS], v[DT];
-    float2 scale;
-    int j0;
-  };
-  int ids = -1, nums = 0;
-  // block n of the wave's own, the i-th: its page number and page, or page < 0
-  auto fetch = [&](int n, int i, Codes& x) -> bool {
-    if ((i & (kWave - 1)) == 0) {  // the next 64 of the wave's pages, one per lane
-      const int64_t mine = n + static_cast<int64_t>(lane) * WK;
-      nums = -1;
-      if (mine < full_end) {
-        const int at = static_cast<int>(mine) >> (c.plog - 5);
-        nums = a.list ? a.list[((t.start + t.token0) * c.hkv + kvh) * a.count + at] : at;
-        if (nums < 0 || nums >= t.closed >> c.plog) nums = -1;
-      }
-      ids = cache_page(c, t.s, nums);
+  const int sub_mask = (1 << (c.plog - 5)) - 1;
+
+  // the wave's steps: n blocks from b0 + wk B on, every WK B
+  int pages = -1, firsts = 0;  // of the next blocks, one per lane: page and first token
+  auto look = [&](int n) {
+    const int64_t mine = n + static_cast<int64_t>(lane / B) * (WK * B) + lane % B;
+    int num = -1;
+    firsts = 0;
+    if (mine < b1) {
+      const int at = static_cast<int>(mine) >> (c.plog - 5);
+      num = a.list ? a.list[((t.start + t.token0) * c.hkv + kvh) * a.count + at] : at;
+      if (num >= t.closed >> c.plog) num = -1;
+      firsts = (num << c.plog) + ((static_cast<int>(mine) & sub_mask) << 5);
     }
-    const int page = __builtin_amdgcn_readlane(ids, i & (kWave - 1));
-    if (page < 0) return false;
-    const int sub = n & sub_mask;
-    x.j0 = (__builtin_amdgcn_readlane(nums, i & (kWave - 1)) << c.plog) + sub * kCacheBlock;
-    const int64_t at = static_cast<int64_t>(page) * c.hkv + kvh;
-    const uint8_t* kp = c.data + at * 2 * page_bytes;
-    const uint8_t* vp = kp + page_bytes;
-#pragma unroll
-    for (int i = 0; i < KS; ++i)
-      x.k[i] = *reinterpret_cast<const u32x4*>(kp + ((((2 * i + half) << c.plog) + sub * kCacheBlock + key) << 4));
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-      x.v[i] = *reinterpret_cast<const u32x4*>(vp + (((sub * 2 + half) * HD + i * 32 + col) << 4));
-    x.scale = reinterpret_cast<const float2*>(c.scales)[at];
-    return true;
+    pages = cache_page(c, t.s, num);
   };
-  auto absorb = [&](const Codes& x) {
-    f32x16 sc = {};
+  // block i of the step at place j (0 .. 64 / B - 1) of those looked up
+  auto page_at = [&](int j, int i) { return B == 1 ? __builtin_amdgcn_readlane(pages, j) : __shfl(pages, j * B + i, kWave); };
+  auto first_at = [&](int j, int i) { return B == 1 ? __builtin_amdgcn_readlane(firsts, j) : __shfl(firsts, j * B + i, kWave); };
+
+  u32x4 kc[KT][KC], vc[DT];
+  float2 scale = make_float2(0.0f, 0.0f);
+  auto load_keys = [&](int j) {
+    const int i = B == 1 ? 0 : col >> 3;  // the lane's keys lie in one block
+    const int page = page_at(j, i), sub = (first_at(j, i) >> 5) & sub_mask;
+    const uint8_t* p = c.data + (static_cast<int64_t>(page) * c.hkv + kvh) * 2 * page_bytes;
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
+    for (int x = 0; x < KT; ++x)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 kf[1] = {codes8<E4M3>(x.k[i][2 * u], x.k[i][2 * u + 1])};
-        sc = mma_pieces(kf, qf[2 * i + u], sc);
+      for (int y = 0; y < KC; ++y) {
+        const int chunk = y * G + grp;
+        kc[x][y] = u32x4{0, 0, 0, 0};
+        if (page >= 0 && (HD >= 16 * G || chunk < HD / 16))
+          kc[x][y] = *reinterpret_cast<const u32x4*>(p + (((chunk << c.plog) + sub * kCacheBlock + (key_of(x) & 31)) << 4));
       }
+  };
+  auto load_values = [&](int j) -> int {  // the lane's first key, or -1
+    const int i = B == 1 ? 0 : grp >> 1;
+    const int page = page_at(j, i), first = first_at(j, i), sub = (first >> 5) & sub_mask;
+    const int64_t at = static_cast<int64_t>(page) * c.hkv + kvh;
+    const uint8_t* p = c.data + (at * 2 + 1) * page_bytes;
+    scale = make_float2(0.0f, 0.0f);
+    if (page >= 0) scale = reinterpret_cast<const float2*>(c.scales)[at];
+#pragma unroll
+    for (int x = 0; x < DT; ++x) {
+      vc[x] = u32x4{0, 0, 0, 0};
+      if (page >= 0) vc[x] = *reinterpret_cast<const u32x4*>(p + (((sub * 2 + (grp & 1)) * HD + x * M + col) << 4));
+    }
+    return page >= 0 ? first + (grp & 1) * 16 : -1;
+  };
+
+  const int stride = WK * B;
+  int n = b0 + wk * B, j = 0;
+  if (n < b1) {
+    look(n);
+    load_keys(0);
+  }
+  for (; n < b1; n += stride) {
+    const int key0 = load_values(j);
     float p[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = sc[i];
-    soften(st, p, rp, capped, sloped, x.scale.x, x.scale.y, x.j0, half);
+    for (int x = 0; x < KT; ++x) {
+      typename S::acc sc = {};
+#pragma unroll
+      for (int y = 0; y < KC; ++y)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 kf[1] = {codes8<E4M3>(kc[x][y][2 * u], kc[x][y][2 * u + 1])};
+          sc = mma_pieces<M>(kf, qf[2 * y + u], sc);
+        }
+#pragma unroll
+      for (int i = 0; i < 16 / KT; ++i) p[x * (16 / KT) + i] = sc[i];
+    }
+    // the next keys into the same registers, under the softmax and the second product
+    if (n + stride < b1) {
+      j = j + 1 == kWave / B ? 0 : j + 1;
+      if (j == 0) look(n + stride);
+      load_keys(j);
+    }
+    RowParams now = rp;
+    now.limit = key0 < 0 ? INT32_MIN / 2 : rp.limit;  // a page that is not there
+    const bool masked = !__all(key0 >= 0 && key0 + 16 <= least);
+    soften<T>(st, p, now, capped, sloped, scale.x, scale.y, key0, masked);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float y[8];
-      halves(p, u, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
       bf16x8 pf[NP];
       split(y, pf);
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        const bf16x8 vf[1] = {codes8<E4M3>(x.v[i][2 * u], x.v[i][2 * u + 1])};
-        st.acc[i] = mma_pieces(vf, pf, st.acc[i]);
+      for (int x = 0; x < DT; ++x) {
+        const bf16x8 vf[1] = {codes8<E4M3>(vc[x][2 * u], vc[x][2 * u + 1])};
+        st.acc[x] = mma_pieces<M>(vf, pf, st.acc[x]);
       }
     }
-  };
-
-  {
-    Codes now, next;
-    int n = b0 + wk, i = 0;
-    bool have = n < full_end && fetch(n, i, now);
-    while (n < full_end) {
-      const int n1 = n + WK;
-      const bool more = n1 < full_end && fetch(n1, i + 1, next);
-      if (have) absorb(now);
-      now = next;
-      have = more;
-      n = n1;
-      ++i;
-    }
   }
-  // the open page
-  const int slot = cache_slot(c, t.s);
-  for (int n = b0 + wk; n < b1 && slot >= 0; n += WK) {
-    if (n < t.full_blocks) continue;
-    const int k0 = (n - t.full_blocks) * kCacheBlock, held = t.lk - t.closed;
+  // the open page, with the last part
+  const int slot = cache_slot(c, t.s), held = t.lk - t.closed, most = t.end - t.closed;
+  if (part == t.parts - 1 && slot >= 0) {
     const T* kp = static_cast<const T*>(c.open) + open_at(c, slot, t.closed >> c.plog, kvh, 0);
     const T* vp = kp + (static_cast<int64_t>(c.d) << c.plog);
-    f32x16 sc = {};
+    for (int k0 = wk * 16 * G; k0 < most; k0 += WK * 16 * G) {
+      float p[16];
 #pragma unroll
-    for (int i = 0; i < 2 * KS; ++i) {
-      const int d0 = i / 2 * 32 + half * 16 + (i & 1) * 8;
-      bf16x8 kf[NP];
-      load8(kp + (k0 + key) * c.d + d0, k0 + key < held && d0 < c.d, kf);
-      sc = mma_pieces(kf, qf[i], sc);
-    }
-    float p[16];
+      for (int x = 0; x < KT; ++x) {
+        const int k = k0 + key_of(x);
+        typename S::acc sc = {};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = sc[i];
-    RowParams tp = rp;
-    tp.least = 0;  // the page ends somewhere in here
-    soften(st, p, tp, capped, sloped, 1.0f, 1.0f, t.closed + k0, half);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      float y[8];
-      halves(p, u, y);
-      bf16x8 pf[NP];
-      split(y, pf);
-#pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        T x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int k = k0 + half * 16 + u * 8 + e;
-          x[e] = T(0);
-          if (k < held && i * 32 + col < c.d) x[e] = vp[k * c.d + i * 32 + col];
+        for (int y = 0; y < 2 * KC; ++y) {
+          const int d0 = y / 2 * 16 * G + grp * 16 + (y & 1) * 8;
+          bf16x8 kf[NP];
+          load8(kp + k * c.d + d0, k < held && d0 < c.d, kf);
+          sc = mma_pieces<M>(kf, qf[y], sc);
         }
-        bf16x8 vf[NP];
-        pieces_of(x, vf);
-        st.acc[i] = mma_pieces(vf, pf, st.acc[i]);
+#pragma unroll
+        for (int i = 0; i < 16 / KT; ++i) p[x * (16 / KT) + i] = sc[i];
+      }
+      soften<T>(st, p, rp, capped, sloped, 1.0f, 1.0f, t.closed + k0 + grp * 16, true);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
+        bf16x8 pf[NP];
+        split(y, pf);
+#pragma unroll
+        for (int x = 0; x < DT; ++x) {
+          T z[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int k = k0 + grp * 16 + u * 8 + e;
+            z[e] = T(0);
+            if (k < held && x * M + col < c.d) z[e] = vp[k * c.d + x * M + col];
+          }
+          bf16x8 vf[NP];
+          pieces_of(z, vf);
+          st.acc[x] = mma_pieces<M>(vf, pf, st.acc[x]);
+        }
       }
     }
   }
 
-  st.l = other_half_sum(st.l);
+  st.l = S::column_sum(st.l);
   float m = st.m, l = st.l;
+  constexpr int R = M == 32 ? 16 : 4;  // a lane's registers of a tile
   if constexpr (WK > 1) {
     // the waves' parts: m = max m_w, acc = sum acc_w 2^(m_w - m), l alike
-    constexpr int kPart = DT * 16 * kWave * sizeof(float);
+    constexpr int kPart = DT * R * kWave * sizeof(float);
     __shared__ __align__(16) char parts[WK / 2 * WR * kPart];
-    __shared__ float2 sh_ml[WK][WR][32];
-    if (half == 0) sh_ml[wk][wr][col] = make_float2(m, l);
+    __shared__ float2 sh_ml[WK][WR][M];
+    if (grp == 0) sh_ml[wk][wr][col] = make_float2(m, l);
     __syncthreads();
     float base = -INFINITY;
 #pragma unroll
@@ -425,16 +483,16 @@ __global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a)
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            at[(i * 4 + e) * kWave] =
+          for (int e = 0; e < R / 4; ++e)
+            at[(i * (R / 4) + e) * kWave] =
                 f32x4{st.acc[i][4 * e], st.acc[i][4 * e + 1], st.acc[i][4 * e + 2], st.acc[i][4 * e + 3]};
       __syncthreads();
       if (wk < w)
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4 x = at[(i * 4 + e) * kWave];
+          for (int e = 0; e < R / 4; ++e) {
+            const f32x4 x = at[(i * (R / 4) + e) * kWave];
 #pragma unroll
             for (int y = 0; y < 4; ++y) st.acc[i][4 * e + y] += x[y];
           }
@@ -451,18 +509,18 @@ __global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a)
   }
   // rows of the tile: those of the padded copy past the sequence's end get 0
   const int64_t out_rows = a.list ? a.group : c.pad > 0 ? c.pad * a.group : static_cast<int64_t>(t.rows);
-  if (r >= out_rows || (!live && split_at > 0)) return;
+  if (r >= out_rows || (!live && part > 0)) return;
   if (joined && live) {
-    const int64_t at = ((unit * c.hkv + kvh) * a.splits + split_at) * kRows + wr * 32 + col;
+    const int64_t at = ((unit * c.hkv + kvh) * a.splits + part) * kRows + wr * M + col;
     float* po = a.part_o + at * c.d;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d0 = i * 32 + g * 8 + half * 4;
+      for (int g = 0; g < R / 4; ++g) {
+        const int d0 = i * M + g * 4 * G + grp * 4;
         if (d0 < c.d) store4(po + d0, st.acc[i][4 * g], st.acc[i][4 * g + 1], st.acc[i][4 * g + 2], st.acc[i][4 * g + 3]);
       }
-    if (half == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, l);
+    if (grp == 0) reinterpret_cast<float2*>(a.part_ml)[at] = make_float2(m, l);
     return;
   }
   const bool none = !live || l == 0.0f;  // no key: 0 (a NaN sum stays)
@@ -471,8 +529,8 @@ __global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a)
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d0 = i * 32 + g * 8 + half * 4;
+    for (int g = 0; g < R / 4; ++g) {
+      const int d0 = i * M + g * 4 * G + grp * 4;
       if (d0 >= c.d) continue;
       float x[4];
 #pragma unroll
@@ -485,7 +543,7 @@ __global__ __launch_bounds__(WR* WK* kWave) void k_cache_attn(const CacheAttn a)
 // columns and a share of the splits each.
 //   m = max m_c,  l = sum l_c 2^(m_c - m),  out = sum acc_c 2^(m_c - m) / l
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_rows, int waves, int64_t block0) {
+__global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_rows, int64_t block0) {
   __shared__ float4 sh_o[NT];
   __shared__ float sh_l[NT], sh_m[NT / kWave];
   const CacheArgs& c = a.c;
@@ -505,8 +563,8 @@ __global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_r
   int64_t unit;
   int at;
   if (a.list) {
-    const int parts = (a.group + tile_rows - 1) / tile_rows, r = head - kvh * a.group;
-    unit = u * parts + r / tile_rows;
+    const int tiles = (a.group + tile_rows - 1) / tile_rows, r = head - kvh * a.group;
+    unit = u * tiles + r / tile_rows;
     at = r % tile_rows;
   } else {
     const int64_t r = token * a.group + head - kvh * a.group;
@@ -516,9 +574,8 @@ __global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_r
     at = static_cast<int>(r % tile_rows);
   }
   TileAt t;
-  if (!tile_at(a, unit, tile_rows, waves, t)) return;
-  if (t.blocks <= t.per) return;  // written
-  const int parts = (t.blocks + t.per - 1) / t.per;
+  if (!tile_at(a, unit, tile_rows, t) || t.parts == 1) return;  // written
+  const int parts = t.parts;
   const int64_t slot0 = (unit * c.hkv + kvh) * a.splits * tile_rows + at;
 
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
@@ -571,7 +628,6 @@ __global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_r
          none ? 0.0f : o.y * inv, none ? 0.0f : o.z * inv, none ? 0.0f : o.w * inv);
 }
 
-constexpr int kKeyWaves = 8, kRowWaves = 4;
 constexpr int64_t kMostBlocks = int64_t(1) << 21;
 
 template <typename T, bool E4M3, int HD>
@@ -580,16 +636,16 @@ hipError_t run(CacheAttn a, hipStream_t s) {
   for (int64_t b = 0; b < blocks; b += kMostBlocks) {
     a.block0 = b;
     const unsigned now = static_cast<unsigned>(std::min(blocks - b, kMostBlocks));
-    if (a.wide) k_cache_attn<T, E4M3, HD, kRowWaves, 1><<<now, kRowWaves * kWave, 0, s>>>(a);
-    else k_cache_attn<T, E4M3, HD, 1, kKeyWaves><<<now, kKeyWaves * kWave, 0, s>>>(a);
+    if (a.tile_rows == 16) k_cache_attn<T, E4M3, HD, 16, 1, 4><<<now, 4 * kWave, 0, s>>>(a);
+    else if (a.tile_rows == 32) k_cache_attn<T, E4M3, HD, 32, 1, 4><<<now, 4 * kWave, 0, s>>>(a);
+    else k_cache_attn<T, E4M3, HD, 32, 4, 1><<<now, 4 * kWave, 0, s>>>(a);
   }
   if (a.splits > 1) {
-    const int tile_rows = a.wide ? 32 * kRowWaves : 32, waves = a.wide ? 1 : kKeyWaves;
     const int64_t rows = (a.c.pad > 0 ? a.c.rows : a.c.rows + a.c.seqs) * a.hq;
     for (int64_t b = 0; b < rows; b += kMostBlocks) {
       const unsigned now = static_cast<unsigned>(std::min(rows - b, kMostBlocks));
-      if (a.splits > 32) k_cache_join<T, 1024><<<now, 1024, 0, s>>>(a, tile_rows, waves, b);
-      else k_cache_join<T, 128><<<now, 128, 0, s>>>(a, tile_rows, waves, b);
+      if (a.splits > 32) k_cache_join<T, 1024><<<now, 1024, 0, s>>>(a, a.tile_rows, b);
+      else k_cache_join<T, 128><<<now, 128, 0, s>>>(a, a.tile_rows, b);
     }
   }
   return hipGetLastError();
@@ -616,8 +672,8 @@ size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_
   if (c.seqs == 0 || c.rows == 0) return 0;
   int64_t most_q = c.pad > 0 ? c.pad : c.rows;
   if (c.pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
-  a->wide = !a->list && most_q * a->group > 32;
-  const int tile_rows = a->wide ? 32 * kRowWaves : 32;
+  const int64_t most_rows = a->list ? a->group : most_q * a->group;
+  const int tile_rows = a->tile_rows = most_rows <= 16 ? 16 : most_rows <= 32 || a->list ? 32 : 128;
   if (a->list) {
     a->units = (c.pad > 0 ? c.rows : c.rows + c.seqs) * ((a->group + tile_rows - 1) / tile_rows);
   } else if (c.pad > 0) {

@@ -59,8 +59,8 @@ struct CacheAttn {
   const int32_t* list;  // [rows][hkv][count] page numbers of a sequence, or null
   int count;
   void* out;
-  int wide;    // waves along the rows instead of along the keys
-  int splits;  // blocks that share a row tile's keys
+  int tile_rows;  // of a block: 16 or 32, its waves along the keys, or 128, along the rows
+  int splits;     // blocks that share a row tile's keys
   int64_t units;
   int64_t block0;
   float *part_o, *part_ml;
@@ -79,7 +79,7 @@ struct CacheSelect {
 
 hipError_t launch_cache_append(const CacheAppend& a, bool bf16, bool e4m3, hipStream_t s);
 hipError_t launch_cache_read(const CacheRead& a, bool bf16, bool e4m3, hipStream_t s);
-// Fills wide, splits and units for at most max_q queries and max_len tokens a
+// Fills tile_rows, splits and units for at most max_q queries and max_len tokens a
 // sequence; returns the workspace bytes.
 size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_at);
 hipError_t launch_cache_attn(const CacheAttn& a, bool bf16, bool e4m3, hipStream_t s);
