@@ -97,22 +97,10 @@ __device__ inline typename Shape<M>::acc mma_pieces(const bf16x8 (&a)[NA], const
 }
 
 // Eight values of a row as pieces, from global memory.
-__device__ inline void load8(const uint16_t* p, bool in, bf16x8 (&f)[1]) {
-  f[0] = bf16x8{};
-  if (in) f[0] = *reinterpret_cast<const bf16x8*>(p);
-}
-__device__ inline void load8(const float* p, bool in, bf16x8 (&f)[3]) {
-  float x[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-  if (in) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = a[e];
-      x[4 + e] = b[e];
-    }
-  }
+__device__ inline void load8(const uint16_t* p, bf16x8 (&f)[1]) { f[0] = *reinterpret_cast<const bf16x8*>(p); }
+__device__ inline void load8(const float* p, bf16x8 (&f)[3]) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   split(x, f);
 }
 __device__ inline void pieces_of(const uint16_t (&x)[8], bf16x8 (&f)[1]) {
@@ -124,42 +112,39 @@ __device__ inline void pieces_of(const uint16_t (&x)[8], bf16x8 (&f)[1]) {
 }
 __device__ inline void pieces_of(const float (&x)[8], bf16x8 (&f)[3]) { split(x, f); }
 
-constexpr int kPartBlocks = 8;
+constexpr int kKeyWaves = 4;  // of a block whose waves lie along the keys
+constexpr int kPartBlocks = 2 * kKeyWaves;
 
 // Where a row tile stands and which blocks of 32 keys its sequence has for it.
 struct TileAt {
   int s, token0, row0;  // row0: the tile's first row (of the sequence, or of the token's heads where pages are listed)
   int rows, lk, lq;     // rows: of the sequence (of the token)
   int64_t start;
-  int closed, end;      // tokens in full pages, tokens that any row of the tile sees
+  int closed, end;         // tokens in full pages, tokens that any row of the tile sees
   int blocks, per, parts;  // blocks of 32 keys in full pages; per: of a part
 };
 
-// False: no such tile.
-__device__ inline bool tile_at(const CacheAttn& a, int64_t unit, int tile_rows, TileAt& t) {
-  const CacheArgs& c = a.c;
-  int64_t tile;
-  if (a.list) {
-    const int parts = (a.group + tile_rows - 1) / tile_rows;
-    const int64_t u = unit / parts;
-    t.row0 = static_cast<int>(unit - u * parts) * tile_rows;
-    if (c.pad > 0) {
-      if (u >= c.rows) return false;
-      t.s = static_cast<int>(u / c.pad);
-      tile = u - t.s * c.pad;
-    } else {
-      t.s = find_seq(c.off, c.seqs, 1, 1, u, tile);
-    }
-  } else if (c.pad > 0) {
-    const int64_t per = (c.pad * a.group + tile_rows - 1) / tile_rows;
-    t.s = static_cast<int>(unit / per);
-    tile = unit - t.s * per;
-    if (t.s >= c.seqs) return false;
-  } else {
-    t.s = find_seq(c.off, c.seqs, a.group, tile_rows, unit, tile);
+// find_seq for tiles of 1 << log rows.
+__device__ inline int find_tile(const int64_t* __restrict__ off, int seqs, int group, int log, uint32_t b, int64_t& tile) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = static_cast<int>(static_cast<uint32_t>(n + kWave - 1) / kWave);
+    const int s = lane * step;
+    const bool below = s < n && (max(off[lo + s], int64_t(0)) * group >> log) + (lo + s) <= static_cast<int64_t>(b);
+    const int c = max(1, static_cast<int>(__popcll(__ballot(below))));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
   }
-  if (tile < 0) return false;
-  const SeqSpan q = seq_span(c.off, t.s, c.pad, c.rows);
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  tile = static_cast<int64_t>(b) - ((max(off[lo], int64_t(0)) * group >> log) + lo);
+  return lo;
+}
+
+// A tile of sequence t.s: number `tile` of its tiles of 1 << log rows, or where
+// pages are listed rows t.row0 on of its token `tile`. False: no such tile.
+__device__ inline bool tile_of(const CacheAttn& a, const SeqSpan& q, int64_t tile, int log, TileAt& t) {
+  const CacheArgs& c = a.c;
   t.start = q.start;
   t.lq = q.len;
   t.lk = cache_len(c, t.s);
@@ -170,22 +155,48 @@ __device__ inline bool tile_at(const CacheAttn& a, int64_t unit, int tile_rows, 
     t.token0 = last = static_cast<int>(tile);
     t.rows = tile < q.len ? a.group : 0;
   } else {
-    const int64_t r0 = tile * tile_rows, all = c.pad > 0 ? c.pad * a.group : static_cast<int64_t>(q.len) * a.group;
+    const int64_t r0 = tile << log, all = (c.pad > 0 ? c.pad : int64_t(q.len)) * a.group;
     if (r0 >= all) return false;
     t.row0 = static_cast<int>(r0);
     t.token0 = 0;
     t.rows = q.len * a.group;
-    last = t.row0 < t.rows ? div_group(min(t.row0 + tile_rows, t.rows) - 1, a.group) : -1;
+    last = t.row0 < t.rows ? div_group(min(t.row0 + (1 << log), t.rows) - 1, a.group) : -1;
   }
   t.end = last < 0 || t.rows == 0 ? 0 : a.causal ? max(0, min(t.lk, last + t.lk - t.lq + 1)) : t.lk;
   if (t.end == 0) t.blocks = 0;
   else if (a.list) t.blocks = a.count << (c.plog - 5);
   else t.blocks = (min(t.end, t.closed) + kCacheBlock - 1) / kCacheBlock;
-  // at least eight blocks to a part: fewer are not worth its way through memory
-  const int share = (t.blocks + a.splits - 1) / a.splits;
+  // a part is at least two steps of every wave: fewer are not worth its way through memory
+  const int share = static_cast<int>(static_cast<uint32_t>(t.blocks + a.splits - 1) / static_cast<uint32_t>(a.splits));
   t.per = max(kPartBlocks, (share + kPartBlocks - 1) / kPartBlocks * kPartBlocks);
-  t.parts = max(1, (t.blocks + t.per - 1) / t.per);
+  t.parts = max(1, static_cast<int>(static_cast<uint32_t>(t.blocks + t.per - 1) / static_cast<uint32_t>(t.per)));
   return true;
+}
+
+// Tile number `unit` of all. Fewer than 2^31 of them.
+__device__ inline bool tile_at(const CacheAttn& a, uint32_t unit, int log, TileAt& t) {
+  const CacheArgs& c = a.c;
+  int64_t tile;
+  const int tile_rows = 1 << log;
+  if (a.list) {
+    const uint32_t tiles = static_cast<uint32_t>(a.group + tile_rows - 1) >> log;
+    const uint32_t u = tiles == 1 ? unit : unit / tiles;
+    t.row0 = static_cast<int>(unit - u * tiles) << log;
+    if (c.pad > 0) {
+      t.s = static_cast<int>(u / static_cast<uint32_t>(c.pad));
+      tile = u - static_cast<uint32_t>(t.s) * static_cast<uint32_t>(c.pad);
+    } else {
+      t.s = find_tile(c.off, c.seqs, 1, 0, u, tile);
+    }
+  } else if (c.pad > 0) {
+    const uint32_t tiles = static_cast<uint32_t>(c.pad * a.group + tile_rows - 1) >> log;
+    t.s = static_cast<int>(unit / tiles);
+    tile = unit - static_cast<uint32_t>(t.s) * tiles;
+  } else {
+    t.s = find_tile(c.off, c.seqs, a.group, log, unit, tile);
+  }
+  if (tile < 0 || t.s >= c.seqs) return false;
+  return tile_of(a, seq_span(c.off, t.s, c.pad, c.rows), tile, log, t);
 }
 
 // A lane's output columns and its row's running maximum, the height above it at
@@ -196,38 +207,52 @@ struct AttnState {
   float m, move, l;
 };
 
+template <typename T>
+__device__ inline void capped_scores(float (&x)[16], float scale) {
+  tanh_scores<T>(x, scale);
+}
+template <typename T>
+__device__ inline void capped_scores(float (&x)[8], float scale) {
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = x[i & 7];  // the second eight fall away as the same
+  tanh_scores<T>(y, scale);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = y[i];
+}
+
 struct RowParams {
   int limit, pos, least;  // keys the row sees; least: of the wave's rows
   float slope, scale, cap;
 };
 
-// The lane's 16 keys from position j on into the softmax: p comes as the products
+// The lane's NS keys from position j on into the softmax: p comes as the products
 // of the codes and leaves as probabilities times vs. masked: some lane's row may
 // not see some key of the step.
-template <typename T, int M, int HD>
-__device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[16], const RowParams& r, bool capped, bool sloped,
+template <typename T, int M, int HD, int NS>
+__device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[NS], const RowParams& r, bool capped, bool sloped,
                                        float ks, float vs, int j, bool masked) {
   float c = r.scale * kLog2e * ks;
   if (capped) {
     c = r.cap * kLog2e;
-    tanh_scores<T>(p, r.scale / r.cap * ks);
+    capped_scores<T>(p, r.scale / r.cap * ks);
   }
   if (!sloped) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = p[i] * c - st.m;
+    for (int i = 0; i < NS; ++i) p[i] = p[i] * c - st.m;
   } else {
     const float dist = static_cast<float>(j - r.pos);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = p[i] * c - (r.slope * fabsf(dist + static_cast<float>(i)) + st.m);
+    for (int i = 0; i < NS; ++i) p[i] = p[i] * c - (r.slope * fabsf(dist + static_cast<float>(i)) + st.m);
   }
   if (masked) {
     const int left = r.limit - j;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = i < left ? p[i] : -INFINITY;
+    for (int i = 0; i < NS; ++i) p[i] = i < left ? p[i] : -INFINITY;
   }
   float top = p[0];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+  for (int i = 1; i < NS; ++i) top = fmaxf(top, p[i]);
   top = Shape<M>::column_max(top);
   // the running maximum moves only when a score passes it by 2^8
   if (__any(top > st.move)) {
@@ -240,11 +265,11 @@ __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[16], con
 #pragma unroll
     for (int i = 0; i < HD / M; ++i) st.acc[i] *= alpha;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] -= by;
+    for (int i = 0; i < NS; ++i) p[i] -= by;
   }
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < NS; ++i) {
     p[i] = exp2_hw(p[i]);
     sum += p[i];
     p[i] *= vs;
@@ -254,45 +279,50 @@ __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[16], con
 
 // Waves of a SIMD that the registers are kept down for.
 template <typename T, int HD, int M>
-constexpr int kResident = HD <= 32 ? 3 : HD <= 64 && (M == 16 || sizeof(T) == 2) ? 3 : HD * sizeof(T) <= 256 || M == 16 ? 2 : 1;
+constexpr int kResident = M == 16 ? (sizeof(T) == 4 ? (HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 3) : HD <= 64 ? (sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? 2 : 1;
 
-// Tiles of WR M rows: WR waves along the rows, WK along the keys, each taking steps
-// of 1024 / M keys.
+__device__ inline float lane_value(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+
+// Tiles of WR M rows: WR waves along the rows, WK along the keys, each taking 32
+// keys at a time.
 template <typename T, bool E4M3, int HD, int M, int WR, int WK>
 __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_attn(const CacheAttn a) {
   typedef Shape<M> S;
-  constexpr int G = kWave / M;                       // lane groups
-  constexpr int B = 16 * G / kCacheBlock;            // blocks of a step
-  constexpr int KT = 16 * G / M;                     // key tiles of a step
+  constexpr int G = kWave / M;                         // lane groups
+  constexpr int NS = kCacheBlock / G;                  // keys of a group: consecutive ones
+  constexpr int KT = kCacheBlock / M;                  // key tiles of a step
   constexpr int KC = HD < 16 * G ? 1 : HD / (16 * G);  // 16-column chunks of a key per lane
-  constexpr int DT = HD / M, NP = Pieces<T>::N, kRows = M * WR;
+  constexpr int DT = HD / M, NU = NS / 8, NP = Pieces<T>::N, kRows = M * WR;
+  typedef uint32_t codes_t __attribute__((ext_vector_type(NS / 4)));
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wr = wave % WR, wk = wave / WR, grp = lane / M, col = lane % M;
-  const int64_t b = a.block0 + blockIdx.x;
-  const int part = static_cast<int>(b % a.splits);
-  const int kvh = static_cast<int>(b / a.splits % c.hkv);
-  const int64_t unit = b / a.splits / c.hkv;
+  const uint32_t unit = a.unit0 + blockIdx.x;
+  const int kvh = blockIdx.y, part = blockIdx.z;
   TileAt t;
-  if (!tile_at(a, unit, kRows, t) || part >= t.parts) return;  // block-uniform
+  if (!tile_at(a, unit, kRows == 16 ? 4 : kRows == 32 ? 5 : 7, t) || part >= t.parts) return;  // block-uniform
   const int b0 = part * t.per, b1 = min(b0 + t.per, t.blocks);
   const bool joined = t.parts > 1;
 
   const int r = t.row0 + wr * M + col;
   const bool live = r < t.rows;
+  // rows that are not there stand for the last: what they get is not written
+  const int r_in = live ? r : max(t.rows - 1, 0);
   RowOf me;
   if (a.list) {
     me.token = t.token0;
-    me.head = kvh * a.group + r;
+    me.head = kvh * a.group + r_in;
   } else {
-    me = row_of(r, kvh, a.group);
+    me = row_of(r_in, kvh, a.group);
   }
   RowParams rp;
-  rp.limit = !live ? 0 : a.causal ? max(0, min(t.lk, me.token + t.lk - t.lq + 1)) : t.lk;
+  rp.limit = a.causal ? max(0, min(t.lk, me.token + t.lk - t.lq + 1)) : t.lk;
   rp.pos = me.token + t.lk - t.lq;
   // keys that every row of the wave sees: limits do not fall along the rows
   const int least = __builtin_amdgcn_readfirstlane(rp.limit);
-  rp.slope = a.slopes && live ? a.slopes[me.head] * kLog2e : 0.0f;
+  rp.slope = a.slopes ? a.slopes[me.head] * kLog2e : 0.0f;
   rp.scale = a.scale;
   rp.cap = a.cap;
   const bool capped = a.cap > 0.0f, sloped = a.slopes != nullptr;
@@ -303,7 +333,13 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
 #pragma unroll
     for (int i = 0; i < 2 * KC; ++i) {
       const int d0 = i / 2 * 16 * G + grp * 16 + (i & 1) * 8;
-      load8(q + d0, live && d0 < c.d, qf[i]);
+      const bool in = d0 < c.d && t.rows > 0;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) qf[i][n] = bf16x8{};
+      if (t.rows > 0) load8(q + (in ? d0 : 0), qf[i]);
+      if (!in)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) qf[i][n] = bf16x8{};
     }
   }
   AttnState<M, HD> st;
@@ -313,69 +349,62 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   st.move = -INFINITY;
   st.l = 0.0f;
 
-  // the lane's row of a key tile, so that scores 0 .. 15 of group g are keys 16 g ..
-  auto key_of = [&](int tile) { return M == 32 ? ((col >> 2) & 1) * 16 + (col >> 3) * 4 + (col & 3) : (col >> 2) * 16 + tile * 4 + (col & 3); };
+  // the lane's row of a key tile, so that a lane's results are keys NS grp + 0 ..
+  auto key_of = [&](int tile) {
+    return M == 32 ? ((col >> 2) & 1) * 16 + (col >> 3) * 4 + (col & 3) : (col >> 2) * 8 + tile * 4 + (col & 3);
+  };
   const int64_t page_bytes = static_cast<int64_t>(HD) << c.plog;
   const int sub_mask = (1 << (c.plog - 5)) - 1;
 
-  // the wave's steps: n blocks from b0 + wk B on, every WK B
-  int pages = -1, firsts = 0;  // of the next blocks, one per lane: page and first token
-  auto look = [&](int n) {
-    const int64_t mine = n + static_cast<int64_t>(lane / B) * (WK * B) + lane % B;
+  // of the wave's next 64 blocks, one per lane: page, first token and scales (a
+  // load of a step's scales in the step would make it wait for the next keys too)
+  int pages = -1, firsts = 0;
+  float2 scales = make_float2(0.0f, 0.0f);
+  const int part_blocks = b1 - b0;
+  auto look = [&](int s) {
+    const int64_t step = s + static_cast<int64_t>(lane) * WK;
     int num = -1;
     firsts = 0;
-    if (mine < b1) {
-      const int at = static_cast<int>(mine) >> (c.plog - 5);
+    if (step < part_blocks) {
+      const int mine = b0 + static_cast<int>(step), at = mine >> (c.plog - 5);
       num = a.list ? a.list[((t.start + t.token0) * c.hkv + kvh) * a.count + at] : at;
       if (num >= t.closed >> c.plog) num = -1;
-      firsts = (num << c.plog) + ((static_cast<int>(mine) & sub_mask) << 5);
+      firsts = (num << c.plog) + ((mine & sub_mask) << 5);
     }
     pages = cache_page(c, t.s, num);
+    if (pages >= 0) scales = reinterpret_cast<const float2*>(c.scales)[static_cast<int64_t>(pages) * c.hkv + kvh];
   };
-  // block i of the step at place j (0 .. 64 / B - 1) of those looked up
-  auto page_at = [&](int j, int i) { return B == 1 ? __builtin_amdgcn_readlane(pages, j) : __shfl(pages, j * B + i, kWave); };
-  auto first_at = [&](int j, int i) { return B == 1 ? __builtin_amdgcn_readlane(firsts, j) : __shfl(firsts, j * B + i, kWave); };
 
-  u32x4 kc[KT][KC], vc[DT];
+  u32x4 kc[KT][KC];
+  codes_t vc[DT];
   float2 scale = make_float2(0.0f, 0.0f);
+  // a page that is not there stands as page 0, and its step is left out
   auto load_keys = [&](int j) {
-    const int i = B == 1 ? 0 : col >> 3;  // the lane's keys lie in one block
-    const int page = page_at(j, i), sub = (first_at(j, i) >> 5) & sub_mask;
+    const int page = max(__builtin_amdgcn_readlane(pages, j), 0), sub = (__builtin_amdgcn_readlane(firsts, j) >> 5) & sub_mask;
     const uint8_t* p = c.data + (static_cast<int64_t>(page) * c.hkv + kvh) * 2 * page_bytes;
 #pragma unroll
     for (int x = 0; x < KT; ++x)
 #pragma unroll
       for (int y = 0; y < KC; ++y) {
-        const int chunk = y * G + grp;
-        kc[x][y] = u32x4{0, 0, 0, 0};
-        if (page >= 0 && (HD >= 16 * G || chunk < HD / 16))
-          kc[x][y] = *reinterpret_cast<const u32x4*>(p + (((chunk << c.plog) + sub * kCacheBlock + (key_of(x) & 31)) << 4));
+        const uint32_t chunk = HD >= 16 * G ? y * G + grp : min(grp, HD / 16 - 1);  // past the head: q is 0 there
+        const uint32_t at = ((chunk << c.plog) + sub * kCacheBlock + key_of(x)) << 4;
+        kc[x][y] = *reinterpret_cast<const u32x4*>(p + at);
       }
   };
-  auto load_values = [&](int j) -> int {  // the lane's first key, or -1
-    const int i = B == 1 ? 0 : grp >> 1;
-    const int page = page_at(j, i), first = first_at(j, i), sub = (first >> 5) & sub_mask;
-    const int64_t at = static_cast<int64_t>(page) * c.hkv + kvh;
+  auto load_values = [&](int j) -> int {  // the step's first key, or -1
+    const int page = __builtin_amdgcn_readlane(pages, j), first = __builtin_amdgcn_readlane(firsts, j);
+    const int64_t at = static_cast<int64_t>(max(page, 0)) * c.hkv + kvh;
     const uint8_t* p = c.data + (at * 2 + 1) * page_bytes;
-    scale = make_float2(0.0f, 0.0f);
-    if (page >= 0) scale = reinterpret_cast<const float2*>(c.scales)[at];
+    const uint32_t chunk = ((first >> 5) & sub_mask) * 2 + NS * grp / 16;
+    scale = make_float2(lane_value(scales.x, j), lane_value(scales.y, j));
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
-      vc[x] = u32x4{0, 0, 0, 0};
-      if (page >= 0) vc[x] = *reinterpret_cast<const u32x4*>(p + (((sub * 2 + (grp & 1)) * HD + x * M + col) << 4));
+      const uint32_t to = ((chunk * HD + x * M + col) << 4) + NS * grp % 16;
+      vc[x] = *reinterpret_cast<const codes_t*>(p + to);
     }
-    return page >= 0 ? first + (grp & 1) * 16 : -1;
+    return page >= 0 ? first : -1;
   };
-
-  const int stride = WK * B;
-  int n = b0 + wk * B, j = 0;
-  if (n < b1) {
-    look(n);
-    load_keys(0);
-  }
-  for (; n < b1; n += stride) {
-    const int key0 = load_values(j);
-    float p[16];
+  auto scores_coded = [&](float (&p)[NS]) {
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
       typename S::acc sc = {};
@@ -387,77 +416,123 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
           sc = mma_pieces<M>(kf, qf[2 * y + u], sc);
         }
 #pragma unroll
-      for (int i = 0; i < 16 / KT; ++i) p[x * (16 / KT) + i] = sc[i];
+      for (int i = 0; i < NS / KT; ++i) p[x * (NS / KT) + i] = sc[i];
     }
-    // the next keys into the same registers, under the softmax and the second product
-    if (n + stride < b1) {
-      j = j + 1 == kWave / B ? 0 : j + 1;
-      if (j == 0) look(n + stride);
-      load_keys(j);
-    }
-    RowParams now = rp;
-    now.limit = key0 < 0 ? INT32_MIN / 2 : rp.limit;  // a page that is not there
-    const bool masked = !__all(key0 >= 0 && key0 + 16 <= least);
-    soften<T>(st, p, now, capped, sloped, scale.x, scale.y, key0, masked);
+  };
+  auto output_coded = [&](const bf16x8 (&pf)[NU][NP]) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
-      bf16x8 pf[NP];
-      split(y, pf);
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int x = 0; x < DT; ++x) {
         const bf16x8 vf[1] = {codes8<E4M3>(vc[x][2 * u], vc[x][2 * u + 1])};
-        st.acc[x] = mma_pieces<M>(vf, pf, st.acc[x]);
+        st.acc[x] = mma_pieces<M>(vf, pf[u], st.acc[x]);
+        if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // no operands are made ahead
       }
+  };
+
+  // the wave's steps: every WK-th, those of full pages first, then with the last
+  // part those of the open page
+  const int slot = cache_slot(c, t.s), held = t.lk - t.closed;
+  const int most = part == t.parts - 1 && slot >= 0 ? t.end - t.closed : 0;
+  const int full_steps = c.pages > 0 ? part_blocks : 0;
+  const int steps = full_steps + (most > 0 ? (most + kCacheBlock - 1) / kCacheBlock : 0);
+  const T* open = static_cast<const T*>(c.open) + (most > 0 ? open_at(c, slot, t.closed >> c.plog, kvh, 0) : 0);
+  // tokens past the page's last stand for it and columns past the head for the
+  // first: their scores are masked, their products with q are with 0
+  auto scores_open = [&](float (&p)[NS], int k0) {
+    int last = held - 1;
+    asm volatile("" : "+s"(last));  // or the addresses are made ahead of the loop and kept
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const uint32_t row = min(k0 + key_of(x), last) * c.d;
+      typename S::acc sc = {};
+#pragma unroll
+      for (int y = 0; y < 2 * KC; ++y) {
+        const int d0 = y / 2 * 16 * G + grp * 16 + (y & 1) * 8;
+        bf16x8 kf[NP];
+        load8(open + (row + (d0 < c.d ? d0 : 0)), kf);
+        sc = mma_pieces<M>(kf, qf[y], sc);
+      }
+#pragma unroll
+      for (int i = 0; i < NS / KT; ++i) p[x * (NS / KT) + i] = sc[i];
     }
-  }
-  // the open page, with the last part
-  const int slot = cache_slot(c, t.s), held = t.lk - t.closed, most = t.end - t.closed;
-  if (part == t.parts - 1 && slot >= 0) {
-    const T* kp = static_cast<const T*>(c.open) + open_at(c, slot, t.closed >> c.plog, kvh, 0);
-    const T* vp = kp + (static_cast<int64_t>(c.d) << c.plog);
-    for (int k0 = wk * 16 * G; k0 < most; k0 += WK * 16 * G) {
-      float p[16];
+  };
+  auto output_open = [&](const bf16x8 (&pf)[NU][NP], int k0) {
+    int last = held - 1;
+    asm volatile("" : "+s"(last));
+    const char* v = reinterpret_cast<const char*>(open + (static_cast<int64_t>(c.d) << c.plog));
 #pragma unroll
-      for (int x = 0; x < KT; ++x) {
-        const int k = k0 + key_of(x);
-        typename S::acc sc = {};
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int y = 0; y < 2 * KC; ++y) {
-          const int d0 = y / 2 * 16 * G + grp * 16 + (y & 1) * 8;
-          bf16x8 kf[NP];
-          load8(kp + k * c.d + d0, k < held && d0 < c.d, kf);
-          sc = mma_pieces<M>(kf, qf[y], sc);
+      for (int x = 0; x < DT; ++x) {
+        T z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t at = min(k0 + grp * NS + u * 8 + e, last) * c.d + min(x * M + col, c.d - 1);
+          z[e] = *reinterpret_cast<const T*>(v + at * static_cast<uint32_t>(sizeof(T)));
         }
-#pragma unroll
-        for (int i = 0; i < 16 / KT; ++i) p[x * (16 / KT) + i] = sc[i];
+        bf16x8 vf[NP];
+        pieces_of(z, vf);
+        st.acc[x] = mma_pieces<M>(vf, pf[u], st.acc[x]);
+        if (x % (M / 8) == M / 8 - 1) __builtin_amdgcn_sched_barrier(0);  // not all loads at once: they spill
       }
-      soften<T>(st, p, rp, capped, sloped, 1.0f, 1.0f, t.closed + k0 + grp * 16, true);
+  };
+  auto pieces = [&](const float (&p)[NS], bf16x8 (&pf)[NU][NP]) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float y[8];
+    for (int u = 0; u < NU; ++u) {
+      float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
-        bf16x8 pf[NP];
-        split(y, pf);
-#pragma unroll
-        for (int x = 0; x < DT; ++x) {
-          T z[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int k = k0 + grp * 16 + u * 8 + e;
-            z[e] = T(0);
-            if (k < held && x * M + col < c.d) z[e] = vp[k * c.d + x * M + col];
-          }
-          bf16x8 vf[NP];
-          pieces_of(z, vf);
-          st.acc[x] = mma_pieces<M>(vf, pf, st.acc[x]);
-        }
-      }
+      for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
+      split(y, pf[u]);
     }
+  };
+
+  int j = 0;
+  if (wk < full_steps) {
+    look(wk);
+    load_keys(0);
   }
+  // Few rows: a block lives for a few steps, and what it fetches of the kernel's
+  // code counts as much as its data (the open page in a loop of its own: token of
+  // 256 users 77 us, so 67), so both kinds of steps share one softmax.
+  constexpr bool kShared = M == 16;
+  int s = wk;
+  for (; s < (kShared ? steps : full_steps); s += WK) {
+    const bool coded = !kShared || s < full_steps;  // wave-uniform
+    const int k0 = (s - full_steps) * kCacheBlock;
+    int key0 = t.closed + k0;
+    float p[NS];
+    if (coded) {
+      key0 = load_values(j);
+      scores_coded(p);
+      // the next keys into the same registers, under the softmax and the second product
+      if (s + WK < full_steps) {
+        j = j + 1 == kWave ? 0 : j + 1;
+        if (j == 0) look(s + WK);
+        load_keys(j);
+      }
+      if (key0 < 0) continue;  // a page that is not there
+    } else {
+      scale = make_float2(1.0f, 1.0f);
+      scores_open(p, k0);
+    }
+    const bool masked = !coded || key0 + kCacheBlock > least;
+    soften<T>(st, p, rp, capped, sloped, scale.x, scale.y, key0 + grp * NS, masked);
+    bf16x8 pf[NU][NP];
+    pieces(p, pf);
+    if (coded) output_coded(pf);
+    else output_open(pf, k0);
+  }
+  if (!kShared)
+    for (; s < steps; s += WK) {
+      const int k0 = (s - full_steps) * kCacheBlock;
+      float p[NS];
+      scores_open(p, k0);
+      soften<T>(st, p, rp, capped, sloped, 1.0f, 1.0f, t.closed + k0 + grp * NS, true);
+      bf16x8 pf[NU][NP];
+      pieces(p, pf);
+      output_open(pf, k0);
+    }
 
   st.l = S::column_sum(st.l);
   float m = st.m, l = st.l;
@@ -511,7 +586,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   const int64_t out_rows = a.list ? a.group : c.pad > 0 ? c.pad * a.group : static_cast<int64_t>(t.rows);
   if (r >= out_rows || (!live && part > 0)) return;
   if (joined && live) {
-    const int64_t at = ((unit * c.hkv + kvh) * a.splits + part) * kRows + wr * M + col;
+    const int64_t at = ((static_cast<int64_t>(unit) * c.hkv + kvh) * a.splits + part) * kRows + wr * M + col;
     float* po = a.part_o + at * c.d;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -525,7 +600,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   }
   const bool none = !live || l == 0.0f;  // no key: 0 (a NaN sum stays)
   const float inv = none ? 0.0f : 1.0f / l;
-  T* out = static_cast<T*>(a.out) + ((t.start + me.token) * a.hq + me.head) * c.d;
+  const RowOf to = a.list ? RowOf{t.token0, kvh * a.group + r} : row_of(r, kvh, a.group);
+  T* out = static_cast<T*>(a.out) + ((t.start + to.token) * a.hq + to.head) * c.d;
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -539,64 +615,75 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
     }
 }
 
-// Joins the splits of a row: a block per query token and head, threads four
-// columns and a share of the splits each.
+// Joins the parts of a row: NT threads a query token and head, each four columns
+// and a share of the parts. Bound by the latency of its loads, one after another:
+// the sequence, its length, then maxima, sums and parts together.
 //   m = max m_c,  l = sum l_c 2^(m_c - m),  out = sum acc_c 2^(m_c - m) / l
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_rows, int64_t block0) {
-  __shared__ float4 sh_o[NT];
-  __shared__ float sh_l[NT], sh_m[NT / kWave];
+__global__ __launch_bounds__(NT < kBlock ? kBlock : NT) void k_cache_join(const CacheAttn a) {
+  constexpr int kThreads = NT < kBlock ? kBlock : NT, kRows = kThreads / NT;  // rows: heads of one token
+  __shared__ float4 sh_o[kThreads];
+  __shared__ float sh_l[kThreads], sh_m[kThreads / kWave];
   const CacheArgs& c = a.c;
-  const int64_t b = block0 + blockIdx.x;
-  const int head = static_cast<int>(b % a.hq), kvh = head / a.group;
-  const int64_t u = b / a.hq;
-  int s;
+  const int th = threadIdx.x % NT, row = threadIdx.x / NT;
+  const uint32_t u = a.unit0 + blockIdx.x;
+  TileAt t;
   int64_t token;
   if (c.pad > 0) {
-    s = static_cast<int>(u / c.pad);
-    token = u - s * c.pad;
+    t.s = static_cast<int>(u / static_cast<uint32_t>(c.pad));
+    token = u - static_cast<uint32_t>(t.s) * static_cast<uint32_t>(c.pad);
   } else {
-    s = find_seq(c.off, c.seqs, 1, 1, u, token);
+    t.s = find_tile(c.off, c.seqs, 1, 0, u, token);
   }
-  const SeqSpan q = seq_span(c.off, s, c.pad, c.rows);
-  if (token < 0 || token >= q.len) return;  // rows past a padded sequence's end are written
-  int64_t unit;
+  const SeqSpan q = seq_span(c.off, t.s, c.pad, c.rows);
+  if (token < 0 || token >= q.len) return;  // block-uniform; rows past a padded sequence's end are written
+  const int head = min(static_cast<int>(blockIdx.y) * kRows + row, a.hq - 1);
+  const bool twice = static_cast<int>(blockIdx.y) * kRows + row >= a.hq;
+  const int kvh = static_cast<int>(static_cast<uint32_t>(head) / static_cast<uint32_t>(a.group));
+  const int log = a.tile_log, tile_rows = 1 << log;
+  uint32_t unit;
+  int64_t tile;
   int at;
   if (a.list) {
-    const int tiles = (a.group + tile_rows - 1) / tile_rows, r = head - kvh * a.group;
-    unit = u * tiles + r / tile_rows;
-    at = r % tile_rows;
+    const int r = head - kvh * a.group;
+    unit = u * (static_cast<uint32_t>(a.group + tile_rows - 1) >> log) + (static_cast<uint32_t>(r) >> log);
+    at = r & (tile_rows - 1);
+    t.row0 = r - at;
+    tile = token;
   } else {
-    const int64_t r = token * a.group + head - kvh * a.group;
-    const int64_t first = c.pad > 0 ? s * ((c.pad * a.group + tile_rows - 1) / tile_rows)
-                                    : tile_base(c.off, s, a.group, tile_rows);
-    unit = first + r / tile_rows;
-    at = static_cast<int>(r % tile_rows);
+    const int r = static_cast<int>(token) * a.group + head - kvh * a.group;
+    const uint32_t first = c.pad > 0 ? static_cast<uint32_t>(t.s) * (static_cast<uint32_t>(c.pad * a.group + tile_rows - 1) >> log)
+                                     : static_cast<uint32_t>(max(c.off[t.s], int64_t(0)) * a.group >> log) + t.s;
+    tile = static_cast<uint32_t>(r) >> log;
+    unit = first + static_cast<uint32_t>(tile);
+    at = r & (tile_rows - 1);
   }
-  TileAt t;
-  if (!tile_at(a, unit, tile_rows, t) || t.parts == 1) return;  // written
-  const int parts = t.parts;
-  const int64_t slot0 = (unit * c.hkv + kvh) * a.splits * tile_rows + at;
+  tile_of(a, q, tile, log, t);
+  const int parts = t.parts;  // 1: written. A group's heads may lie in two tiles of other ends
+  const int64_t slot0 = (static_cast<int64_t>(unit) * c.hkv + kvh) * a.splits * tile_rows + at;
 
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   float m = -INFINITY;
-  for (int i = threadIdx.x; i < parts; i += NT) {
-    const float2 x = ml[slot0 + static_cast<int64_t>(i) * tile_rows];
-    m = fmaxf(m, x.y == 0.0f ? -INFINITY : x.x);
-  }
+  if (parts > 1)
+    for (int i = th; i < parts; i += NT) {
+      const float2 x = ml[slot0 + static_cast<int64_t>(i) * tile_rows];
+      m = fmaxf(m, x.y == 0.0f ? -INFINITY : x.x);
+    }
 #pragma unroll
   for (int i = kWave / 2; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i, kWave));
-  if ((threadIdx.x & (kWave - 1)) == 0) sh_m[threadIdx.x / kWave] = m;
-  __syncthreads();
+  if constexpr (NT > kWave) {
+    if ((threadIdx.x & (kWave - 1)) == 0) sh_m[threadIdx.x / kWave] = m;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < NT / kWave; ++w) m = fmaxf(m, sh_m[w]);
+    for (int w = 0; w < NT / kWave; ++w) m = fmaxf(m, sh_m[w]);
+  }
   const float base = m == -INFINITY ? 0.0f : m;
 
-  const int quads = c.d / 4;  // at most 32
-  const int shares = NT / quads, quad = threadIdx.x % quads, share = threadIdx.x / quads;
+  const uint32_t quads = c.d / 4;  // at most 32
+  const int shares = NT / quads, quad = th % quads, share = th / quads;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float l = 0.0f;
-  if (share < shares) {
+  if (share < shares && parts > 1) {
 #pragma unroll 4
     for (int i = share; i < parts; i += shares) {
       const int64_t slot = slot0 + static_cast<int64_t>(i) * tile_rows;
@@ -613,10 +700,11 @@ __global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_r
   sh_o[threadIdx.x] = o;
   sh_l[threadIdx.x] = l;
   __syncthreads();
-  if (share > 0) return;
+  if (share > 0 || parts == 1 || twice) return;
   for (int k = 1; k < shares; ++k) {
-    const float4 y = sh_o[k * quads + quad];
-    l += sh_l[k * quads + quad];
+    const int from = row * NT + k * static_cast<int>(quads) + quad;
+    const float4 y = sh_o[from];
+    l += sh_l[from];
     o.x += y.x;
     o.y += y.y;
     o.z += y.z;
@@ -628,25 +716,24 @@ __global__ __launch_bounds__(NT) void k_cache_join(const CacheAttn a, int tile_r
          none ? 0.0f : o.y * inv, none ? 0.0f : o.z * inv, none ? 0.0f : o.w * inv);
 }
 
-constexpr int64_t kMostBlocks = int64_t(1) << 21;
+// Fewer than 2^32 threads along an axis of a launch.
+constexpr int64_t kMostUnits = int64_t(1) << 21;
 
 template <typename T, bool E4M3, int HD>
 hipError_t run(CacheAttn a, hipStream_t s) {
-  const int64_t blocks = a.units * a.c.hkv * a.splits;
-  for (int64_t b = 0; b < blocks; b += kMostBlocks) {
-    a.block0 = b;
-    const unsigned now = static_cast<unsigned>(std::min(blocks - b, kMostBlocks));
-    if (a.tile_rows == 16) k_cache_attn<T, E4M3, HD, 16, 1, 4><<<now, 4 * kWave, 0, s>>>(a);
-    else if (a.tile_rows == 32) k_cache_attn<T, E4M3, HD, 32, 1, 4><<<now, 4 * kWave, 0, s>>>(a);
-    else k_cache_attn<T, E4M3, HD, 32, 4, 1><<<now, 4 * kWave, 0, s>>>(a);
+  for (int64_t u = 0; u < a.units; u += kMostUnits) {
+    a.unit0 = static_cast<uint32_t>(u);
+    const dim3 grid(static_cast<unsigned>(std::min(a.units - u, kMostUnits)), a.c.hkv, a.splits);
+    if (a.tile_log == 4) k_cache_attn<T, E4M3, HD, 16, 1, kKeyWaves><<<grid, kKeyWaves * kWave, 0, s>>>(a);
+    else if (a.tile_log == 5) k_cache_attn<T, E4M3, HD, 32, 1, kKeyWaves><<<grid, kKeyWaves * kWave, 0, s>>>(a);
+    else k_cache_attn<T, E4M3, HD, 32, 4, 1><<<grid, 4 * kWave, 0, s>>>(a);
   }
-  if (a.splits > 1) {
-    const int64_t rows = (a.c.pad > 0 ? a.c.rows : a.c.rows + a.c.seqs) * a.hq;
-    for (int64_t b = 0; b < rows; b += kMostBlocks) {
-      const unsigned now = static_cast<unsigned>(std::min(rows - b, kMostBlocks));
-      if (a.splits > 32) k_cache_join<T, 1024><<<now, 1024, 0, s>>>(a, a.tile_rows, b);
-      else k_cache_join<T, 128><<<now, 128, 0, s>>>(a, a.tile_rows, b);
-    }
+  const int64_t tokens = a.splits > 1 ? (a.c.pad > 0 ? a.c.rows : a.c.rows + a.c.seqs) : 0;
+  for (int64_t u = 0; u < tokens; u += kMostUnits) {
+    a.unit0 = static_cast<uint32_t>(u);
+    const unsigned n = static_cast<unsigned>(std::min(tokens - u, kMostUnits));
+    if (a.splits > 32) k_cache_join<T, 1024><<<dim3(n, a.hq), 1024, 0, s>>>(a);
+    else k_cache_join<T, kWave><<<dim3(n, (a.hq + 3) / 4), kBlock, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -660,8 +747,16 @@ hipError_t run_width(const CacheAttn& a, hipStream_t s) {
 
 }  // namespace
 
-constexpr int64_t kSplitBlocks = 1024;
-constexpr int64_t kLeastChunk = 256;
+// Blocks that a call's keys are split into: two rounds of what the chip holds at 128
+// columns, so that a long sequence's parts spread (one token of 256 users with 1 to
+// 4096 keys: 67 us with 512, 66 with 1024, 59 with 1536, 61 with 2304), but for few
+// row tiles, whose many parts the join has to read, two blocks a CU (four rows over
+// 1,000,003 keys of 64: 53 with 512, 60 with 1024, 62 with 1536).
+constexpr int64_t kSplitBlocks = 1536, kFewTileBlocks = 512, kFewTiles = 64;
+// Tiles of 128 rows: two rounds of two blocks a CU, each more parts to join (chunks of
+// 33 to 257 queries over 2000 to 8191 keys: 91 us with 512, 90 with 1024, 93 with 1536).
+constexpr int64_t kWideBlocks = 1024;
+constexpr int64_t kLeastChunk = 32 * kPartBlocks;
 constexpr size_t kMostPartBytes = size_t(256) << 20;
 
 size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_at) {
@@ -673,7 +768,8 @@ size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_
   int64_t most_q = c.pad > 0 ? c.pad : c.rows;
   if (c.pad == 0 && max_q > 0) most_q = std::min(most_q, max_q);
   const int64_t most_rows = a->list ? a->group : most_q * a->group;
-  const int tile_rows = a->tile_rows = most_rows <= 16 ? 16 : most_rows <= 32 || a->list ? 32 : 128;
+  a->tile_log = most_rows <= 16 ? 4 : most_rows <= 32 || a->list ? 5 : 7;
+  const int tile_rows = 1 << a->tile_log;
   if (a->list) {
     a->units = (c.pad > 0 ? c.rows : c.rows + c.seqs) * ((a->group + tile_rows - 1) / tile_rows);
   } else if (c.pad > 0) {
@@ -685,7 +781,8 @@ size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_
   if (max_len > 0) keys = std::min(keys, max_len);
   if (a->list) keys = (static_cast<int64_t>(a->count) << c.plog) + (1 << c.plog);
   const int64_t blocks = a->units * c.hkv;
-  int64_t splits = std::min((kSplitBlocks + blocks - 1) / blocks, keys / kLeastChunk);
+  const int64_t most = a->tile_log == 7 ? kWideBlocks : blocks < kFewTiles ? kFewTileBlocks : kSplitBlocks;
+  int64_t splits = std::min((most + blocks - 1) / blocks, keys / kLeastChunk);
   const size_t one = static_cast<size_t>(blocks) * tile_rows * (c.d + 2) * sizeof(float);
   splits = std::min<int64_t>(splits, kMostPartBytes / one);
   if (splits <= 1) return 0;

@@ -66,6 +66,23 @@ __device__ inline int unit_exp(float top, float mant, int exp2) {
 }
 __device__ inline float exp2_int(int k) { return __uint_as_float(static_cast<uint32_t>(k + 127) << 23); }
 
+// Two signed bytes of a word as bf16. Written out, since the compiler else turns
+// all the bytes of a step into floats first and spills them.
+template <int HIGH>
+__device__ inline uint32_t pack_i8(uint32_t x) {
+  float a = 0.0f, b = 0.0f;
+#if defined(__HIP_DEVICE_COMPILE__)
+  if (HIGH) {
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(a) : "v"(x));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(b) : "v"(x));
+  } else {
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(a) : "v"(x));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(b) : "v"(x));
+  }
+#endif
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // whole numbers: no rounding
+}
+
 // Eight codes as bf16: both kinds are exact there.
 template <bool E4M3>
 __device__ inline bf16x8 codes8(uint32_t lo, uint32_t hi) {
@@ -77,12 +94,10 @@ __device__ inline bf16x8 codes8(uint32_t lo, uint32_t hi) {
     w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
     w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = (i < 2 ? lo : hi) >> (i & 1) * 16;
-      const float a = static_cast<float>(static_cast<int8_t>(x)), b = static_cast<float>(static_cast<int8_t>(x >> 8));
-      w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // whole numbers: no rounding
-    }
+    w[0] = pack_i8<0>(lo);
+    w[1] = pack_i8<1>(lo);
+    w[2] = pack_i8<0>(hi);
+    w[3] = pack_i8<1>(hi);
   }
   return __builtin_bit_cast(bf16x8, w);
 }

@@ -59,10 +59,10 @@ struct CacheAttn {
   const int32_t* list;  // [rows][hkv][count] page numbers of a sequence, or null
   int count;
   void* out;
-  int tile_rows;  // of a block: 16 or 32, its waves along the keys, or 128, along the rows
-  int splits;     // blocks that share a row tile's keys
+  int tile_log;  // rows of a block, 1 << tile_log: 16 or 32, its waves along the keys, or 128, along the rows
+  int splits;    // blocks that share a row tile's keys
   int64_t units;
-  int64_t block0;
+  uint32_t unit0;
   float *part_o, *part_ml;
 };
 
@@ -74,12 +74,12 @@ struct CacheSelect {
   float* scores;          // [tokens][hkv][width]
   int64_t max_pages;      // the caller's bound of a sequence's pages (0: none)
   int64_t row0, tokens;   // the rows of this launch
-  int tiles;
+  int tiles, run;         // blocks along the pages; rows of a block
 };
 
 hipError_t launch_cache_append(const CacheAppend& a, bool bf16, bool e4m3, hipStream_t s);
 hipError_t launch_cache_read(const CacheRead& a, bool bf16, bool e4m3, hipStream_t s);
-// Fills tile_rows, splits and units for at most max_q queries and max_len tokens a
+// Fills tile_log, splits and units for at most max_q queries and max_len tokens a
 // sequence; returns the workspace bytes.
 size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_at);
 hipError_t launch_cache_attn(const CacheAttn& a, bool bf16, bool e4m3, hipStream_t s);

@@ -510,16 +510,35 @@ def test_ties_go_to_the_lower_page():
     assert 600 in got and got[:10] == list(range(10)) and got[10] == 20
 
 
-def test_many_pages_are_chosen_exactly():
-    c = _cache(200, 1, 2, 64, 32, "i8", F32, bounds=True, causal=False)
+@pytest.mark.parametrize("width", [300, 1024, 1025, 16384, 20000, 65537])
+@pytest.mark.parametrize("distinct", [200, 3])
+def test_many_pages_are_chosen_exactly(width, distinct):
+    """Every way of picking; few distinct pages make nearly every score a tie."""
+    c = _cache(distinct, 1, 2, 64, 32, "i8", F32, bounds=True, causal=False)
     g = ref.fill(c, 4)
-    width = 20000
-    table = torch.randint(0, 200, (1, width), generator=g, device="cuda").to(torch.int32)
+    table = torch.randint(0, distinct, (1, width), generator=g, device="cuda").to(torch.int32)
     q = torch.randn(2, 6, 64, generator=g, device="cuda")
-    for count, max_len in ((1, 0), (64, 0), (4096, 1000), (19999, 0)):
+    for count, max_len in ((1, 0), (64, 0), (width // 4, 1000), (width - 1, 0)):
         got = c.select(q, _dev([0, 2]), _dev([width * 32]), table, count, max_len=max_len)
         for i in range(2):
             assert got[i].tolist() == ref.select(q[i], c, table[0].tolist(), width * 32, 0, count, False)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (5, 1), (8, 1), (18, 2), (40, 1), (12, 3)])
+@pytest.mark.parametrize("d,dtype", [(128, BF), (40, F32), (16, BF)])
+def test_groups_of_heads_choose_together(hq, hkv, d, dtype):
+    """Runs of rows over several sequences, under the causal mask, with rows that see few pages."""
+    c = _cache(150, 9, hkv, d, 32, "e4m3", dtype, bounds=True)
+    g = ref.fill(c, 6)
+    lens, new = [32 * 40 + 5, 3, 32 * 30, 700, 0], [37, 2, 1, 19, 1]
+    table = torch.randint(0, 150, (5, 41), generator=g, device="cuda").to(torch.int32)
+    q = torch.randn(sum(new), hq, d, generator=g, device="cuda").to(dtype)
+    off = ref.offsets(new)
+    got = c.select(q, off, _dev(lens), table, 21)
+    for b, n in enumerate(new):
+        for i in range(n):
+            want = ref.select(q[off[b] + i], c, table[b].tolist(), lens[b], lens[b] - n + i, 21, True)
+            assert [[x for x in h if x >= 0] for h in got[off[b] + i].tolist()] == want, (b, i)
 
 
 # ---------------------------------------------------------------------------
