@@ -16,6 +16,8 @@
 // 1 KiB stores a wave.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "cache_common.h"
 
 namespace rs {
@@ -60,11 +62,19 @@ __device__ inline Angle angle_of(uint64_t phase) {
   sincos_turn(phase, g.s, g.c);
   return g;
 }
+// The angle further on by another: off by 2^-53, where a series takes 15 times as
+// many instructions.
+__device__ inline void advance(Angle& g, const Angle& by) {
+  const double s = g.s * by.c + g.c * by.s;
+  g.c = g.c * by.c - g.s * by.s;
+  g.s = s;
+}
 // A pair of columns turned, in the model's type.
 __device__ inline void turn(const Angle& g, uint16_t& a, uint16_t& b) {
   const double x = bf16_to_f32(a), y = bf16_to_f32(b);
-  a = f32_to_bf16(static_cast<float>(x * g.c - y * g.s));
-  b = f32_to_bf16(static_cast<float>(y * g.c + x * g.s));
+  const uint32_t w = pack_bf16(static_cast<float>(x * g.c - y * g.s), static_cast<float>(y * g.c + x * g.s));
+  a = static_cast<uint16_t>(w);
+  b = static_cast<uint16_t>(w >> 16);
 }
 __device__ inline void turn(const Angle& g, float& a, float& b) {
   const double x = a, y = b;
@@ -153,10 +163,15 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
     const int f = threadIdx.x & (pw - 1), per = NT / pw;
     if (f < half_rot) {
       const uint64_t step = a.turns[f];
-      for (int t = max(t0, old) + threadIdx.x / pw; t < last; t += per) {
-        const Angle g = angle_of(static_cast<uint64_t>(first + t) * step);
-        T* x = reinterpret_cast<T*>(lds + t * stride) + ca * f;
-        turn(g, x[0], x[cb]);
+      int t = max(t0, old) + threadIdx.x / pw;
+      if (t < last) {
+        Angle g = angle_of(static_cast<uint64_t>(first + t) * step);
+        const Angle by = angle_of(static_cast<uint64_t>(per) * step);
+        for (; t < last; t += per) {
+          T* x = reinterpret_cast<T*>(lds + t * stride) + ca * f;
+          turn(g, x[0], x[cb]);
+          advance(g, by);
+        }
       }
     }
     __syncthreads();
@@ -258,8 +273,121 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
   }
 }
 
-// The grid: blocks of (touched page, key head, side), then blocks of four query
-// rows, then blocks of NT sequences for their new lengths.
+// Eight columns of a row.
+template <typename T>
+struct Eight {
+  u32x4 w[sizeof(T) / 2];
+  __device__ inline void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ inline void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<u32x4*>(p)[i] = w[i];
+  }
+  __device__ inline T get(int i) const {
+    if constexpr (sizeof(T) == 2) return static_cast<T>(w[0][i >> 1] >> 16 * (i & 1));
+    else return __uint_as_float(w[i >> 2][i & 3]);
+  }
+  __device__ inline void set(int i, T x) {
+    if constexpr (sizeof(T) == 2) w[0][i >> 1] = (w[0][i >> 1] & (i & 1 ? 0xFFFFu : 0xFFFF0000u)) | static_cast<uint32_t>(x) << 16 * (i & 1);
+    else w[i >> 2][i & 3] = __float_as_uint(x);
+  }
+};
+
+// Query rows: a wave takes four of a sequence, one after another, an angle a lane
+// and by LDS to every head, then eight pairs of a head a lane where the columns allow
+// whole 16-byte loads.
+constexpr int kTurnRows = 4;
+template <typename T, int NT>
+__device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64_t b) {
+  constexpr int kTile = kTurnRows * NT / kWave;  // rows of a block
+  const CacheArgs& c = a.c;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), d = c.d;
+  int64_t tile;
+  int s;
+  if (c.pad > 0) {
+    const int64_t per = (c.pad + kTile - 1) / kTile;
+    s = static_cast<int>(b / per);
+    tile = b - s * per;
+    if (s >= c.seqs) return;
+  } else {
+    s = find_seq(c.off, c.seqs, 1, kTile, b, tile);
+  }
+  const SeqSpan span = seq_span(c.off, s, c.pad, c.rows);
+  const int64_t all = c.pad > 0 ? c.pad : int64_t(span.len), first = tile * kTile + wave * kTurnRows;
+  if (tile < 0 || first >= all) return;
+  const int64_t base = max(c.lens[s], int64_t(0));
+  const RotPairs rp(a);
+  Angle* angles = reinterpret_cast<Angle*>(lds) + wave * kWave;  // rotary / 2 is at most 64
+  Angle g = {0.0, 1.0}, by = g;
+  if (lane < rp.count) {
+    g = angle_of(static_cast<uint64_t>(base + first) * a.turns[lane]);
+    by = angle_of(a.turns[lane]);
+  }
+  const uint32_t chunks = rp.count / 8, rest = (d - a.rotary) / 8, per = chunks + rest;
+  for (int64_t token = first; token < min(all, first + kTurnRows); ++token) {
+    const int64_t row = span.start + token;
+    T* out = static_cast<T*>(a.q_out) + row * a.hq * d;
+    if (token >= span.len) {  // past the sequence's end
+      for (int i = lane; i < a.hq * d; i += kWave) out[i] = T(0);
+      continue;
+    }
+    const T* q = static_cast<const T*>(a.q.p) + row * a.q.row;
+    angles[lane] = g;
+    advance(g, by);
+    __builtin_amdgcn_wave_barrier();
+    if (rp.count % 8 == 0) {
+      for (uint32_t i = lane; i < per * a.hq; i += kWave) {
+        const uint32_t h = i / per, k = i - h * per;
+        const T* from = q + h * a.q.head;
+        T* to = out + h * d;
+        Eight<T> x, y;
+        if (k >= chunks) {  // columns that stay
+          x.load(from + a.rotary + (k - chunks) * 8);
+          x.store(to + a.rotary + (k - chunks) * 8);
+          continue;
+        }
+        const int f = k * 8, ca = a.next ? 2 * f : f, cb = a.next ? 2 * f + 8 : f + rp.count;
+        x.load(from + ca);
+        y.load(from + cb);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const Angle at = angles[f + e];
+          if (a.next) {
+            Eight<T>& z = e < 4 ? x : y;
+            T v = z.get(2 * (e & 3)), w = z.get(2 * (e & 3) + 1);
+            turn(at, v, w);
+            z.set(2 * (e & 3), v);
+            z.set(2 * (e & 3) + 1, w);
+          } else {
+            T v = x.get(e), w = y.get(e);
+            turn(at, v, w);
+            x.set(e, v);
+            y.set(e, w);
+          }
+        }
+        x.store(to + ca);
+        y.store(to + cb);
+      }
+    } else {
+      const int f = lane & (rp.lanes - 1), step = kWave / rp.lanes;
+      if (f < rp.count)
+        for (int h = lane / rp.lanes; h < a.hq; h += step) {
+          T x = q[h * a.q.head + rp.step * f], y = q[h * a.q.head + rp.step * f + rp.apart];
+          turn(angles[f], x, y);
+          out[h * d + rp.step * f] = x;
+          out[h * d + rp.step * f + rp.apart] = y;
+        }
+      for (int h = 0; h < a.hq && a.rotary < d; ++h)
+        for (int i = a.rotary + lane; i < d; i += kWave) out[h * d + i] = q[h * a.q.head + i];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The grid: blocks of (touched page, key head, side), then blocks of query rows, then
+// blocks of NT sequences for their new lengths.
 template <typename T, bool E4M3, int NT>
 __global__ __launch_bounds__(NT) void k_cache_append(const CacheAppend a) {
   extern __shared__ __align__(16) char lds[];
@@ -273,42 +401,7 @@ __global__ __launch_bounds__(NT) void k_cache_append(const CacheAppend a) {
   if (b >= a.page_units * c.hkv * 2) {
     b -= a.page_units * c.hkv * 2;
     if (b < a.q_units) {
-      // a wave per query row
-      int64_t u = b * (NT / kWave) + wave, token;
-      int s;
-      if (c.pad > 0) {
-        if (u >= c.rows) return;
-        s = static_cast<int>(u / c.pad);
-        token = u - s * c.pad;
-      } else {
-        if (u >= c.rows + c.seqs) return;
-        s = find_seq(c.off, c.seqs, 1, 1, u, token);
-      }
-      const SeqSpan span = seq_span(c.off, s, c.pad, c.rows);
-      if (token < 0 || token >= (c.pad > 0 ? c.pad : int64_t(span.len))) return;
-      const int64_t row = span.start + token;
-      T* out = static_cast<T*>(a.q_out) + row * a.hq * d;
-      if (token >= span.len) {  // past the sequence's end
-        for (int i = lane; i < a.hq * d; i += kWave) out[i] = T(0);
-        return;
-      }
-      const T* q = static_cast<const T*>(a.q.p) + row * a.q.row;
-      const uint64_t p = static_cast<uint64_t>(max(c.lens[s], int64_t(0)) + token);
-      const RotPairs rp(a);
-      const int half_rot = rp.count, pw = rp.lanes, ca = rp.step, cb = rp.apart;
-      const int f = lane & (pw - 1), sub = lane / pw, step = kWave / pw;
-      if (half_rot > 0 && f < half_rot) {
-        const Angle g = angle_of(p * a.turns[f]);
-        for (int h = sub; h < a.hq; h += step) {
-          T x = q[h * a.q.head + ca * f], y = q[h * a.q.head + ca * f + cb];
-          turn(g, x, y);
-          out[h * d + ca * f] = x;
-          out[h * d + ca * f + cb] = y;
-        }
-      }
-      const int rest = d - a.rotary;
-      for (int h = 0; h < a.hq && rest > 0; ++h)
-        for (int i = a.rotary + lane; i < d; i += kWave) out[h * d + i] = q[h * a.q.head + i];
+      turn_rows<T, NT>(a, lds, b);
       return;
     }
     b -= a.q_units;
@@ -349,19 +442,30 @@ __global__ __launch_bounds__(NT) void k_cache_append(const CacheAppend a) {
     append_page<T, E4M3, NT>(a, lds, sh_top, sh_low, sh_high, s, kvh, side, slot, span, held, end, n_end);
   }
 }
-__device__ inline void put(uint16_t* p, float x) { *p = f32_to_bf16(x); }
-__device__ inline void put(float* p, float x) { *p = x; }
+template <typename O>
+__device__ inline O as_out(float x);
+template <>
+__device__ inline uint16_t as_out<uint16_t>(float x) {
+  return f32_to_bf16(x);
+}
+template <>
+__device__ inline float as_out<float>(float x) {
+  return x;
+}
 
 // Rows start[s] + i of sequence s as the cache holds them: a block per touched
-// page and key head.
+// page, key head and side, 64 tokens at a time through LDS, so that rows are
+// stored whole.
+constexpr int kReadTokens = 64;
 template <typename T, typename O, bool E4M3>
 __global__ __launch_bounds__(kBlock) void k_cache_read(const CacheRead a, int64_t block0) {
+  constexpr int kStride = 128 * static_cast<int>(sizeof(O)) + 16;  // rows start on other banks
+  __shared__ __align__(16) char lds[kReadTokens * kStride];
   const CacheArgs& c = a.c;
   const int d = c.d, P = 1 << c.plog, W = d <= 32 ? 32 : d <= 64 ? 64 : 128;
-  const int64_t b = block0 + blockIdx.x;
-  const int kvh = static_cast<int>(b % c.hkv);
+  const int side = blockIdx.z, kvh = blockIdx.y;
   int64_t tile;
-  const int s = find_pages(c.off, c.seqs, c.plog, b / c.hkv, tile);
+  const int s = find_pages(c.off, c.seqs, c.plog, block0 + blockIdx.x, tile);
   if (tile < 0) return;
   const SeqSpan span = seq_span(c.off, s, 0, c.rows);
   const int64_t begin = a.start ? max(a.start[s], int64_t(0)) : 0, end = begin + span.len;
@@ -372,41 +476,58 @@ __global__ __launch_bounds__(kBlock) void k_cache_read(const CacheRead a, int64_
   const bool full = first + P <= len;
   const int slot = cache_slot(c, s), page = full ? cache_page(c, s, n) : -1;
   const int64_t row0 = span.start + first - begin;  // of the page's token 0
-  auto at = [&](void* base, int t) { return static_cast<O*>(base) + ((row0 + t) * c.hkv + kvh) * d; };
-  if (!full || page < 0) {
+  O* to = static_cast<O*>(side ? a.v : a.k) + (row0 * c.hkv + kvh) * d;
+  const int64_t row = static_cast<int64_t>(c.hkv) * d;
+  const int chunks = d / 8, cw = chunks <= 1 ? 1 : 1 << (32 - __builtin_clz(chunks - 1));  // of eight columns
+  const int ch = threadIdx.x & (cw - 1), per = kBlock / cw;
+  if (page < 0) {  // an open page, or none
     const int held = !full && slot >= 0 ? static_cast<int>(min(max(len - first, int64_t(0)), static_cast<int64_t>(t1))) : 0;
-    for (int side = 0; side < 2; ++side) {
-      const T* open = static_cast<const T*>(c.open) + (held > 0 ? open_at(c, slot, n, kvh, side) : 0);
-      const int cols = d;
-      for (int i = threadIdx.x; i < (t1 - t0) * cols; i += kBlock) {
-        const int t = t0 + i / cols, col = i % cols;
-        put(at(side ? a.v : a.k, t) + col, t < held ? to_f32(open[t * d + col]) : 0.0f);
+    const T* open = static_cast<const T*>(c.open) + (held > 0 ? open_at(c, slot, n, kvh, side) : 0);
+    if (ch < chunks)
+      for (int t = t0 + threadIdx.x / cw; t < t1; t += per) {
+        Eight<T> x;
+        Eight<O> y;
+        if (t < held) x.load(open + t * d + ch * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y.set(e, as_out<O>(t < held ? to_f32(x.get(e)) : 0.0f));
+        y.store(to + t * row + ch * 8);
       }
-    }
     return;
   }
-  const float* sc = c.scales + (static_cast<int64_t>(page) * c.hkv + kvh) * 2;
-  const uint8_t* keys = c.data + cache_at(c, page, kvh, 0, W);
-  for (int i = threadIdx.x; i < (W / 16) << c.plog; i += kBlock) {
-    const int t = i & (P - 1), ch = i >> c.plog;
-    if (t < t0 || t >= t1) continue;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(keys + i * 16);
-    O* to = at(a.k, t) + ch * 16;
+  const float scale = c.scales[(static_cast<int64_t>(page) * c.hkv + kvh) * 2 + side];
+  const uint8_t* data = c.data + cache_at(c, page, kvh, side, W);
+  for (int base = t0 & ~(kReadTokens - 1); base < t1; base += kReadTokens) {
+    const int tokens = min(kReadTokens, P), log = c.plog < 6 ? 5 : 6;  // 1 << log of them
+    __syncthreads();
+    if (side == 0) {
+      for (int i = threadIdx.x; i < W / 16 * tokens; i += kBlock) {
+        const int t = i & (tokens - 1), col = i >> log;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(data + (((col << c.plog) + base + t) << 4));
+        Eight<O> y[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (ch * 16 + j * 4 < d)
+        for (int e = 0; e < 16; ++e)
+          y[e >> 3].set(e & 7, as_out<O>(code_value<E4M3>(static_cast<uint8_t>(w[e >> 2] >> 8 * (e & 3))) * scale));
+        O* at = reinterpret_cast<O*>(lds + t * kStride) + col * 16;
+        y[0].store(at);
+        y[1].store(at + 8);
+      }
+    } else {
+      for (int i = threadIdx.x; i < W * tokens / 16; i += kBlock) {
+        const int col = i & (W - 1), t = i / W * 16;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(data + (((base + t) / 16 * W + col) << 4));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) put(to + j * 4 + e, code_value<E4M3>(static_cast<uint8_t>(w[j] >> 8 * e)) * sc[0]);
-  }
-  const uint8_t* values = c.data + cache_at(c, page, kvh, 1, W);
-  for (int i = threadIdx.x; i < W << (c.plog - 4); i += kBlock) {
-    const int col = i & (W - 1), t = i / W * 16;
-    if (col >= d) continue;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(values + i * 16);
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (t + j >= t0 && t + j < t1)
-        put(at(a.v, t + j) + col, code_value<E4M3>(static_cast<uint8_t>(w[j >> 2] >> 8 * (j & 3))) * sc[1]);
+        for (int e = 0; e < 16; ++e)
+          reinterpret_cast<O*>(lds + (t + e) * kStride)[col] =
+              as_out<O>(code_value<E4M3>(static_cast<uint8_t>(w[e >> 2] >> 8 * (e & 3))) * scale);
+      }
+    }
+    __syncthreads();
+    if (ch < chunks)
+      for (int t = max(t0, base) + threadIdx.x / cw; t < min(t1, base + tokens); t += per) {
+        Eight<O> y;
+        y.load(reinterpret_cast<const O*>(lds + (t - base) * kStride) + ch * 8);
+        y.store(to + t * row + ch * 8);
+      }
   }
 }
 
@@ -417,7 +538,8 @@ hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
   const bool rows = a.k.p != nullptr && a.c.rows > 0;
   const int64_t u = a.c.pad > 0 ? a.c.seqs * ((a.c.pad >> a.c.plog) + 2) : (a.c.rows >> a.c.plog) + 2 * int64_t(a.c.seqs);
   a.page_units = rows ? u : 0;
-  a.q_units = a.q.p ? ((a.c.pad > 0 ? a.c.rows : a.c.rows + a.c.seqs) + NT / kWave - 1) / (NT / kWave) : 0;
+  constexpr int64_t kTile = kTurnRows * NT / kWave;
+  a.q_units = !a.q.p ? 0 : a.c.pad > 0 ? a.c.seqs * ((a.c.pad + kTile - 1) / kTile) : a.c.rows / kTile + a.c.seqs;
   const int64_t lens = a.new_lens ? (a.c.seqs + NT - 1) / NT : 0;
   const int64_t blocks = a.page_units * a.c.hkv * 2 + a.q_units + lens;
   if (bytes > 65536) {
@@ -435,17 +557,18 @@ hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
 
 template <typename T, bool E4M3>
 hipError_t append_type(const CacheAppend& a, hipStream_t s) {
-  const int bytes = lds_stride<T>(a.c.d) << a.c.plog;
+  const int angles = kBlock * static_cast<int>(sizeof(Angle)), page = lds_stride<T>(a.c.d) << a.c.plog;
+  const int bytes = page > 65536 ? std::max(page, 4 * angles) : std::max(page, angles);
   // a large page fills a CU's LDS by itself: more waves on it then
   return bytes > 65536 ? append<T, E4M3, 1024>(a, bytes, s) : append<T, E4M3, 256>(a, bytes, s);
 }
 
 template <typename T, typename O, bool E4M3>
 hipError_t read_type(const CacheRead& a, hipStream_t s) {
-  const int64_t blocks = ((a.c.rows >> a.c.plog) + 2 * int64_t(a.c.seqs)) * a.c.hkv;
+  const int64_t blocks = (a.c.rows >> a.c.plog) + 2 * int64_t(a.c.seqs);
   for (int64_t b = 0; b < blocks; b += kMostBlocks) {
     const int64_t now = blocks - b < kMostBlocks ? blocks - b : kMostBlocks;
-    k_cache_read<T, O, E4M3><<<static_cast<unsigned>(now), kBlock, 0, s>>>(a, b);
+    k_cache_read<T, O, E4M3><<<dim3(static_cast<unsigned>(now), a.c.hkv, 2), kBlock, 0, s>>>(a, b);
   }
   return hipGetLastError();
 }
