@@ -220,6 +220,15 @@ def _stream() -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
+# The current device without torch.cuda's own checks; a tensor on the GPU has passed them.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_of(device: int) -> int:
+    """hipStream_t of the current stream of a device."""
+    return torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(device)
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -699,39 +708,45 @@ class SeqCache(_Workspace):
         self._desc = CacheDesc(1 if codes == "e4m3" else 0, _SEQ_TYPES[dtype], heads_kv, head_dim, page, 0, pages, slots,
                                self.codes.data_ptr(), self.scales.data_ptr(), self.open.data_ptr(), _ptr(self.bounds),
                                _ptr(self.units))
+        self._ref = C.byref(self._desc)
+        self._index, self._slots, self._turns = dev.index, slots, _ptr(self.turns)
+        self._odd = 16 // self.open.element_size() - 1
 
+    # The host time of a call counts for the smallest (kernels there take 4 to 10 us): device numbers are compared, not
+    # device objects, and structs are filled by position.
     def _layout(self, t: torch.Tensor, what: str, heads: int = 0):
-        """The tensor (copied if its strides do not serve), rows, pad, row and head strides."""
-        if not t.is_cuda or t.device != self.codes.device:
+        """The tensor (copied if its strides do not serve), its address, rows, pad, row and head strides."""
+        if t.get_device() != self._index:
             raise RecisError(EINVAL, "tensors must be on the GPU, the cache's")
         if t.dtype != self.dtype:
             raise RecisError(EINVAL, f"{what} must be {self.dtype}, got {t.dtype}")
-        if t.dim() not in (3, 4) or t.shape[-1] != self.head_dim or (heads and t.shape[-2] != heads):
+        shape, st = t.shape, t.stride()
+        n = len(shape)
+        if n not in (3, 4) or shape[-1] != self.head_dim or (heads and shape[-2] != heads):
             raise RecisError(EINVAL, f"{what} must be [rows, heads, {self.head_dim}] or [seqs, pad, heads, {self.head_dim}]"
                              + (f" with {heads} heads" if heads else ""))
-        unit = 16 // t.element_size()
-        st = t.stride()
-        if (st[-1] != 1 or st[-2] % unit or st[-3] % unit or max(st[-2], st[-3]) >= 1 << 31 or
-                (t.dim() == 4 and st[0] != t.shape[1] * st[1]) or t.data_ptr() % 16):
+        at = t.data_ptr()
+        if (st[-1] != 1 or (st[-2] | st[-3]) & self._odd or st[-2] >> 31 or st[-3] >> 31 or at & 15 or
+                (n == 4 and st[0] != shape[1] * st[1])):
             t = _packed(t)
-            st = t.stride()
-        if t.dim() == 4:
-            return t, t.shape[0] * t.shape[1], t.shape[1], st[1], st[2]
-        return t, t.shape[0], 0, st[0], st[1]
+            st, at = t.stride(), t.data_ptr()
+        if n == 4:
+            return t, at, shape[0] * shape[1], shape[1], st[1], st[2]
+        return t, at, shape[0], 0, st[0], st[1]
 
     def _same(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
-        if t.device != self.codes.device or t.dtype != dtype:
+        if t.get_device() != self._index or t.dtype != dtype:
             raise RecisError(EINVAL, f"{what} must be {dtype} on the cache's GPU")
         return t if t.is_contiguous() else t.contiguous()
 
     def _batch(self, rows, pad, padded, offsets, lens, table, slots, own_slots=True):
-        if torch.cuda.current_device() != self.codes.device.index:
+        if _device() != self._index:
             raise RecisError(EINVAL, "the cache's GPU must be the current one")
         offsets = self._same(offsets, torch.int64, "offsets")
         lens = self._same(lens, torch.int64, "lens")
         table = self._same(table, torch.int32, "table")
-        seqs = offsets.numel() - 1
-        if seqs < 0 or lens.numel() != seqs or table.dim() != 2 or table.shape[0] != seqs:
+        seqs, shape = offsets.numel() - 1, table.shape
+        if seqs < 0 or lens.numel() != seqs or len(shape) != 2 or shape[0] != seqs:
             raise RecisError(EINVAL, "offsets must be [seqs + 1], lens [seqs] and table [seqs, width]")
         if padded is not None and padded != seqs:
             raise RecisError(EINVAL, "a padded tensor must have one block per sequence")
@@ -739,10 +754,10 @@ class SeqCache(_Workspace):
             slots = self._same(slots, torch.int32, "slots")
             if slots.numel() != seqs:
                 raise RecisError(EINVAL, "slots must have one slot per sequence")
-        elif own_slots and self.open.shape[0] < seqs:
+        elif own_slots and self._slots < seqs:
             raise RecisError(EINVAL, "more sequences than slots")
-        return CacheBatch(seqs, rows, pad, table.shape[1], offsets.data_ptr(), lens.data_ptr(), table.data_ptr(),
-                          _ptr(slots)), (offsets, lens, table, slots)
+        return CacheBatch(seqs, rows, pad, shape[1], offsets.data_ptr(), lens.data_ptr(), table.data_ptr(),
+                          None if slots is None else slots.data_ptr()), (offsets, lens, table, slots)
 
     def append(self, k: Optional[torch.Tensor], v: Optional[torch.Tensor], offsets: torch.Tensor, lens: torch.Tensor,
                table: torch.Tensor, q: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
@@ -752,27 +767,29 @@ class SeqCache(_Workspace):
         would be with the rows kept, and nothing is written."""
         if (k is None) != (v is None) or (k is None and q is None):
             raise RecisError(EINVAL, "append takes k and v, q, or all three")
-        shape, r, q_out = None, CacheRows(rotary=self.rotary, interleaved=int(self.interleaved), turns=_ptr(self.turns)), None
+        q_out, ka, va, qa, oa, heads = None, None, None, None, None, 0
+        ks = kh = vs = vh = qs = qh = 0
         if k is not None:
-            k, rows, pad, r.k_stride, r.k_head_stride = self._layout(k, "k", self.heads_kv)
-            v, _, _, r.v_stride, r.v_head_stride = self._layout(v, "v", self.heads_kv)
-            if k.shape != v.shape:
+            k, ka, rows, pad, ks, kh = self._layout(k, "k", self.heads_kv)
+            v, va, _, _, vs, vh = self._layout(v, "v", self.heads_kv)
+            shape = k.shape
+            if shape != v.shape:
                 raise RecisError(EINVAL, "k and v must have one shape")
-            r.k, r.v, shape = k.data_ptr(), v.data_ptr(), k.shape
         if q is not None:
-            q, rows, pad, r.q_stride, r.q_head_stride = self._layout(q, "q")
-            if shape is not None and q.shape[:-2] != shape[:-2]:
+            q, qa, rows, pad, qs, qh = self._layout(q, "q")
+            if k is not None and q.shape[:-2] != shape[:-2]:
                 raise RecisError(EINVAL, "q must have the rows of k")
             q_out, shape = _like(q), q.shape
-            r.q, r.q_out, r.heads_q = q.data_ptr(), q_out.data_ptr(), q.shape[-2]
-        if k is not None and k.numel() == 0:
-            r.k = r.v = None
-        if q is not None and q.numel() == 0:
-            r.q = r.q_out = None
+            oa, heads = q_out.data_ptr(), shape[-2]
+        if rows == 0:
+            ka = va = qa = oa = None
         b, keep = self._batch(rows, pad, shape[0] if len(shape) == 4 else None, offsets, lens, table, slots)
         new_lens = torch.empty_like(keep[1])
-        r.new_lens = new_lens.data_ptr()
-        _check(lib().seq_cache_append(C.byref(self._desc), C.byref(b), C.byref(r), int(validate), _stream()))
+        r = CacheRows(ka, va, qa, oa, ks, kh, vs, vh, qs, qh, heads, self.rotary, self.interleaved, 0, self._turns,
+                      new_lens.data_ptr())
+        st = lib().seq_cache_append(self._ref, b, r, validate, _stream_of(self._index))
+        if st:
+            _check(st)
         return new_lens, q_out
 
     def read(self, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, rows: Optional[int] = None,
@@ -791,20 +808,22 @@ class SeqCache(_Workspace):
             start = self._same(start, torch.int64, "start")
             if start.numel() != b.seqs:
                 raise RecisError(EINVAL, "start must have one position per sequence")
-        k = torch.empty(rows, self.heads_kv, self.head_dim, dtype=dtype, device=self.codes.device)
+        k = torch.empty((rows, self.heads_kv, self.head_dim), dtype=dtype, device=self.codes.device)
         v = torch.empty_like(k)
-        _check(lib().seq_cache_read(C.byref(self._desc), C.byref(b), _ptr(start), k.data_ptr(), v.data_ptr(),
-                                    _SEQ_TYPES[dtype], int(validate), _stream()))
+        st = lib().seq_cache_read(self._ref, b, _ptr(start), k.data_ptr(), v.data_ptr(), _SEQ_TYPES[dtype], validate,
+                                  _stream_of(self._index))
+        if st:
+            _check(st)
         return k, v
 
     def _query(self, q, offsets, lens, table, slots, count, max_q, max_len, own_slots=True):
-        q, rows, pad, qs, qh = self._layout(q, "q")
-        if q.shape[-2] < self.heads_kv or q.shape[-2] % self.heads_kv:
+        q, at, rows, pad, qs, qh = self._layout(q, "q")
+        heads = q.shape[-2]
+        if heads < self.heads_kv or heads % self.heads_kv:
             raise RecisError(EINVAL, "q's heads must be a multiple of heads_kv")
-        b, keep = self._batch(rows, pad, q.shape[0] if q.dim() == 4 else None, offsets, lens, table, slots,
-                              own_slots)
+        b, keep = self._batch(rows, pad, q.shape[0] if pad or q.dim() == 4 else None, offsets, lens, table, slots, own_slots)
         scale = self.scale if self.scale is not None else self.head_dim ** -0.5
-        return q, b, keep, CacheQuery(q.shape[-2], int(self.causal), count, 0, max_q, max_len, qs, qh, scale, self.softcap)
+        return q, at, b, keep, CacheQuery(heads, self.causal, count, 0, max_q, max_len, qs, qh, scale, self.softcap)
 
     def attend(self, q: torch.Tensor, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
                pages: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None,
@@ -812,7 +831,7 @@ class SeqCache(_Workspace):
                out: Optional[torch.Tensor] = None, validate: bool = False) -> torch.Tensor:
         shape = q.shape
         count = 0 if pages is None else pages.shape[-1]
-        q, b, keep, d = self._query(q, offsets, lens, table, slots, count, max_q, max_len)
+        q, at, b, keep, d = self._query(q, offsets, lens, table, slots, count, max_q, max_len)
         if pages is not None:
             pages = self._same(pages, torch.int32, "pages")
             if pages.shape != (*shape[:-2], self.heads_kv, count) or count < 1:
@@ -825,10 +844,13 @@ class SeqCache(_Workspace):
             out = _like(q)
         elif out.shape != shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
             raise RecisError(EINVAL, "out must be a contiguous GPU tensor of q's shape and type")
-        need = lib().seq_cache_attention_workspace_bytes(C.byref(self._desc), C.byref(b), C.byref(d))
+        L = lib()
+        need = L.seq_cache_attention_workspace_bytes(self._ref, b, d)
         ws = self._take(need, q) if need else None
-        _check(lib().seq_cache_attention(C.byref(self._desc), C.byref(b), C.byref(d), q.data_ptr(), _ptr(pages), _ptr(slopes),
-                                         out.data_ptr(), _ptr(ws), ws.numel() if need else 0, int(validate), _stream()))
+        st = L.seq_cache_attention(self._ref, b, d, at, _ptr(pages), _ptr(slopes), out.data_ptr(), _ptr(ws),
+                                   ws.numel() if need else 0, validate, _stream_of(self._index))
+        if st:
+            _check(st)
         return out
 
     def select(self, q: torch.Tensor, offsets: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, count: int,
@@ -840,12 +862,15 @@ class SeqCache(_Workspace):
         if count < 1:
             raise RecisError(EINVAL, "count must be >= 1")
         shape = q.shape
-        q, b, keep, d = self._query(q, offsets, lens, table, None, count, max_q, max_len, False)
-        pages = torch.empty(*shape[:-2], self.heads_kv, count, dtype=torch.int32, device=q.device)
-        need = lib().seq_cache_select_workspace_bytes(C.byref(self._desc), C.byref(b), C.byref(d))
+        q, at, b, keep, d = self._query(q, offsets, lens, table, None, count, max_q, max_len, False)
+        pages = torch.empty((*shape[:-2], self.heads_kv, count), dtype=torch.int32, device=q.device)
+        L = lib()
+        need = L.seq_cache_select_workspace_bytes(self._ref, b, d)
         ws = self._take(need, q) if need else None
-        _check(lib().seq_cache_select(C.byref(self._desc), C.byref(b), C.byref(d), q.data_ptr(), pages.data_ptr(), _ptr(ws),
-                                      ws.numel() if need else 0, int(validate), _stream()))
+        st = L.seq_cache_select(self._ref, b, d, at, pages.data_ptr(), _ptr(ws), ws.numel() if need else 0, validate,
+                                _stream_of(self._index))
+        if st:
+            _check(st)
         return pages
 
 
