@@ -227,9 +227,9 @@ struct RowParams {
 };
 
 // The lane's NS keys from position j on into the softmax: p comes as the products
-// of the codes and leaves as probabilities times vs. masked: some lane's row may
-// not see some key of the step.
-template <typename T, int M, int HD, int NS>
+// of the codes and leaves as probabilities, SCALED times vs. masked: some lane's row
+// may not see some key of the step.
+template <typename T, bool SCALED, int M, int HD, int NS>
 __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[NS], const RowParams& r, bool capped, bool sloped,
                                        float ks, float vs, int j, bool masked) {
   float c = r.scale * kLog2e * ks;
@@ -272,14 +272,14 @@ __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[NS], con
   for (int i = 0; i < NS; ++i) {
     p[i] = exp2_hw(p[i]);
     sum += p[i];
-    p[i] *= vs;
+    if (SCALED) p[i] *= vs;
   }
   st.l += sum;
 }
 
 // Waves of a SIMD that the registers are kept down for.
 template <typename T, int HD, int M>
-constexpr int kResident = M == 16 ? (sizeof(T) == 4 ? (HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 3) : HD <= 64 ? (sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? 2 : 1;
+constexpr int kResident = M == 16 ? (sizeof(T) == 4 ? (HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 3) : HD <= 64 ? (sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? 3 : 1;
 
 __device__ inline float lane_value(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
@@ -327,21 +327,39 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   rp.cap = a.cap;
   const bool capped = a.cap > 0.0f, sloped = a.slopes != nullptr;
 
-  bf16x8 qf[2 * KC][NP];
+  // The rows as an operand. Those of 128 bf16 columns lie in LDS, in the order of the
+  // lanes: their 32 registers are what keeps a third wave off a SIMD.
+  constexpr bool kRowsInLds = M == 32 && WR == 1 && HD == 128 && sizeof(T) == 2;
+  __shared__ __align__(16) char q_rows[kRowsInLds ? WR * 2 * KC * kWave * 16 : 16];
+  bf16x8* const my_rows = reinterpret_cast<bf16x8*>(q_rows) + wr * 2 * KC * kWave + lane;
+  bf16x8 qf[kRowsInLds ? 1 : 2 * KC][NP];
   {
     const T* q = static_cast<const T*>(a.q.p) + (t.start + me.token) * a.q.row + me.head * a.q.head;
 #pragma unroll
     for (int i = 0; i < 2 * KC; ++i) {
       const int d0 = i / 2 * 16 * G + grp * 16 + (i & 1) * 8;
       const bool in = d0 < c.d && t.rows > 0;
+      bf16x8 f[NP];
 #pragma unroll
-      for (int n = 0; n < NP; ++n) qf[i][n] = bf16x8{};
-      if (t.rows > 0) load8(q + (in ? d0 : 0), qf[i]);
-      if (!in)
+      for (int n = 0; n < NP; ++n) f[n] = bf16x8{};
+      if (t.rows > 0) load8(q + (in ? d0 : 0), f);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) qf[i][n] = bf16x8{};
+      for (int n = 0; n < NP; ++n) {
+        if (!in) f[n] = bf16x8{};
+        if (!kRowsInLds) qf[i][n] = f[n];
+      }
+      if (kRowsInLds && wk == 0) my_rows[i * kWave] = f[0];
     }
+    if (kRowsInLds) __syncthreads();
   }
+  auto with_rows = [&](const auto& kf, int i, typename S::acc sc) {
+    if constexpr (kRowsInLds) {
+      const bf16x8 f[1] = {my_rows[i * kWave]};
+      return mma_pieces<M>(kf, f, sc);
+    } else {
+      return mma_pieces<M>(kf, qf[i], sc);
+    }
+  };
   AttnState<M, HD> st;
 #pragma unroll
   for (int i = 0; i < DT; ++i) st.acc[i] = typename S::acc{};
@@ -373,6 +391,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
     }
     pages = cache_page(c, t.s, num);
     if (pages >= 0) scales = reinterpret_cast<const float2*>(c.scales)[static_cast<int64_t>(pages) * c.hkv + kvh];
+    if (scales.y != scales.y) scales.x = scales.y;  // the conversion of e4m3 takes a scale's exponent alone
   };
 
   u32x4 kc[KT][KC];
@@ -405,6 +424,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
     return page >= 0 ? first : -1;
   };
   auto scores_coded = [&](float (&p)[NS]) {
+    if (kRowsInLds) asm volatile("" ::: "memory");  // the rows are read again, not kept
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
       typename S::acc sc = {};
@@ -412,8 +432,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
       for (int y = 0; y < KC; ++y)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bf16x8 kf[1] = {codes8<E4M3>(kc[x][y][2 * u], kc[x][y][2 * u + 1])};
-          sc = mma_pieces<M>(kf, qf[2 * y + u], sc);
+          const bf16x8 kf[1] = {codes8<E4M3>(kc[x][y][2 * u], kc[x][y][2 * u + 1], 1.0f)};
+          sc = with_rows(kf, 2 * y + u, sc);
         }
 #pragma unroll
       for (int i = 0; i < NS / KT; ++i) p[x * (NS / KT) + i] = sc[i];
@@ -424,7 +444,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
     for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int x = 0; x < DT; ++x) {
-        const bf16x8 vf[1] = {codes8<E4M3>(vc[x][2 * u], vc[x][2 * u + 1])};
+        const bf16x8 vf[1] = {codes8<E4M3>(vc[x][2 * u], vc[x][2 * u + 1], scale.y)};
         st.acc[x] = mma_pieces<M>(vf, pf[u], st.acc[x]);
         if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // no operands are made ahead
       }
@@ -451,7 +471,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
         const int d0 = y / 2 * 16 * G + grp * 16 + (y & 1) * 8;
         bf16x8 kf[NP];
         load8(open + (row + (d0 < c.d ? d0 : 0)), kf);
-        sc = mma_pieces<M>(kf, qf[y], sc);
+        sc = with_rows(kf, y, sc);
       }
 #pragma unroll
       for (int i = 0; i < NS / KT; ++i) p[x * (NS / KT) + i] = sc[i];
@@ -487,48 +507,127 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
     }
   };
 
-  int j = 0;
-  if (wk < full_steps) {
-    look(wk);
-    load_keys(0);
-  }
   // Few rows: a block lives for a few steps, and what it fetches of the kernel's
   // code counts as much as its data (the open page in a loop of its own: token of
   // 256 users 77 us, so 67), so both kinds of steps share one softmax.
   constexpr bool kShared = M == 16;
   int s = wk;
-  for (; s < (kShared ? steps : full_steps); s += WK) {
-    const bool coded = !kShared || s < full_steps;  // wave-uniform
-    const int k0 = (s - full_steps) * kCacheBlock;
-    int key0 = t.closed + k0;
-    float p[NS];
-    if (coded) {
-      key0 = load_values(j);
-      scores_coded(p);
-      // the next keys into the same registers, under the softmax and the second product
-      if (s + WK < full_steps) {
-        j = j + 1 == kWave ? 0 : j + 1;
-        if (j == 0) look(s + WK);
-        load_keys(j);
+  if constexpr (WR > 1) {
+    // Waves along the rows read the same keys: each makes the operands of its share
+    // of them, once, into LDS, a step ahead. (Every wave by itself: 4096 rows over
+    // 16384 keys 338 us in e4m3 and 435 in i8: bound by those conversions.)
+    constexpr int kItems = KC + DT, kEach = (kItems + WR - 1) / WR;  // 16-byte loads of a step, of a wave
+    constexpr int kFrags = 2 * KC + NU * DT;
+    __shared__ __align__(16) bf16x8 operands[2][kFrags * kWave];
+    struct Step {
+      int first;  // below 0: a page that is not there
+      float ks, vs;
+    };
+    u32x4 raw[kEach];
+    auto fetch = [&](int n) {
+      const int j = n & (kWave - 1);
+      if (j == 0) look(n);
+      const int page = __builtin_amdgcn_readlane(pages, j), first = __builtin_amdgcn_readlane(firsts, j);
+      const int sub = (first >> 5) & sub_mask;
+      const uint8_t* p = c.data + (static_cast<int64_t>(max(page, 0)) * c.hkv + kvh) * 2 * page_bytes;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int item = wr * kEach + k;
+        if (item < KC) {
+          const uint32_t chunk = HD >= 16 * G ? item * G + grp : min(grp, HD / 16 - 1);
+          raw[k] = *reinterpret_cast<const u32x4*>(p + (((chunk << c.plog) + sub * kCacheBlock + key_of(0)) << 4));
+        } else if (item < kItems) {
+          raw[k] = *reinterpret_cast<const u32x4*>(p + page_bytes + (((sub * 2 + grp) * HD + (item - KC) * M + col) << 4));
+        }
       }
-      if (key0 < 0) continue;  // a page that is not there
-    } else {
-      scale = make_float2(1.0f, 1.0f);
-      scores_open(p, k0);
+      return Step{page >= 0 ? first : -1, lane_value(scales.x, j), lane_value(scales.y, j)};
+    };
+    auto place = [&](int n, const Step& x) {
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int item = wr * kEach + k;
+        if (item >= kItems) continue;
+        const bool keys = item < KC;
+        bf16x8* to = operands[n & 1] + (keys ? 2 * item : 2 * KC + item - KC) * kWave + lane;
+        const float vs = keys ? 1.0f : x.vs;
+        to[0] = codes8<E4M3>(raw[k][0], raw[k][1], vs);
+        to[(keys ? 1 : DT) * kWave] = codes8<E4M3>(raw[k][2], raw[k][3], vs);
+      }
+    };
+    const int furthest = __builtin_amdgcn_readlane(rp.limit, M - 1);  // keys that any row of the wave sees
+    Step now{}, next{};
+    if (full_steps > 0) {
+      now = fetch(0);
+      place(0, now);
+      if (full_steps > 1) next = fetch(1);
     }
-    const bool masked = !coded || key0 + kCacheBlock > least;
-    soften<T>(st, p, rp, capped, sloped, scale.x, scale.y, key0 + grp * NS, masked);
-    bf16x8 pf[NU][NP];
-    pieces(p, pf);
-    if (coded) output_coded(pf);
-    else output_open(pf, k0);
+    for (s = 0; s < full_steps; ++s) {
+      __syncthreads();  // this step's operands are there, the other place has been read
+      const Step at = now;
+      now = next;
+      if (s + 1 < full_steps) place(s + 1, next);
+      if (s + 2 < full_steps) next = fetch(s + 2);
+      if (at.first < 0 || at.first >= furthest) continue;
+      const bf16x8* from = operands[s & 1] + lane;
+      typename S::acc sc = {};
+#pragma unroll
+      for (int i = 0; i < 2 * KC; ++i) {
+        const bf16x8 kf[1] = {from[i * kWave]};
+        sc = mma_pieces<M>(kf, qf[i], sc);
+      }
+      float p[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) p[i] = sc[i];
+      soften<T, !E4M3>(st, p, rp, capped, sloped, at.ks, at.vs, at.first + grp * NS, at.first + kCacheBlock > least);
+      bf16x8 pf[NU][NP];
+      pieces(p, pf);
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int x = 0; x < DT; ++x) {
+          const bf16x8 vf[1] = {from[(2 * KC + u * DT + x) * kWave]};
+          st.acc[x] = mma_pieces<M>(vf, pf[u], st.acc[x]);
+        }
+    }
+  } else {
+    int j = 0;
+    if (wk < full_steps) {
+      look(wk);
+      load_keys(0);
+    }
+    for (; s < (kShared ? steps : full_steps); s += WK) {
+      const bool coded = !kShared || s < full_steps;  // wave-uniform
+      const int k0 = (s - full_steps) * kCacheBlock;
+      int key0 = t.closed + k0;
+      float p[NS];
+      if (coded) {
+        key0 = load_values(j);
+        scores_coded(p);
+        // the next keys into the same registers, under the softmax and the second product
+        if (s + WK < full_steps) {
+          j = j + 1 == kWave ? 0 : j + 1;
+          if (j == 0) look(s + WK);
+          load_keys(j);
+        }
+        if (key0 < 0) continue;  // a page that is not there
+      } else {
+        scale = make_float2(1.0f, 1.0f);
+        scores_open(p, k0);
+      }
+      const bool masked = !coded || key0 + kCacheBlock > least;
+      soften<T, !E4M3>(st, p, rp, capped, sloped, scale.x, scale.y, key0 + grp * NS, masked);
+      bf16x8 pf[NU][NP];
+      pieces(p, pf);
+      if (coded) output_coded(pf);
+      else output_open(pf, k0);
+    }
   }
   if (!kShared)
     for (; s < steps; s += WK) {
       const int k0 = (s - full_steps) * kCacheBlock;
       float p[NS];
       scores_open(p, k0);
-      soften<T>(st, p, rp, capped, sloped, 1.0f, 1.0f, t.closed + k0 + grp * NS, true);
+      soften<T, false>(st, p, rp, capped, sloped, 1.0f, 1.0f, t.closed + k0 + grp * NS, true);
       bf16x8 pf[NU][NP];
       pieces(p, pf);
       output_open(pf, k0);
@@ -755,7 +854,7 @@ hipError_t run_width(const CacheAttn& a, hipStream_t s) {
 constexpr int64_t kSplitBlocks = 1536, kFewTileBlocks = 512, kFewTiles = 64;
 // Tiles of 128 rows: two rounds of two blocks a CU, each more parts to join (chunks of
 // 33 to 257 queries over 2000 to 8191 keys: 91 us with 512, 90 with 1024, 93 with 1536).
-constexpr int64_t kWideBlocks = 1024;
+constexpr int64_t kWideBlocks = 768;
 constexpr int64_t kLeastChunk = 32 * kPartBlocks;
 constexpr size_t kMostPartBytes = size_t(256) << 20;
 

@@ -83,16 +83,17 @@ __device__ inline uint32_t pack_i8(uint32_t x) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // whole numbers: no rounding
 }
 
-// Eight codes as bf16: both kinds are exact there.
+// Eight codes as bf16, where both kinds are exact; e4m3 times a power of two, which
+// the conversion takes along.
 template <bool E4M3>
-__device__ inline bf16x8 codes8(uint32_t lo, uint32_t hi) {
+__device__ inline bf16x8 codes8(uint32_t lo, uint32_t hi, float scale) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   u32x4 w;
   if (E4M3) {
-    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   } else {
     w[0] = pack_i8<0>(lo);
     w[1] = pack_i8<1>(lo);
