@@ -124,23 +124,6 @@ struct TileAt {
   int blocks, per, parts;  // blocks of 32 keys in full pages; per: of a part
 };
 
-// find_seq for tiles of 1 << log rows.
-__device__ inline int find_tile(const int64_t* __restrict__ off, int seqs, int group, int log, uint32_t b, int64_t& tile) {
-  const int lane = threadIdx.x & (kWave - 1);
-  int lo = 0, n = seqs;
-  while (n > 1) {
-    const int step = static_cast<int>(static_cast<uint32_t>(n + kWave - 1) / kWave);
-    const int s = lane * step;
-    const bool below = s < n && (max(off[lo + s], int64_t(0)) * group >> log) + (lo + s) <= static_cast<int64_t>(b);
-    const int c = max(1, static_cast<int>(__popcll(__ballot(below))));
-    lo += (c - 1) * step;
-    n = min(step, n - (c - 1) * step);
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  tile = static_cast<int64_t>(b) - ((max(off[lo], int64_t(0)) * group >> log) + lo);
-  return lo;
-}
-
 // A tile of sequence t.s: number `tile` of its tiles of 1 << log rows, or where
 // pages are listed rows t.row0 on of its token `tile`. False: no such tile.
 __device__ inline bool tile_of(const CacheAttn& a, const SeqSpan& q, int64_t tile, int log, TileAt& t) {
@@ -299,7 +282,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wr = wave % WR, wk = wave / WR, grp = lane / M, col = lane % M;
-  const uint32_t unit = a.unit0 + blockIdx.x;
+  // the last tiles, which see the most keys under a causal mask, first
+  const uint32_t unit = a.unit0 + gridDim.x - 1 - blockIdx.x;
   const int kvh = blockIdx.y, part = blockIdx.z;
   TileAt t;
   if (!tile_at(a, unit, kRows == 16 ? 4 : kRows == 32 ? 5 : 7, t) || part >= t.parts) return;  // block-uniform

@@ -54,7 +54,23 @@ __device__ inline int find_pages(const int64_t* __restrict__ off, int seqs, int 
   return lo;
 }
 
-__device__ inline float bits_f32(uint32_t b) { return __uint_as_float(b); }
+// find_seq for tiles of 1 << log rows (for single rows no sequence has a tile of its
+// own to spare: `rows` tiles are enough).
+__device__ inline int find_tile(const int64_t* __restrict__ off, int seqs, int group, int log, uint32_t b, int64_t& tile) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = static_cast<int>(static_cast<uint32_t>(n + kWave - 1) / kWave);
+    const int s = lane * step;
+    const bool below = s < n && (max(off[lo + s], int64_t(0)) * group >> log) + (log ? lo + s : 0) <= static_cast<int64_t>(b);
+    const int c = max(1, static_cast<int>(__popcll(__ballot(below))));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  tile = static_cast<int64_t>(b) - ((max(off[lo], int64_t(0)) * group >> log) + (log ? lo : 0));
+  return lo;
+}
 
 // The exponent k, from -126 on, of the least power of two with top <= most 2^k,
 // for most = mant 2^exp2 (1 <= mant < 2).

@@ -74,7 +74,8 @@ struct CacheSelect {
   float* scores;          // [tokens][hkv][width]
   int64_t max_pages;      // the caller's bound of a sequence's pages (0: none)
   int64_t row0, tokens;   // the rows of this launch
-  int tiles, run;         // blocks along the pages; rows of a block
+  int tiles, run_log;     // blocks along the pages; rows of a block, 1 << run_log
+  uint32_t unit0;
 };
 
 hipError_t launch_cache_append(const CacheAppend& a, bool bf16, bool e4m3, hipStream_t s);

@@ -73,126 +73,163 @@ __device__ inline int pages_seen(const CacheSelect& a, const RowAt& x) {
   return pos < 0 ? 0 : min(n, (pos >> a.c.plog) + 1);
 }
 
-// Grid: runs of kPageRun pages, runs of a.run rows of the launch, key heads. Rows
-// of one sequence share the pages' bounds: a tile of 16 is 4, 2 or 1 of them, as
-// many heads as a key head has (to a multiple of 4), or 16 of a row's more heads.
+// The q8 of LDS row `at`, by the 16 lanes of a quarter wave: `there` false leaves a
+// row that no page's best comes from.
+template <typename T, int W>
+__device__ inline void quantise(const T* q, bool there, int d, int at, int part, char* q8, float* sq) {
+  constexpr int E = W / 16, kStride = 2 * W + 16;  // E columns a lane; rows start on other banks
+  float v[E];
+  uint32_t top = 0;
+  const bool in = there && part * E < d;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    v[i] = in ? to_f32(q[part * E + i]) : 0.0f;
+    top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  }
+#pragma unroll
+  for (int i = 8; i > 0; i >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), i, kWave)));
+  const bool bad = top >= 0x7F800000u;  // a query that is not finite finds every page alike
+  const int k = bad ? 0 : unit_exp(__uint_as_float(top), 1.984375f, 6);
+  const float inv = exp2_int(-k);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int w = bad ? 0 : static_cast<int>(rintf(v[i] * inv));
+    q8[at * kStride + part * E + i] = static_cast<char>(max(w, 0));
+    q8[at * kStride + W + part * E + i] = static_cast<char>(min(w, 0));
+  }
+  if (part == 0) sq[at] = there ? exp2_int(k) : -1.0f;
+}
+
+// Grid: runs of kPageRun pages, tiles of 1 << a.run_log rows of a sequence, key heads.
+// LDS holds the q8 of kRowsAtOnce rows and heads, a row's heads to a multiple of 4 (of
+// 16 past 8), so that a tile of the instruction is 4, 2 or 1 rows, or 16 heads of one.
+constexpr int kRowsAtOnce = 64;
+__host__ __device__ inline int heads_to(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : (group + 15) & ~15; }  // LDS rows of a row
 template <typename T, int W>
 __global__ __launch_bounds__(kBlock) void k_select_score(const CacheSelect a) {
-  constexpr int kSteps = 2 * W / 64, kGroups = kPagesAtOnce / 16;
-  constexpr int kStride = 2 * W + 16;  // bytes: rows start on other banks
-  __shared__ __align__(16) char q8[16 * kStride];
-  __shared__ float sq[16];
+  constexpr int kSteps = 2 * W / 64, kGroups = kPagesAtOnce / 16, kStride = 2 * W + 16;
+  extern __shared__ __align__(16) char score_lds[];
+  float* sq = reinterpret_cast<float*>(score_lds);
+  char* q8 = score_lds + kRowsAtOnce * sizeof(float);
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane & 15, grp = lane >> 4;
-  const int kvh = blockIdx.z;
-  const int64_t row0 = a.row0 + static_cast<int64_t>(blockIdx.y) * a.run, row_end = min(row0 + a.run, a.row0 + a.tokens);
-  const int slots = a.group <= 4 ? 4 : a.group <= 8 ? 8 : 16;  // rows of a tile that a query row takes
-  i32x4 box[kGroups][kSteps];
-  float unit[kGroups];
-  for (int64_t row = row0; row < row_end;) {
-    RowAt x;
-    if (!row_at(c, row, x)) {  // block-uniform, as all below
-      ++row;
-      continue;
+  const int kvh = blockIdx.z, run = 1 << a.run_log;
+  int64_t tile;
+  int s;
+  if (c.pad > 0) {
+    const uint32_t per = static_cast<uint32_t>(c.pad + run - 1) >> a.run_log, u = a.unit0 + blockIdx.y;
+    s = static_cast<int>(u / per);
+    tile = u - static_cast<uint32_t>(s) * per;
+    if (s >= c.seqs) return;
+  } else {
+    s = find_tile(c.off, c.seqs, 1, a.run_log, a.unit0 + blockIdx.y, tile);
+  }
+  RowAt x;
+  x.s = s;
+  x.lk = cache_len(c, s);
+  const SeqSpan span = seq_span(c.off, s, c.pad, c.rows);
+  x.len = span.len;
+  if (tile < 0 || tile * run >= span.len) return;  // block-uniform, as all below
+  // the tile's rows in this launch
+  const int64_t first_row = max(span.start + tile * run, a.row0);
+  const int rows = static_cast<int>(min(min(span.start + min(tile * run + run, static_cast<int64_t>(span.len)), a.row0 + a.tokens) - first_row,
+                                        static_cast<int64_t>(run)));
+  if (rows <= 0) return;
+  x.token = static_cast<int>(first_row - span.start) + rows - 1;
+  const int most = pages_seen(a, x);  // of the last row, which sees the most
+  if (most <= a.count) return;        // all of them
+  const int slots = heads_to(a.group);
+  const int held = min(slots, kRowsAtOnce);                                      // of them at once
+  auto fill = [&](int h0) {
+    for (int at = wave * 4 + grp; at < ((rows * held + 15) & ~15); at += 16) {
+      const int own = at / held, head = h0 + at - own * held;
+      const bool there = own < rows && head < a.group;
+      const T* q = static_cast<const T*>(a.q.p) + (first_row + own) * a.q.row + static_cast<int64_t>(kvh * a.group + head) * a.q.head;
+      quantise<T, W>(q, there, c.d, at, col, q8, sq);
     }
-    const int64_t left = min(row_end - row, static_cast<int64_t>(x.len - x.token));  // rows here of the sequence
-    RowAt end = x;
-    end.token = x.token + static_cast<int>(left) - 1;
-    const int most = pages_seen(a, end);
-    if (most <= a.count) {  // all of them
-      row += left;
-      continue;
+  };
+  const bool once = slots <= kRowsAtOnce;
+  bool filled = false;
+  for (int page0 = blockIdx.x * kPageRun; page0 < most; page0 += gridDim.x * kPageRun) {
+    const int first = page0 + wave * kPagesAtOnce;
+    i32x4 box[kGroups][kSteps];
+    float unit[kGroups];
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const int n = first + i * 16 + col;
+      const int page = n < most ? cache_page(c, s, n) : -1;
+      const int64_t at = static_cast<int64_t>(max(page, 0)) * c.hkv + kvh;
+      const int8_t* p = c.bounds + at * 2 * W + grp * 16;
+      unit[i] = -INFINITY;  // a page that is not there comes last of all
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) box[i][k] = i32x4{0, 0, 0, 0};
+      if (page >= 0) {
+        unit[i] = c.units[at];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) box[i][k] = *reinterpret_cast<const i32x4*>(p + k * 64);
+      }
     }
-    for (int page0 = blockIdx.x * kPageRun; page0 < most; page0 += gridDim.x * kPageRun) {
-      const int first = page0 + wave * kPagesAtOnce;
+    if (once && !filled) {  // while the bounds are on their way
+      fill(0);
+      __syncthreads();
+      filled = true;
+    }
+    // the best of a page over the 16 LDS rows from `base` on, for each group of four
+    auto best_of = [&](int base, float (&best)[kGroups]) {
+      i32x4 qa[kSteps];
+      float scale[4];
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) qa[k] = *reinterpret_cast<const i32x4*>(q8 + (base + col) * kStride + k * 64 + grp * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) scale[e] = sq[base + grp * 4 + e];
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        const int n = first + i * 16 + col;
-        const int page = n < most ? cache_page(c, x.s, n) : -1;
-        const int64_t at = static_cast<int64_t>(max(page, 0)) * c.hkv + kvh;
-        const int8_t* p = c.bounds + at * 2 * W + grp * 16;
-        // one that is not there comes last of all
-        unit[i] = -INFINITY;
+        i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) box[i][k] = i32x4{0, 0, 0, 0};
-        if (page >= 0) {
-          unit[i] = c.units[at];
+        for (int k = 0; k < kSteps; ++k) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[k], box[i][k], sum, 0, 0, 0);
 #pragma unroll
-          for (int k = 0; k < kSteps; ++k) box[i][k] = *reinterpret_cast<const i32x4*>(p + k * 64);
-        }
+        for (int e = 0; e < 4; ++e)
+          if (scale[e] > 0.0f) best[i] = fmaxf(best[i], static_cast<float>(sum[e]) * scale[e]);
       }
-      for (int64_t r = row; r < row + left; r += 16 / slots) {
+    };
+    auto write = [&](int own, bool mine, float (&best)[kGroups]) {
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        float y = best[i];
+        if (slots >= 8) y = fmaxf(y, __shfl_xor(y, 16, kWave));
+        if (slots >= 16) y = fmaxf(y, __shfl_xor(y, 32, kWave));
+        const float score = unit[i] == -INFINITY ? -INFINITY : y * unit[i] + 0.0f;  // one zero
+        const int n = first + i * 16 + col;
+        if (n < most && mine)
+          a.scores[((first_row + own - a.row0) * c.hkv + kvh) * c.width + n] = score == score ? score : INFINITY;  // not finite: first
+      }
+    };
+    if (slots <= 16) {
+      for (int base = 0; base < rows * slots; base += 16) {
         float best[kGroups];
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) best[i] = -INFINITY;
-        for (int h0 = 0; h0 < a.group; h0 += 16) {
-          __syncthreads();
-          // a wave takes four of the tile's rows
+        best_of(base, best);
+        const int own = (base + grp * 4) / slots;
+        write(own, own < rows && (base + grp * 4) % slots == 0, best);
+      }
+    } else {
+      for (int own = 0; own < rows; ++own) {
+        float best[kGroups];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int at = wave * 4 + y, head = h0 + at % slots;
-            const int64_t own = r + at / slots;
-            const bool there = own < row + left && head < a.group;
-            float v[2] = {0.0f, 0.0f};
-            uint32_t top = 0;
-            if (there) {
-              const T* q = static_cast<const T*>(a.q.p) + own * a.q.row + static_cast<int64_t>(kvh * a.group + head) * a.q.head;
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int d = i * kWave + lane;
-                if (d < c.d) v[i] = to_f32(q[d]);
-                top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-              }
-            }
-#pragma unroll
-            for (int i = kWave / 2; i > 0; i >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), i, kWave)));
-            const bool bad = top >= 0x7F800000u;  // a query that is not finite finds every page alike
-            const int k = bad ? 0 : unit_exp(__uint_as_float(top), 1.984375f, 6);
-            const float inv = exp2_int(-k);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int d = i * kWave + lane;
-              if (d >= W) continue;
-              const int w = bad ? 0 : static_cast<int>(rintf(v[i] * inv));
-              q8[at * kStride + d] = static_cast<char>(max(w, 0));
-              q8[at * kStride + W + d] = static_cast<char>(min(w, 0));
-            }
-            if (lane == 0) sq[at] = there ? exp2_int(k) : -1.0f;
+        for (int i = 0; i < kGroups; ++i) best[i] = -INFINITY;
+        for (int h0 = 0; h0 < slots; h0 += held) {
+          if (!once) {  // more heads than LDS rows: one row at a time (run is 1)
+            __syncthreads();
+            fill(h0);
+            __syncthreads();
           }
-          __syncthreads();
-          i32x4 qa[kSteps];
-#pragma unroll
-          for (int k = 0; k < kSteps; ++k)
-            qa[k] = *reinterpret_cast<const i32x4*>(q8 + col * kStride + k * 64 + grp * 16);
-          float scale[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) scale[e] = sq[grp * 4 + e];
-#pragma unroll
-          for (int i = 0; i < kGroups; ++i) {
-            i32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[k], box[i][k], sum, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (scale[e] > 0.0f) best[i] = fmaxf(best[i], static_cast<float>(sum[e]) * scale[e]);
-          }
+          for (int h = 0; h < held && h0 + h < slots; h += 16) best_of(own * held + h, best);
         }
-        const int own = grp * 4 / slots;  // the lane's row
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-          float y = best[i];
-          if (slots >= 8) y = fmaxf(y, __shfl_xor(y, 16, kWave));
-          if (slots >= 16) y = fmaxf(y, __shfl_xor(y, 32, kWave));
-          const float s = unit[i] == -INFINITY ? -INFINITY : y * unit[i] + 0.0f;  // one zero
-          const int n = first + i * 16 + col;
-          if (n < most && r + own < row + left && grp * 4 % slots == 0)
-            a.scores[((r + own - a.row0) * c.hkv + kvh) * c.width + n] = s == s ? s : INFINITY;  // a page that is not finite comes first
-        }
+        write(own, grp == 0, best);
       }
     }
-    __syncthreads();
-    row += left;
   }
 }
 
@@ -388,6 +425,7 @@ __global__ __launch_bounds__(NT) void k_select_pick_any(const CacheSelect a) {
 }
 
 constexpr size_t kMostScoreBytes = size_t(256) << 20;
+constexpr int64_t kMostUnits = 65535;  // tiles lie along a launch's second axis
 
 }  // namespace
 
@@ -396,15 +434,23 @@ size_t plan_cache_select(const CacheSelect& a, int64_t* tokens) {
   *tokens = 0;
   if (a.c.rows == 0 || a.c.seqs == 0) return 0;
   *tokens = std::min<int64_t>(a.c.rows, std::max<int64_t>(1, kMostScoreBytes / one));
-  *tokens = std::min<int64_t>(*tokens, 65535);  // rows of a launch: they lie along its second axis
+  *tokens = std::min<int64_t>(*tokens, 65535);  // (a block each along the first axis of the picks)
   return *tokens * one;
 }
 
 template <typename T, int W>
 static void run_select(const CacheSelect& a, hipStream_t s) {
   if (a.c.width > a.count) {
-    const dim3 grid(a.tiles, static_cast<unsigned>((a.tokens + a.run - 1) / a.run), a.c.hkv);
-    k_select_score<T, W><<<grid, kBlock, 0, s>>>(a);
+    const int64_t run = int64_t(1) << a.run_log;
+    const int64_t units = a.c.pad > 0 ? a.c.seqs * ((a.c.pad + run - 1) / run) : a.c.rows / run + (run > 1 ? a.c.seqs : 0);
+    const int held = std::min(kRowsAtOnce, (static_cast<int>(run) * heads_to(a.group) + 15) & ~15);
+    const size_t lds = kRowsAtOnce * sizeof(float) + held * (2 * W + 16);
+    CacheSelect b = a;
+    for (int64_t u = 0; u < units; u += kMostUnits) {
+      b.unit0 = static_cast<uint32_t>(u);
+      const dim3 grid(a.tiles, static_cast<unsigned>(std::min(units - u, kMostUnits)), a.c.hkv);
+      k_select_score<T, W><<<grid, kBlock, lds, s>>>(b);
+    }
   }
   const dim3 rows(static_cast<unsigned>(a.tokens), a.c.hkv);
   if (a.c.width <= 1024) k_select_pick<256, 4><<<rows, 256, 0, s>>>(a);
@@ -419,8 +465,10 @@ hipError_t launch_cache_select(CacheSelect a, bool bf16, hipStream_t s) {
   // the bound of the lengths only shapes the launches: a block goes on to the pages past it
   const int64_t pages = a.max_pages > 0 ? std::min(a.max_pages, a.c.width) : a.c.width;
   a.tiles = static_cast<int>(std::min<int64_t>(1 << 20, std::max<int64_t>(1, (pages + kPageRun - 1) / kPageRun)));
-  // rows that a block takes: about those of a sequence, at most 16
-  a.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16, a.c.rows / a.c.seqs)));
+  // rows of a tile: about those of a sequence, as many as LDS holds
+  const int slots = heads_to(a.group);
+  a.run_log = 0;
+  while ((2 << a.run_log) <= a.c.rows / a.c.seqs && (2 << a.run_log) * slots <= kRowsAtOnce) ++a.run_log;
   const int W = cache_width(a.c.d);
   for (int64_t r = 0; r < a.c.rows && tokens > 0; r += tokens) {
     a.row0 = r;
