@@ -14,6 +14,15 @@
 // cut into calls.  A page's tokens stay in LDS between the rotation, the
 // maximum and the codes: inputs are read once and codes written once, in whole
 // 1 KiB stores a wave.
+//
+// 24 histories of 17 to 8191 tokens (93 thousand rows of 8 query and 2 key heads of
+// 128, bf16 to e4m3 with bounds, 524 MB moved): 125 us, 4.2 TB/s, where a plain copy
+// of the queries' 380 MB takes 72. Query rows alone take 72 us, pages alone 54 to 64:
+// a page waits for one thing after another (its sequence, its place, its tokens, then
+// four steps with barriers between), and keys turn at 14 us of those. Blocks of
+// both kinds mixed in the grid, the next row loaded a step ahead, angles without
+// LDS bank conflicts: no change, 126 to 128. One token of 256 users: 9.6 us, bound by
+// latency. Reading the 24 histories back (143 MB moved): 25 us, 5.7 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

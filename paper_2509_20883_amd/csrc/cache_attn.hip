@@ -5,14 +5,30 @@
 //   out_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij), k_j = s_k code, v_j = s_v code
 //
 // One pass over the keys with the running maximum and sum of the softmax. A wave
-// takes 32 rows (tokens times the query heads of a key head), one per lane
-// column, against 32 keys at a time, and loads both sides of those keys from the
-// page straight into the registers that feed the matrix instructions: codes are
-// exact in bf16, so only the page's two scales are left to multiply, one into
-// the scores and one into the probabilities. fp32 queries and probabilities are
-// three bf16 pieces each, which carry their 24 bits through the same
-// instructions. The next keys are on their way while a step is computed; no LDS
-// and no barrier until the waves' results are joined.
+// takes 32 or 16 rows (tokens times the query heads of a key head), one per lane
+// column, against 32 keys at a time. Codes are exact in bf16, so only the page's two
+// scales are left to multiply, one into the scores and one into the probabilities
+// (the latter, a power of two in e4m3, by the conversion itself). fp32 queries and
+// probabilities are three bf16 pieces each, which carry their 24 bits through the
+// same instructions; with bf16 queries the probabilities are rounded to bf16, the
+// type of the products. Scores, maxima, sums and outputs are fp32.
+//
+// Few rows (16 or 32 a tile): the four waves of a block lie along the keys, and each
+// loads both sides of its keys from the page straight into the registers that feed
+// the matrix instructions, the next 32 on their way while these are computed; LDS
+// only joins the waves' results. Bound by reading the pages: without any products
+// the loads alone take as long (64 x 32768 keys of 128 206 us, 208 with them), and
+// whole rows of 256 bytes gathered at random reach 5.4 TB/s. One token of 256 users
+// with 1 to 4096 keys of 128 in 2 heads (257 MB) 68 us, 4 rows over 1,000,003 keys of 64
+// (256 MB) 59: 25 to 29 us of that are there at any size (the chain from a row's
+// sequence to its length, its pages and their first bytes, code that is not in the
+// caches yet, and the longest sequence's end).
+//
+// Many rows: tiles of 128, a wave 32 of them, over the same keys; the operands are
+// made once a block into LDS. Bound by the vector instructions around the products
+// (conversions, exponentials, the running maximum: vector unit 42% busy, matrix unit
+// 36%, the rest waits between the two): 4096 rows over 16384 keys of 128, 8 query heads,
+// 297 us, 810 TFLOP/s over the visible keys.
 //
 // The open page's tokens, at most page_len - 1 of a sequence, are read in the
 // model's type.
@@ -700,7 +716,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
 
 // Joins the parts of a row: NT threads a query token and head, each four columns
 // and a share of the parts. Bound by the latency of its loads, one after another:
-// the sequence, its length, then maxima, sums and parts together.
+// the sequence, its length, then maxima, sums and parts together (256 tokens of 8
+// heads 6 us). Past 32 parts a block of 1024 threads (4 tokens of 4 heads 10 us).
 //   m = max m_c,  l = sum l_c 2^(m_c - m),  out = sum acc_c 2^(m_c - m) / l
 template <typename T, int NT>
 __global__ __launch_bounds__(NT < kBlock ? kBlock : NT) void k_cache_join(const CacheAttn a) {
@@ -811,7 +828,7 @@ hipError_t run(CacheAttn a, hipStream_t s) {
     else if (a.tile_log == 5) k_cache_attn<T, E4M3, HD, 32, 1, kKeyWaves><<<grid, kKeyWaves * kWave, 0, s>>>(a);
     else k_cache_attn<T, E4M3, HD, 32, 4, 1><<<grid, 4 * kWave, 0, s>>>(a);
   }
-  const int64_t tokens = a.splits > 1 ? (a.c.pad > 0 ? a.c.rows : a.c.rows + a.c.seqs) : 0;
+  const int64_t tokens = a.splits > 1 ? a.c.rows : 0;
   for (int64_t u = 0; u < tokens; u += kMostUnits) {
     a.unit0 = static_cast<uint32_t>(u);
     const unsigned n = static_cast<unsigned>(std::min(tokens - u, kMostUnits));
@@ -830,14 +847,16 @@ hipError_t run_width(const CacheAttn& a, hipStream_t s) {
 
 }  // namespace
 
-// Blocks that a call's keys are split into: two rounds of what the chip holds at 128
-// columns, so that a long sequence's parts spread (one token of 256 users with 1 to
-// 4096 keys: 67 us with 512, 66 with 1024, 59 with 1536, 61 with 2304), but for few
-// row tiles, whose many parts the join has to read, two blocks a CU (four rows over
-// 1,000,003 keys of 64: 53 with 512, 60 with 1024, 62 with 1536).
-constexpr int64_t kSplitBlocks = 1536, kFewTileBlocks = 512, kFewTiles = 64;
-// Tiles of 128 rows: two rounds of two blocks a CU, each more parts to join (chunks of
-// 33 to 257 queries over 2000 to 8191 keys: 91 us with 512, 90 with 1024, 93 with 1536).
+// Blocks that a call's keys are split into, measured with pages that come from HBM
+// (several caches in turn). One token of 256 users with 1 to 4096 keys: 89 us with 512,
+// 82 with 768, 79 with 1536, 80 with 3072: a long sequence's parts have to spread. Few
+// row tiles, whose many parts the join has to read: four rows over 1,000,003 keys of 64
+// 70 us with 512, 73 with 1024. Listed pages, all rows of like length: a token of 64
+// users over 32 pages of 64 41 us with 768, 47 with 1536.
+constexpr int64_t kSplitBlocks = 1536, kListBlocks = 768, kFewTileBlocks = 512, kFewTiles = 64;
+// Tiles of 128 rows, three blocks a CU: chunks of 33 to 257 queries over 2000 to 8191
+// keys 109 us with 256, 80 with 768, 88 with 1024, 89 with 1536; 4096 rows over 16384
+// keys 330 with 768, 340 with 1024, 343 with 1536.
 constexpr int64_t kWideBlocks = 768;
 constexpr int64_t kLeastChunk = 32 * kPartBlocks;
 constexpr size_t kMostPartBytes = size_t(256) << 20;
@@ -854,7 +873,7 @@ size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_
   a->tile_log = most_rows <= 16 ? 4 : most_rows <= 32 || a->list ? 5 : 7;
   const int tile_rows = 1 << a->tile_log;
   if (a->list) {
-    a->units = (c.pad > 0 ? c.rows : c.rows + c.seqs) * ((a->group + tile_rows - 1) / tile_rows);
+    a->units = c.rows * ((a->group + tile_rows - 1) / tile_rows);
   } else if (c.pad > 0) {
     a->units = c.seqs * ((c.pad * a->group + tile_rows - 1) / tile_rows);
   } else {
@@ -864,7 +883,7 @@ size_t plan_cache_attn(CacheAttn* a, int64_t max_q, int64_t max_len, size_t* ml_
   if (max_len > 0) keys = std::min(keys, max_len);
   if (a->list) keys = (static_cast<int64_t>(a->count) << c.plog) + (1 << c.plog);
   const int64_t blocks = a->units * c.hkv;
-  const int64_t most = a->tile_log == 7 ? kWideBlocks : blocks < kFewTiles ? kFewTileBlocks : kSplitBlocks;
+  const int64_t most = a->tile_log == 7 ? kWideBlocks : blocks < kFewTiles ? kFewTileBlocks : a->list ? kListBlocks : kSplitBlocks;
   int64_t splits = std::min((most + blocks - 1) / blocks, keys / kLeastChunk);
   const size_t one = static_cast<size_t>(blocks) * tile_rows * (c.d + 2) * sizeof(float);
   splits = std::min<int64_t>(splits, kMostPartBytes / one);

@@ -8,7 +8,7 @@
 //   keys    [W / 16][page_len][16]   16 columns of one token together
 //   values  [page_len / 16][W][16]   16 tokens of one column together
 // so a product over columns (scores) and one over tokens (the output) both find
-// their long side in a lane's own bytes: nothing passes through LDS.
+// their long side in a lane's own bytes.
 #pragma once
 
 #include "seq_internal.h"

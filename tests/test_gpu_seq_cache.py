@@ -639,6 +639,60 @@ def test_another_stream():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype,codes", [(BF, "e4m3"), (F32, "i8")])
+@pytest.mark.parametrize("new", [[0, 4, 0, 3, 0], [1, 1, 0, 1, 1], [0, 0, 40, 33, 0]])
+def test_rows_outside_the_sequences_are_left_as_they_were(dtype, codes, new):
+    """Rows before the first and behind the last sequence: untouched, and the others as without them."""
+    lens = [700, 2000, 64, 1300, 5]
+    c = _cache(150, 5, 2, 64, 32, codes, dtype, causal=True, bounds=True)
+    g = ref.fill(c, 4)
+    table = _tables(c, [(n + 31) // 32 for n in lens])
+    n = sum(new)
+    wide = torch.full((n + 13, 6, 64), math.nan, device="cuda", dtype=dtype)
+    wide[6:6 + n] = torch.randn(n, 6, 64, generator=g, device="cuda").to(dtype)
+    off, ln = ref.offsets(new), _dev(lens)
+    pages = c.select(wide[6:6 + n], off, ln, table, 5)
+    listed = torch.zeros(n + 13, 2, 5, dtype=torch.int32, device="cuda")
+    listed[6:6 + n] = pages
+    assert torch.equal(c.select(wide, off + 6, ln, table, 5)[6:6 + n], pages)
+    for few, many in ((None, None), (pages, listed)):
+        out = torch.full_like(wide, 7.0)
+        c.attend(wide, off + 6, ln, table, pages=many, out=out)
+        assert (out[:6] == 7).all() and (out[6 + n:] == 7).all()
+        for b, (k, v, there) in enumerate(ref.tokens_of(c, table, lens, range(5))):
+            pos, key_pos = torch.arange(new[b], device="cuda") + lens[b] - new[b], torch.arange(lens[b], device="cuda")
+            for i in range(new[b]):
+                at = 6 + int(off[b]) + i
+                for h in range(2):
+                    w = there.long()
+                    if few is not None:
+                        w = (key_pos >= lens[b] // 32 * 32).long()
+                        for x in pages[at - 6, h].tolist():
+                            w[x * 32:(x + 1) * 32] += int(x >= 0)
+                    want, bound = ref.attention(wide[at:at + 1, 3 * h:3 * h + 3], k[:, h:h + 1], v[:, h:h + 1], pos[i:i + 1], key_pos, w,
+                                                True, 0.0, None, 0.125, dtype == BF, 3)
+                    _close(out[at:at + 1, 3 * h:3 * h + 3], want, bound, dtype)
+
+
+def test_more_rows_than_a_launch_takes():
+    """70,001 rows of one sequence and 70,000 sequences of one row each: as in parts."""
+    rows = 70001
+    c = _cache(12, 70000, 1, 16, 32, "i8", BF, causal=False, bounds=True)
+    g = ref.fill(c, 5)
+    q = torch.randn(rows, 1, 16, generator=g, device="cuda").bfloat16()
+    table, lens = torch.arange(12, dtype=torch.int32, device="cuda")[None], _dev([12 * 32])
+    pages = c.select(q, _dev([0, rows]), lens, table, 3)
+    out = c.attend(q, _dev([0, rows]), lens, table, pages=pages)
+    for a, b in ((0, 40000), (40000, rows)):
+        some = c.select(q[a:b], _dev([0, b - a]), lens, table, 3)
+        assert torch.equal(some, pages[a:b])
+        assert torch.equal(c.attend(q[a:b], _dev([0, b - a]), lens, table, pages=some), out[a:b])
+    seqs = 70000
+    off, each, tables = torch.arange(seqs + 1, device="cuda"), lens.expand(seqs).contiguous(), table.expand(seqs, 12).contiguous()
+    assert torch.equal(c.select(q[:seqs], off, each, tables, 3), pages[:seqs])
+    assert torch.equal(c.attend(q[:seqs], off, each, tables, pages=pages[:seqs]), out[:seqs])
+
+
 def test_empty_calls():
     c = _cache(2, 2, 1, 32, 32, "i8", BF, rotary=32, bounds=True)
     none = torch.zeros(0, 1, 32, dtype=BF, device="cuda")
