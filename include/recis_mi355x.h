@@ -569,7 +569,8 @@ rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k,
  *          power of two with max |k| <= 127 units, rounded outward.  Both NULL
  *          where pages are never selected
  * Pages and slots are the caller's to hand out.  Pages may be shared by
- * sequences that only read them. */
+ * sequences that only read them; a page or slot that two sequences of an append
+ * write, or that one call writes while another reads it, holds no defined values. */
 typedef enum { RS_CACHE_I8 = 0, RS_CACHE_E4M3 = 1 } rs_cache_codes;
 typedef struct {
   int32_t codes;     /* rs_cache_codes                                          */
@@ -647,9 +648,9 @@ rs_status seq_cache_read(const rs_seq_cache* c, const rs_cache_batch* b, const i
  * [count], page numbers of the sequence), row i of a key head sees only the keys
  * of those full pages and of the open page; entries that name no full page are
  * passed over, a page named twice counts twice.  A query without a key gets 0.
- * q may not be rotated any more; out is contiguous.  Scores, statistics and sums
- * are fp32; bf16 probabilities are rounded as operands of the matrix
- * instructions, fp32 ones keep 24 bits.
+ * q is as append turned it (as it is without rotation); out is contiguous and
+ * does not overlap q.  Scores, statistics and sums are fp32; bf16 probabilities
+ * are rounded as operands of the matrix instructions, fp32 ones keep 24 bits.
  * Workspace: seq_cache_attention_workspace_bytes(...), 256-byte aligned, free for
  * the next call once this one has completed in stream order; 0 for arguments the
  * call refuses, or where none is needed. */

@@ -844,6 +844,11 @@ class SeqCache(_Workspace):
             out = _like(q)
         elif out.shape != shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
             raise RecisError(EINVAL, "out must be a contiguous GPU tensor of q's shape and type")
+        elif out.numel():
+            es, at_out = out.element_size(), out.data_ptr()
+            last = (b.rows - 1) * d.q_stride + (shape[-2] - 1) * d.q_head_stride + self.head_dim
+            if at < at_out + out.numel() * es and at_out < at + last * es:
+                raise RecisError(EINVAL, "out must not overlap q")
         L = lib()
         need = L.seq_cache_attention_workspace_bytes(self._ref, b, d)
         ws = self._take(need, q) if need else None

@@ -674,6 +674,19 @@ def test_rows_outside_the_sequences_are_left_as_they_were(dtype, codes, new):
                     _close(out[at:at + 1, 3 * h:3 * h + 3], want, bound, dtype)
 
 
+def test_an_output_over_the_queries_is_refused():
+    c = _cache(2, 1, 1, 32, 32, "i8", BF)
+    ref.fill(c, 7)
+    table, off, lens = torch.zeros(1, 2, dtype=torch.int32, device="cuda"), _dev([0, 4]), _dev([40])
+    both = torch.randn(4, 4, 32, device="cuda").bfloat16()
+    for q, out in ((both, both), (both[:, :2], both.view(8, 2, 32)[4:]), (both.view(8, 2, 32)[:4], both.view(8, 2, 32)[3:7])):
+        with pytest.raises(R.RecisError, match="overlap"):
+            c.attend(q, off, lens, table, out=out)
+    halves = both.view(8, 2, 32)
+    want = c.attend(halves[:4].clone(), off, lens, table)
+    assert torch.equal(c.attend(halves[:4], off, lens, table, out=halves[4:]), want)
+
+
 def test_more_rows_than_a_launch_takes():
     """70,001 rows of one sequence and 70,000 sequences of one row each: as in parts."""
     rows = 70001
