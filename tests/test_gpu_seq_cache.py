@@ -546,6 +546,15 @@ def test_groups_of_heads_choose_together(hq, hkv, d, dtype):
 # ---------------------------------------------------------------------------
 
 
+@pytest.mark.parametrize("hq,hkv", [(100, 1), (260, 2)])
+@pytest.mark.parametrize("d,dtype", [(64, BF), (24, F32)])
+def test_many_heads_of_one_key_head(hq, hkv, d, dtype):
+    """More heads of a key head than a block holds at once: the choice and both attentions."""
+    test_groups_of_heads_choose_together(hq, hkv, d, dtype)
+    _attend_case(hq, hkv, d, 32, "i8", dtype, [300, 0, 70], [2, 1, 3], count=3, seed=21)
+    _attend_case(hq, hkv, d, 32, "e4m3", dtype, [300, 0, 70], [2, 1, 3], cap=7.0, slopes=True, seed=22)
+
+
 def test_a_served_history_against_seq_attention():
     """Histories written, read back and attended: the same as SeqAttention over the tokens read, to both sides' roundings."""
     g = torch.Generator(device="cuda").manual_seed(12)
