@@ -546,6 +546,21 @@ def test_groups_of_heads_choose_together(hq, hkv, d, dtype):
 # ---------------------------------------------------------------------------
 
 
+@pytest.mark.parametrize("width", [900, 3000])
+def test_counts_around_the_threads_of_a_block(width):
+    """The range of scores starts at the least of as many groups' largest: counts at and beside powers of two."""
+    c = _cache(width, 1, 1, 32, 32, "e4m3", BF, bounds=True, causal=False)
+    g = ref.fill(c, 9)
+    table = torch.randperm(width, generator=g, device="cuda").to(torch.int32)[None]
+    table[0, ::7] = -1  # pages that are not there come last
+    q = torch.randn(1, 3, 32, generator=g, device="cuda").bfloat16()
+    for count in (1, 2, 3, 4, 5, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 770, 800, 899, 1023, 1024, 1025,
+                  2047, 2572, 2999):
+        if count < width:
+            got = c.select(q, _dev([0, 1]), _dev([width * 32]), table, count)
+            assert got[0].tolist() == ref.select(q[0], c, table[0].tolist(), width * 32, 0, count, False), count
+
+
 @pytest.mark.parametrize("hq,hkv", [(100, 1), (260, 2)])
 @pytest.mark.parametrize("d,dtype", [(64, BF), (24, F32)])
 def test_many_heads_of_one_key_head(hq, hkv, d, dtype):
