@@ -322,7 +322,7 @@ __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64
     tile = b - s * per;
     if (s >= c.seqs) return;
   } else {
-    s = find_seq(c.off, c.seqs, 1, kTile, b, tile);
+    s = find_tile(c.off, c.seqs, 1, __builtin_ctz(kTile), static_cast<uint32_t>(b), tile);
   }
   const SeqSpan span = seq_span(c.off, s, c.pad, c.rows);
   const int64_t all = c.pad > 0 ? c.pad : int64_t(span.len), first = tile * kTile + wave * kTurnRows;

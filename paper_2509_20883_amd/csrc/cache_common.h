@@ -7,11 +7,6 @@
 
 namespace rs {
 
-struct CacheSeq {
-  int64_t start;  // the sequence's first row
-  int rows, len, slot;
-};
-
 // Tokens that sequence s holds: lens[s], cut to what its table can name.
 __device__ inline int cache_len(const CacheArgs& c, int s) {
   return static_cast<int>(min(max(c.lens[s], int64_t(0)), min(c.width << c.plog, int64_t(0x7FFFFF00))));
@@ -54,8 +49,9 @@ __device__ inline int find_pages(const int64_t* __restrict__ off, int seqs, int 
   return lo;
 }
 
-// find_seq for tiles of 1 << log rows (for single rows no sequence has a tile of its
-// own to spare: `rows` tiles are enough).
+// The sequence of block b and its tile there, for tiles of 1 << log rows: sequence s from
+// off[s] >> log on, and s more as each may end within a tile; single rows never do, so
+// there `rows` blocks are enough.
 __device__ inline int find_tile(const int64_t* __restrict__ off, int seqs, int group, int log, uint32_t b, int64_t& tile) {
   const int lane = threadIdx.x & (kWave - 1);
   int lo = 0, n = seqs;

@@ -29,8 +29,6 @@
 namespace rs {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagesAtOnce = 64;  // of a wave
