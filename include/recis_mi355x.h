@@ -595,10 +595,13 @@ typedef struct {
  * number; entries past a sequence's pages are not read.  slots int32 [seqs]
  * (NULL: slot s for sequence s).
  * Entries outside the cache are passed over: their tokens are neither written
- * nor seen, and read as 0.  validate != 0 in the calls below checks offsets,
- * lens, the table's entries in use and the slots on the host (and, where tokens
- * are written, that no page or slot is written twice); it copies them back:
- * synchronizing. */
+ * nor seen, and read as 0.  Without a slot the tokens of an open page are lost, and
+ * the page with them when it fills: it is passed over too (its scales are 0), while
+ * pages that one call fills whole need no slot.  An entry has to stay outside the
+ * cache once tokens came for it: put inside later, it holds no defined values.
+ * validate != 0 in the calls below checks offsets, lens, the table's entries in
+ * use and the slots on the host (and, where tokens are written, that no page or
+ * slot is written twice); it copies them back: synchronizing. */
 typedef struct {
   int64_t seqs, rows, pad; /* seqs < 2^24, rows < 2^31 - 1024                   */
   int64_t table_width;     /* at most 2^26                                      */

@@ -134,6 +134,20 @@ struct RotPairs {
   }
 };
 
+// A page that fills while its first tokens are gone (they came for a slot outside the
+// cache): what it held before, another sequence's maybe, goes, and a scale of 0, which
+// no page of tokens has, says that there is nothing to see.
+__device__ inline void lost_page(const CacheArgs& c, int page, int kvh, int side, int W) {
+  const int64_t at = static_cast<int64_t>(page) * c.hkv + kvh;
+  u32x4* data = reinterpret_cast<u32x4*>(c.data + cache_at(c, page, kvh, side, W));
+  for (int i = threadIdx.x; i < (W / 16) << c.plog; i += blockDim.x) data[i] = u32x4{0, 0, 0, 0};
+  if (threadIdx.x == 0) c.scales[at * 2 + side] = 0.0f;
+  if (side == 0 && c.bounds) {
+    for (int i = threadIdx.x; i < 2 * W; i += blockDim.x) c.bounds[at * 2 * W + i] = 0;
+    if (threadIdx.x == 0) c.units[at] = -INFINITY;  // chosen last, like a page that is not there
+  }
+}
+
 // Page number n of a sequence that holds tokens [held, end) after the call: coded
 // if it is full, else its new tokens put into the open page.
 template <typename T, bool E4M3, int NT>
@@ -151,7 +165,11 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
   const int old = static_cast<int>(max(held - first, int64_t(0)));               // tokens the open page holds
   const int last = static_cast<int>(min(end - first, static_cast<int64_t>(P)));  // tokens the page holds now
   const int page = full ? cache_page(c, s, n) : -1;
-  if ((full ? page < 0 : slot < 0) || (old > 0 && slot < 0)) return;  // block-uniform
+  if (full ? page < 0 : slot < 0) return;  // block-uniform
+  if (old > 0 && slot < 0) {
+    lost_page(c, page, kvh, side, W);
+    return;
+  }
 
   const int stride = lds_stride<T>(d), cpr = d / kPer;  // bytes, 16-byte chunks of a row
   const int cw = cpr <= 1 ? 1 : 1 << (32 - __builtin_clz(cpr - 1));

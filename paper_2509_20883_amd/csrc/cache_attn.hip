@@ -397,7 +397,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
   u32x4 kc[KT][KC];
   codes_t vc[DT];
   float2 scale = make_float2(0.0f, 0.0f);
-  // a page that is not there stands as page 0, and its step is left out
+  // a page that is not there stands as page 0, and its step is left out; so is that of
+  // a page whose tokens are lost (keys' scale 0, looked at where the scales are needed)
   auto load_keys = [&](int j) {
     const int page = max(__builtin_amdgcn_readlane(pages, j), 0), sub = (__builtin_amdgcn_readlane(firsts, j) >> 5) & sub_mask;
     const uint8_t* p = c.data + (static_cast<int64_t>(page) * c.hkv + kvh) * 2 * page_bytes;
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
       const uint32_t to = ((chunk * HD + x * M + col) << 4) + NS * grp % 16;
       vc[x] = *reinterpret_cast<const codes_t*>(p + to);
     }
-    return page >= 0 ? first : -1;
+    return page >= 0 && scale.x != 0.0f ? first : -1;
   };
   auto scores_coded = [&](float (&p)[NS]) {
     if (kRowsInLds) asm volatile("" ::: "memory");  // the rows are read again, not kept
@@ -540,7 +541,8 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
           raw[k] = *reinterpret_cast<const u32x4*>(p + page_bytes + (((sub * 2 + grp) * HD + (item - KC) * M + col) << 4));
         }
       }
-      return Step{page >= 0 ? first : -1, lane_value(scales.x, j), lane_value(scales.y, j)};
+      const float ks = lane_value(scales.x, j);
+      return Step{page >= 0 && ks != 0.0f ? first : -1, ks, lane_value(scales.y, j)};
     };
     auto place = [&](int n, const Step& x) {
 #pragma unroll

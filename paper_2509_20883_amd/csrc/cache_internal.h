@@ -20,10 +20,10 @@ constexpr int kCacheBlock = 32;  // tokens a wave takes at a time
 // The cache and the sequences of a call, as the kernels see them.
 struct CacheArgs {
   uint8_t* data;   // [pages][hkv][2][page_len * W]
-  float* scales;   // [pages][hkv][2]
+  float* scales;   // [pages][hkv][2], both 0: tokens lost, a page that is passed over
   void* open;      // [slots][2][hkv][2][page_len][d]
   int8_t* bounds;  // [pages][hkv][2][W] column maxima, minima; or null
-  float* units;    // [pages][hkv]
+  float* units;    // [pages][hkv], -inf where tokens are lost
   int64_t pages, slots;
   int hkv, d, plog;  // page_len = 1 << plog
   const int64_t *off, *lens;

@@ -1,0 +1,75 @@
+"""The paged cache at its limits: entries outside it, turning alone, extreme magnitudes, large pages, tiles of padded rows.
+
+References and their error bounds: cache_reference."""
+import math
+
+import pytest
+import torch
+
+from paper_2509_20883_amd import recis as R
+from tests import cache_reference as ref
+from tests import test_gpu_seq_cache as base
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+_dev, _cache, _close = base._dev, base._cache, base._close
+
+
+# ---------------------------------------------------------------------------
+# slots outside the cache
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("slot", [-1, 2])
+@pytest.mark.parametrize("dtype,codes", [(BF, "i8"), (BF, "e4m3"), (F32, "i8"), (F32, "e4m3")])
+def test_a_page_whose_first_tokens_had_no_slot_is_passed_over(dtype, codes, slot):
+    """Tokens that came for a slot outside the cache are gone when their page fills: the page then stands for nothing, whatever it
+    held before.  Its later pages, coded from one call's tokens, are there."""
+    P, hq, hkv, d = 32, 4, 2, 64
+    c = _cache(8, 2, hkv, d, P, codes, dtype, bounds=True, causal=False)
+    g = ref.fill(c, 31)  # of another user
+    table = torch.tensor([[4, 2, 5, 0], [1, 3, 6, 7]], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([slot, 1], dtype=torch.int32, device="cuda")
+    slot_list = [slot, 1]
+    k, v = (torch.randn(300, hkv, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+    lens, at = _dev([0, 0]), 0
+    # pages of the first sequence that are lost after each call: 0 (20 of its tokens), 1 (8 of them)
+    for new, lost in ((20, [0]), (20, [0]), (56, [0, 1]), (30, [0, 1, 3])):
+        off = _dev([0, new, 2 * new])
+        lens, _ = c.append(k[at:at + 2 * new], v[at:at + 2 * new], off, lens, table, slots=slots)
+        at += 2 * new
+        total = lens.tolist()
+        hold = ref.tokens_of(c, table, total, slot_list)
+        for p in lost:
+            hold[0][2][p * P:(p + 1) * P] = False
+        gk, gv = c.read(_dev([0, total[0], 2 * total[0]]), lens, table, 2 * total[0], slots=slots, dtype=F32)
+        for b in range(2):
+            there = hold[b][2][:, None, None]
+            for got, want in ((gk, hold[b][0]), (gv, hold[b][1])):
+                assert torch.equal(got[b * total[0]:(b + 1) * total[0]], torch.where(there, want, 0.0).float()), (b, total)
+        for rows in (1, 40):  # both kinds of tiles
+            q = torch.randn(2 * rows, hq, d, generator=g, device="cuda").to(dtype)
+            off = _dev([0, rows, 2 * rows])
+            out = c.attend(q, off, lens, table, slots=slots)
+            key_pos = torch.arange(total[0], device="cuda")
+            for b in range(2):
+                pos = torch.arange(rows, device="cuda") + total[b] - rows
+                want, bound = ref.attention(q[b * rows:(b + 1) * rows], *hold[b][:2], pos, key_pos, hold[b][2].long(), False, 0.0, None,
+                                            d ** -0.5, dtype == BF, hq // hkv)
+                _close(out[b * rows:(b + 1) * rows], want, bound, dtype)
+            n = total[0] // P
+            if n:
+                picks = c.select(q, off, lens, table, 1)[:rows]
+                seen = [p for p in range(n) if p not in lost]
+                assert (picks == 0).all() if not seen else all(x in seen for x in picks.flatten().tolist())
+                listed = torch.arange(n, dtype=torch.int32, device="cuda").expand(2 * rows, hkv, n).contiguous()
+                again = c.attend(q, off, lens, table, pages=listed, slots=slots)
+                for b in range(2):
+                    pos = torch.arange(rows, device="cuda") + total[b] - rows
+                    want, bound = ref.attention(q[b * rows:(b + 1) * rows], *hold[b][:2], pos, key_pos, hold[b][2].long(), False, 0.0, None,
+                                                d ** -0.5, dtype == BF, hq // hkv)
+                    _close(again[b * rows:(b + 1) * rows], want, bound, dtype)
+    # written again from its slot, the page is there again
+    c.append(k[:32], v[:32], _dev([0, 32]), _dev([0]), table[:1], slots=_dev([0], torch.int32))
+    gk, _ = c.read(_dev([0, 32]), _dev([32]), table[:1], 32, slots=_dev([0], torch.int32))
+    assert (gk != 0).any()
