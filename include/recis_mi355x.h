@@ -601,7 +601,8 @@ typedef struct {
  * cache once tokens came for it: put inside later, it holds no defined values.
  * validate != 0 in the calls below checks offsets, lens, the table's entries in
  * use and the slots on the host (and, where tokens are written, that no page or
- * slot is written twice); it copies them back: synchronizing. */
+ * slot is written twice; where queries are turned alone, offsets and lens only);
+ * it copies them back: synchronizing. */
 typedef struct {
   int64_t seqs, rows, pad; /* seqs < 2^24, rows < 2^31 - 1024                   */
   int64_t table_width;     /* at most 2^26                                      */
@@ -616,7 +617,8 @@ typedef struct {
  * by position * frequency_i, in the model's type afterwards; columns from rotary
  * on stay.  `turns`: device copy of rs_rotation_turns' result. */
 typedef struct {
-  const void *k, *v; /* [rows][heads_kv][head_dim]; both NULL: only q is turned */
+  const void *k, *v; /* [rows][heads_kv][head_dim]; both NULL: q alone is turned,
+                      by offsets and lens; no table or slots are read      */
   const void* q;     /* [rows][heads_q][head_dim], or NULL                      */
   void* q_out;       /* q turned, contiguous; rows past a padded sequence's end 0 */
   int64_t k_stride, k_head_stride, v_stride, v_head_stride, q_stride, q_head_stride;

@@ -94,11 +94,17 @@ CacheArgs cache_args(const rs_seq_cache& c, const rs_cache_batch& b) {
   return a;
 }
 
-// Host check of a call's sequences: copies them back, so it synchronizes. `grow`:
-// the rows are new tokens after lens; written pages and slots must then be distinct.
-// `open`: the call takes the open pages.
-rs_status check_sequences(const rs_seq_cache& c, const rs_cache_batch& b, const int64_t* start, bool grow, bool open,
-                          hipStream_t s) {
+// What a call does with its sequences.
+enum class Use {
+  kTurn,    // takes their positions alone
+  kAppend,  // writes its rows as new tokens after lens; pages and slots must then be distinct
+  kHeld,    // takes the tokens held
+  kPages,   // the full pages of those
+};
+
+// Host check of a call's sequences: copies them back, so it synchronizes.
+rs_status check_sequences(const rs_seq_cache& c, const rs_cache_batch& b, const int64_t* start, Use use, hipStream_t s) {
+  const bool grow = use == Use::kAppend;
   try {
     RS_HIP(hipStreamSynchronize(s));
     const size_t n = static_cast<size_t>(b.seqs);
@@ -117,6 +123,7 @@ rs_status check_sequences(const rs_seq_cache& c, const rs_cache_batch& b, const 
       if (more < 0) return fail(RS_EINVAL, "offsets must be nondecreasing");
       if (b.pad > 0) more = std::min(more, b.pad);
       if (lens[i] < 0) return fail(RS_EINVAL, "lens must be >= 0");
+      if (use == Use::kTurn) continue;
       if (lens[i] > b.table_width * c.page_len) return fail(RS_EINVAL, "a sequence is longer than its table");
       if (start && (first[i] < 0 || first[i] > lens[i] || more > lens[i] - first[i]))
         return fail(RS_EINVAL, "the rows read must lie in the sequence");
@@ -124,7 +131,7 @@ rs_status check_sequences(const rs_seq_cache& c, const rs_cache_batch& b, const 
       if (end > b.table_width * c.page_len || end >= kMost) return fail(RS_EINVAL, "a sequence outgrows its table");
       if (more == 0) continue;
       const int64_t slot = b.slots ? slots[i] : static_cast<int64_t>(i);
-      if (open) {
+      if (use != Use::kPages) {
         if (slot < 0 || slot >= c.slots) return fail(RS_EINVAL, "a slot is outside the cache");
         if (grow && slot_used[static_cast<size_t>(slot)]) return fail(RS_EINVAL, "two sequences share a slot");
         slot_used[static_cast<size_t>(slot)] = true;
@@ -240,7 +247,7 @@ rs_status seq_cache_append(const rs_seq_cache* c, const rs_cache_batch* b, const
   if (r->new_lens && r->new_lens == b->lens) return fail(RS_EINVAL, "new_lens must not be lens");
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {
-    const rs_status st = check_sequences(*c, *b, nullptr, r->k != nullptr, r->k != nullptr, s);
+    const rs_status st = check_sequences(*c, *b, nullptr, r->k ? Use::kAppend : Use::kTurn, s);
     if (st != RS_OK) return st;
   }
   if (b->seqs == 0) return RS_OK;
@@ -270,7 +277,7 @@ rs_status seq_cache_read(const rs_seq_cache* c, const rs_cache_batch* b, const i
   if (!aligned16(k) || !aligned16(v)) return fail(RS_EINVAL, "k and v must be 16-byte aligned");
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {
-    const rs_status st = check_sequences(*c, *b, start, false, true, s);
+    const rs_status st = check_sequences(*c, *b, start, Use::kHeld, s);
     if (st != RS_OK) return st;
   }
   if (b->seqs == 0 || b->rows == 0) return RS_OK;
@@ -310,7 +317,7 @@ rs_status seq_cache_attention(const rs_seq_cache* c, const rs_cache_batch* b, co
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {
-    const rs_status st = check_sequences(*c, *b, nullptr, false, true, s);
+    const rs_status st = check_sequences(*c, *b, nullptr, Use::kHeld, s);
     if (st != RS_OK) return st;
   }
   if (b->seqs == 0 || b->rows == 0) return RS_OK;
@@ -345,7 +352,7 @@ rs_status seq_cache_select(const rs_seq_cache* c, const rs_cache_batch* b, const
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {
-    const rs_status st = check_sequences(*c, *b, nullptr, false, false, s);
+    const rs_status st = check_sequences(*c, *b, nullptr, Use::kPages, s);
     if (st != RS_OK) return st;
   }
   if (b->seqs == 0 || b->rows == 0) return RS_OK;

@@ -764,7 +764,7 @@ class SeqCache(_Workspace):
                validate: bool = False):
         """Writes k and v as the sequences' tokens from lens on; returns (lens afterwards, q turned by the same
         positions or None).  k = v = None turns q alone (candidates that are not kept): lens then come back as they
-        would be with the rows kept, and nothing is written."""
+        would be with the rows kept, nothing is written, and neither table nor slots are looked at."""
         if (k is None) != (v is None) or (k is None and q is None):
             raise RecisError(EINVAL, "append takes k and v, q, or all three")
         q_out, ka, va, qa, oa, heads = None, None, None, None, None, 0
@@ -783,7 +783,7 @@ class SeqCache(_Workspace):
             oa, heads = q_out.data_ptr(), shape[-2]
         if rows == 0:
             ka = va = qa = oa = None
-        b, keep = self._batch(rows, pad, shape[0] if len(shape) == 4 else None, offsets, lens, table, slots)
+        b, keep = self._batch(rows, pad, shape[0] if len(shape) == 4 else None, offsets, lens, table, slots, k is not None)
         new_lens = torch.empty_like(keep[1])
         r = CacheRows(ka, va, qa, oa, ks, kh, vs, vh, qs, qh, heads, self.rotary, self.interleaved, 0, self._turns,
                       new_lens.data_ptr())

@@ -73,3 +73,34 @@ def test_a_page_whose_first_tokens_had_no_slot_is_passed_over(dtype, codes, slot
     c.append(k[:32], v[:32], _dev([0, 32]), _dev([0]), table[:1], slots=_dev([0], torch.int32))
     gk, _ = c.read(_dev([0, 32]), _dev([32]), table[:1], 32, slots=_dev([0], torch.int32))
     assert (gk != 0).any()
+
+
+# ---------------------------------------------------------------------------
+# turning alone
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("padded", [False, True])
+def test_turning_alone_needs_neither_slots_nor_pages(padded):
+    """Queries that are turned and not kept: more sequences than slots, tables that name no page, lengths past them."""
+    g = torch.Generator(device="cuda").manual_seed(41)
+    c = R.SeqCache(1, 2, 1, 32, page=32, dtype=F32, rotary=32)
+    held, new = [5, 0, 10 ** 6, 33, 70], [2, 3, 1, 0, 3]
+    off, lens = ref.offsets(new), _dev(held)
+    table = torch.full((5, 1), 2 ** 30, dtype=torch.int32, device="cuda")
+    q = torch.randn(5, 3, 2, 32, generator=g, device="cuda") if padded else torch.randn(sum(new), 2, 32, generator=g, device="cuda")
+    after, out = c.append(None, None, off, lens, table, q=q, validate=True)
+    assert after.tolist() == [a + b for a, b in zip(held, new)]
+    freqs = [10000.0 ** (-2.0 * i / 32) for i in range(16)]
+    for b, n in enumerate(new):
+        rows, got = (q[b, :n], out[b, :n]) if padded else (q[off[b]:off[b + 1]], out[off[b]:off[b + 1]])
+        pos = held[b] + torch.arange(n, device="cuda")
+        want = ref.turned(rows, pos, freqs, 32, False)
+        # the reference's frequencies are off by 2^-53 of themselves
+        slack = 8 * (2.0 ** -31 + (held[b] + n) * 2.0 ** -53)
+        assert bool(((got.double() - want).abs() <= ref.U * (want.abs() + slack) + slack).all()), b
+    for bad_off, bad_lens in (([0, 4, 3, 6, 6, 9], held), ([1, 2, 5, 6, 6, 9], held), (off.tolist(), [5, -1, 0, 0, 0])):
+        with pytest.raises(R.RecisError):
+            c.append(None, None, _dev(bad_off), _dev(bad_lens), table, q=q, validate=True)
+    with pytest.raises(R.RecisError):  # and as without queries alone
+        c.append(q[..., :1, :].contiguous(), q[..., :1, :].contiguous(), off, lens, table, q=q)
