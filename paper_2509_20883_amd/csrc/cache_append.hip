@@ -560,6 +560,11 @@ __global__ __launch_bounds__(kBlock) void k_cache_read(const CacheRead a, int64_
 }
 
 constexpr int64_t kMostBlocks = int64_t(1) << 21;  // of a launch: fewer than 2^32 threads along an axis
+constexpr int kPlainLds = 65536;                   // bytes of a block that a launch takes without asking
+
+// LDS of k_cache_append's own: sh_top, sh_low and sh_high.
+template <int NT>
+constexpr int kOwnLds = NT / kWave * 4 + 2 * NT * 4;
 
 template <typename T, bool E4M3, int NT>
 hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
@@ -570,7 +575,7 @@ hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
   a.q_units = !a.q.p ? 0 : a.c.pad > 0 ? a.c.seqs * ((a.c.pad + kTile - 1) / kTile) : a.c.rows / kTile + a.c.seqs;
   const int64_t lens = a.new_lens ? (a.c.seqs + NT - 1) / NT : 0;
   const int64_t blocks = a.page_units * a.c.hkv * 2 + a.q_units + lens;
-  if (bytes > 65536) {
+  if (bytes + kOwnLds<NT> > kPlainLds) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_append<T, E4M3, NT>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
@@ -586,10 +591,11 @@ hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
 template <typename T, bool E4M3>
 hipError_t append_type(const CacheAppend& a, hipStream_t s) {
   const int angles = kBlock * static_cast<int>(sizeof(Angle)), page = lds_stride<T>(a.c.d) << a.c.plog;
-  const int bytes = page > 65536 ? std::max(page, 4 * angles) : std::max(page, angles);
+  const bool large = page + kOwnLds<256> > kPlainLds;
+  const int bytes = std::max(page, large ? 4 * angles : angles);
   // a large page fills a CU's LDS by itself: more waves on it then (else 256 threads: 24
   // histories in pages of 64 126 us, 141 by 128, 153 by 512)
-  return bytes > 65536 ? append<T, E4M3, 1024>(a, bytes, s) : append<T, E4M3, 256>(a, bytes, s);
+  return large ? append<T, E4M3, 1024>(a, bytes, s) : append<T, E4M3, 256>(a, bytes, s);
 }
 
 template <typename T, typename O, bool E4M3>

@@ -76,6 +76,23 @@ def test_a_page_whose_first_tokens_had_no_slot_is_passed_over(dtype, codes, slot
 
 
 # ---------------------------------------------------------------------------
+# pages at 64 KiB of LDS
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("case", [
+    # 64 KiB with the block's own LDS, and just below: rows of 120 columns lie 256 (bf16) and 496 bytes apart
+    (1, 120, 256, "e4m3", BF, 120, False, [0, 255, 100], [256, 1, 413]),
+    (2, 120, 128, "i8", F32, 48, True, [0, 127, 3], [128, 1, 300]),
+    (1, 112, 256, "i8", BF, 112, True, [5], [520]),
+    (1, 112, 128, "e4m3", F32, 0, False, [5], [260]),
+], ids=str)
+@pytest.mark.parametrize("bounds", [False, True])
+def test_append_of_pages_that_fill_64_kib(case, bounds):
+    base.test_append_writes_exactly_the_codes_of_its_tokens(case, bounds)
+
+
+# ---------------------------------------------------------------------------
 # turning alone
 # ---------------------------------------------------------------------------
 
