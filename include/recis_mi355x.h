@@ -628,8 +628,10 @@ typedef struct {
 } rs_cache_rows;
 
 /* turns (host, [rotary / 2]): the frequencies (radians a position: freqs, host, or
- * where NULL base^(-2 i / rotary)) as 64-bit fractions of a turn, so that an angle
- * is exact at any position.  Errors: RS_EINVAL. */
+ * where NULL base^(-2 i / rotary); below 2^128) as 64-bit fractions of a turn, off by
+ * half of 2^-64 turns (a base's by 2^-64, and below 1 by 2^-60 of the frequency too):
+ * an angle at position p is off by p times that, 2^-33 turns at 2^31.  Errors:
+ * RS_EINVAL. */
 rs_status rs_rotation_turns(const double* freqs, double base, int32_t rotary, uint64_t* turns);
 
 /* Writes the rows of k and v as the sequences' next tokens (one launch).  All

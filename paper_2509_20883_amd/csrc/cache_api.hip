@@ -200,6 +200,36 @@ CacheSelect select_args(const rs_seq_cache& c, const rs_cache_batch& b, const rs
   return a;
 }
 
+// f / 2 pi modulo 1 in units of 2^-64, rounded: f is a whole number m of 64 bits times a
+// power of two, and the product of m with 1 / 2 pi is taken whole. 256 bits of 1 / 2 pi
+// (written from Machin's formula for pi) leave an error of 2^-128 below |f| = 2^128.
+uint64_t turn_of(long double f) {
+  static const uint64_t kInv[4] = {0x28BE60DB9391054A, 0x7F09D5F47D4D3770,
+                                   0x36D8A5664F10E410, 0x7F9458EAF7AEF158};
+  int e = 0;
+  const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(f), &e), 64));
+  uint64_t p[5], carry = 0;  // 0.p times 2^e
+  for (int i = 3; i >= 0; --i) {
+    const unsigned __int128 t = static_cast<unsigned __int128>(m) * kInv[i] + carry;
+    p[i + 1] = static_cast<uint64_t>(t);
+    carry = static_cast<uint64_t>(t >> 64);
+  }
+  p[0] = carry;
+  uint64_t turn = 0, next = 0;  // next: the bit behind
+  if (e >= 0) {
+    const int w = e / 64, left = e % 64;  // at most 2
+    turn = left ? p[w] << left | p[w + 1] >> (64 - left) : p[w];
+    next = p[w + 1] >> (63 - left) & 1;
+  } else if (e > -64) {
+    turn = p[0] >> -e;
+    next = p[0] >> (-e - 1) & 1;
+  } else if (e == -64) {
+    next = p[0] >> 63;
+  }
+  turn += next;
+  return f < 0 ? 0 - turn : turn;
+}
+
 // A list stands for every listed call when only its sizes count.
 const int32_t* listed(const rs_cache_query* q) { return q->count > 0 ? reinterpret_cast<const int32_t*>(16) : nullptr; }
 
@@ -211,15 +241,11 @@ rs_status rs_rotation_turns(const double* freqs, double base, int32_t rotary, ui
   if (rotary < 0 || rotary > 128 || rotary % 2 != 0) return fail(RS_EINVAL, "rotary must be even and in [0, 128]");
   if (rotary > 0 && !turns) return fail(RS_EINVAL, "null turns");
   if (!freqs && !(base > 0.0 && std::isfinite(base))) return fail(RS_EINVAL, "base must be > 0 and finite");
-  const long double two_pi = 6.283185307179586476925286766559005768L;
   for (int32_t i = 0; i < rotary / 2; ++i) {
     const long double f = freqs ? static_cast<long double>(freqs[i])
                                 : std::pow(static_cast<long double>(base), -2.0L * i / static_cast<long double>(rotary));
-    if (!std::isfinite(f)) return fail(RS_EINVAL, "a frequency is not finite");
-    long double t = f / two_pi;
-    t -= std::floor(t);
-    const long double x = std::floor(std::ldexp(t, 64) + 0.5L);
-    turns[i] = x >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(x);
+    if (!(std::fabs(f) < 0x1p128L)) return fail(RS_EINVAL, "frequencies must be below 2^128");
+    turns[i] = turn_of(f);
   }
   return RS_OK;
 }
