@@ -25,6 +25,7 @@
 #include <algorithm>
 
 #include "cache_common.h"
+#include "select_tiles.h"
 
 namespace rs {
 namespace {
@@ -479,14 +480,13 @@ size_t plan_cache_select(const CacheSelect& a, int64_t* tokens) {
 template <typename T, int W>
 static void run_select(const CacheSelect& a, hipStream_t s) {
   if (a.c.width > a.count) {
-    const int64_t run = int64_t(1) << a.run_log;
-    const int64_t units = a.c.pad > 0 ? a.c.seqs * ((a.c.pad + run - 1) / run) : a.c.rows / run + (run > 1 ? a.c.seqs : 0);
-    const int held = std::min(kRowsAtOnce, (static_cast<int>(run) * heads_to(a.group) + 15) & ~15);
+    const TileRange units = tiles_of_rows(a.c.seqs, a.c.rows, a.c.pad, a.run_log, a.row0, a.tokens);
+    const int held = std::min(kRowsAtOnce, ((heads_to(a.group) << a.run_log) + 15) & ~15);
     const size_t lds = kRowsAtOnce * sizeof(float) + held * (2 * W + 16);
     CacheSelect b = a;
-    for (int64_t u = 0; u < units; u += kMostUnits) {
-      b.unit0 = static_cast<uint32_t>(u);
-      const dim3 grid(a.tiles, static_cast<unsigned>(std::min(units - u, kMostUnits)), a.c.hkv);
+    for (int64_t u = 0; u < units.count; u += kMostUnits) {
+      b.unit0 = static_cast<uint32_t>(units.first + u);
+      const dim3 grid(a.tiles, static_cast<unsigned>(std::min(units.count - u, kMostUnits)), a.c.hkv);
       k_select_score<T, W><<<grid, kBlock, lds, s>>>(b);
     }
   }
@@ -503,10 +503,7 @@ hipError_t launch_cache_select(CacheSelect a, bool bf16, hipStream_t s) {
   // the bound of the lengths only shapes the launches: a block goes on to the pages past it
   const int64_t pages = a.max_pages > 0 ? std::min(a.max_pages, a.c.width) : a.c.width;
   a.tiles = static_cast<int>(std::min<int64_t>(1 << 20, std::max<int64_t>(1, (pages + kPageRun - 1) / kPageRun)));
-  // rows of a tile: about those of a sequence, as many as LDS holds
-  const int slots = heads_to(a.group);
-  a.run_log = 0;
-  while ((2 << a.run_log) <= a.c.rows / a.c.seqs && (2 << a.run_log) * slots <= kRowsAtOnce) ++a.run_log;
+  a.run_log = tile_rows_log(a.c.seqs, a.c.rows, a.c.pad, tokens, kRowsAtOnce / heads_to(a.group));
   const int W = cache_width(a.c.d);
   for (int64_t r = 0; r < a.c.rows && tokens > 0; r += tokens) {
     a.row0 = r;

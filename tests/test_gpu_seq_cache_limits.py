@@ -121,3 +121,40 @@ def test_turning_alone_needs_neither_slots_nor_pages(padded):
             c.append(None, None, _dev(bad_off), _dev(bad_lens), table, q=q, validate=True)
     with pytest.raises(R.RecisError):  # and as without queries alone
         c.append(q[..., :1, :].contiguous(), q[..., :1, :].contiguous(), off, lens, table, q=q)
+
+
+# ---------------------------------------------------------------------------
+# more rows than the workspace holds scores of
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("padded", [False, True])
+@pytest.mark.parametrize("new", [[1] * 1200, [3, 0, 700, 1, 1, 40, 300, 2]])
+def test_rows_that_take_several_windows_of_scores(new, padded):
+    """Tables so wide that 256 MiB hold the scores of 536 rows: as in parts, and as the formula for some rows."""
+    hkv, width, count, P, d = 8, 15625, 9, 32, 32
+    c = _cache(60, 1, hkv, d, P, "i8", BF, bounds=True)
+    g = ref.fill(c, 51)
+    if padded:
+        pad, new = max(new[0], 150), [min(n, max(new[0], 150)) for n in new[:8]]
+    seqs = len(new)
+    table = torch.randint(0, 60, (seqs, width), generator=g, device="cuda").to(torch.int32)
+    lens = torch.randint(500, width * P, (seqs,), generator=g, device="cuda")
+    lens[0] = width * P
+    off = ref.offsets(new)
+    q = torch.randn(*((seqs, pad) if padded else (sum(new),)), hkv, d, generator=g, device="cuda").bfloat16()
+    got = c.select(q, off, lens, table, count)
+    if padded:
+        assert seqs * pad > 536 * 2
+        for b, n in enumerate(new):
+            assert (got[b, n:] == -1).all()
+            assert torch.equal(got[b, :n], c.select(q[b, :n], _dev([0, n]), lens[b:b + 1], table[b:b + 1], count))
+        return
+    assert sum(new) > 536
+    for a in range(0, seqs, 2 if seqs < 100 else 300):
+        b = min(seqs, a + (2 if seqs < 100 else 300))
+        rows = slice(int(off[a]), int(off[b]))
+        assert torch.equal(got[rows], c.select(q[rows], off[a:b + 1] - off[a], lens[a:b], table[a:b], count))
+    last = int(off[-1]) - 1
+    want = ref.select(q[last], c, table[-1].tolist(), int(lens[-1]), int(lens[-1]) - 1, count, True)
+    assert got[last].tolist() == want

@@ -1,5 +1,8 @@
 """The paged cache's host arithmetic at its limits (CPU only)."""
 import ctypes as C
+import os
+import random
+import subprocess
 from decimal import Decimal, getcontext
 from fractions import Fraction
 
@@ -68,3 +71,80 @@ def test_frequencies_of_a_base(base, rotary):
         f = (Decimal(base).ln() * Decimal(-2 * i) / Decimal(rotary)).exp()
         bound = 0.5 + float(f) / 6.28 * (2 + abs(float(f.ln())))
         assert _off(got[i], Fraction(f)) <= bound and (base < 1 or bound < 1), i
+
+
+SHIM = r"""
+#include "select_tiles.h"
+extern "C" {
+int rows_log(int64_t seqs, int64_t rows, int64_t pad, int64_t window, int64_t most) { return rs::tile_rows_log(seqs, rows, pad, window, most); }
+void tiles(int64_t seqs, int64_t rows, int64_t pad, int log, int64_t row0, int64_t n, int64_t* out) {
+  const rs::TileRange r = rs::tiles_of_rows(seqs, rows, pad, log, row0, n);
+  out[0] = r.first;
+  out[1] = r.count;
+}
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def st(tmp_path_factory):
+    d = tmp_path_factory.mktemp("select_tiles")
+    (d / "shim.cpp").write_text(SHIM)
+    so = str(d / "shim.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", os.path.join(R.PKG, "csrc"),
+                    str(d / "shim.cpp"), "-o", so], check=True)
+    L = C.CDLL(so)
+    i64 = C.c_int64
+    L.rows_log.argtypes = [i64] * 5
+    L.tiles.argtypes = [i64, i64, i64, C.c_int, i64, i64, C.POINTER(i64)]
+    return L
+
+
+def _windows(st, seqs, rows, pad, log, window):
+    out = (C.c_int64 * 2)()
+    for row0 in range(0, rows, window):
+        n = min(window, rows - row0)
+        st.tiles(seqs, rows, pad, log, row0, n, out)
+        yield row0, n, out[0], out[1]
+
+
+def test_every_row_of_a_window_has_its_tile_launched(st):
+    rng = random.Random(1)
+    for _ in range(400):
+        seqs, padded = rng.randint(1, 30), rng.random() < 0.4
+        if padded:
+            pad = rng.randint(1, 40)
+            rows = seqs * pad
+        else:
+            lens = [rng.choice([0, 0, 1, 2, rng.randint(0, 60)]) for _ in range(seqs)]
+            before, behind = rng.choice([0, 0, 7]), rng.choice([0, 0, 5])
+            off = [before]
+            for n in lens:
+                off.append(off[-1] + n)
+            pad, rows = 0, off[-1] + behind
+        if rows == 0:
+            continue
+        window = rng.randint(1, rows)
+        for log in range(5):
+            for row0, n, first, count in _windows(st, seqs, rows, pad, log, window):
+                for row in range(row0, row0 + n):
+                    if pad:
+                        unit = row // pad * ((pad + (1 << log) - 1) >> log) + (row % pad >> log)
+                    else:
+                        s = next((s for s in range(seqs) if off[s] <= row < off[s + 1]), None)
+                        if s is None:
+                            continue
+                        unit = (off[s] >> log) + (s if log else 0) + ((row - off[s]) >> log)
+                    assert first <= unit < first + count, (pad, log, row0, n, row)
+
+
+@pytest.mark.parametrize("seqs,rows,pad", [(4096, 4096, 0), (100, 4096, 0), (1, 100000, 0), (50000, 100000, 0), (3000, 3 * 3000, 3), (7, 7 * 1000, 1000)])
+@pytest.mark.parametrize("window", [1, 16, 536, 1 << 20])
+@pytest.mark.parametrize("most", [1, 8, 16])
+def test_windows_launch_as_many_tiles_as_rows(st, seqs, rows, pad, window, most):
+    """All windows together: at most a tile a row, and three more of each window, however many there are."""
+    log = st.rows_log(seqs, rows, pad, window, most)
+    got = list(_windows(st, seqs, rows, pad, log, window))
+    assert sum(count for _, _, _, count in got) <= 2 * rows + 3 * len(got)
+    if window >= rows:
+        assert sum(count for _, _, _, count in got) <= rows / (1 << log) + seqs + 1
