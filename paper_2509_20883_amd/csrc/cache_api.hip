@@ -374,7 +374,7 @@ rs_status seq_cache_select(const rs_seq_cache* c, const rs_cache_batch* b, const
   if (need > 0) {
     if (!workspace || workspace_bytes < need) return fail(RS_EINVAL, "workspace missing or too small");
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(RS_EINVAL, "workspace must be 256-byte aligned");
-    a.scores = static_cast<float*>(workspace);
+    a.scores = static_cast<uint32_t*>(workspace);
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (validate) {

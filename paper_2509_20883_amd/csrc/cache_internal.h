@@ -71,7 +71,7 @@ struct CacheSelect {
   HeadRows q;
   int hq, group, causal, count;
   int32_t* out;
-  float* scores;          // [tokens][hkv][width]
+  uint32_t* scores;       // [tokens][hkv][width], the upper halves of fp64 numbers
   int64_t max_pages;      // the caller's bound of a sequence's pages (0: none)
   int64_t row0, tokens;   // the rows of this launch
   int tiles, run_log;     // blocks along the pages; rows of a block, 1 << run_log

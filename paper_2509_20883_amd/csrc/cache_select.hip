@@ -8,9 +8,10 @@
 //
 // mx and mn bound the page's keys column by column, so with q8 for q a score is
 // not below that of any key in the page. Everything is whole numbers of at most
-// 8 bits and powers of two: I is below 2^24, the products are exact, and the
-// choice does not depend on the order of any sum. Equal scores go to the lower
-// page.
+// 8 bits and powers of two: I has at most 21 bits (128 * 127 * 127), the products are
+// exact, and the choice does not depend on the order of any sum. A score may pass the
+// range of fp32 (2^-252 to 2^263), so it is taken in 64 bits and kept as the upper
+// half of those, which holds it all. Equal scores go to the lower page.
 //
 // The scores are a matrix product in 8-bit integers, query heads by pages, over
 // the q8+ with the maxima and the q8- with the minima one after the other. A wave
@@ -34,6 +35,9 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagesAtOnce = 64;  // of a wave
 constexpr int kPageRun = kPagesAtOnce * (kBlock / kWave);
+
+// A score's sign, exponent and first 20 bits: all of it.
+__device__ inline uint32_t high_word(double x) { return static_cast<uint32_t>(__double2hiint(x)); }
 
 __device__ inline float to_f32(uint16_t x) { return bf16_to_f32(x); }
 __device__ inline float to_f32(float x) { return x; }
@@ -180,7 +184,7 @@ __global__ __launch_bounds__(kBlock) void k_select_score(const CacheSelect a) {
       filled = true;
     }
     // the best of a page over the 16 LDS rows from `base` on, for each group of four
-    auto best_of = [&](int base, float (&best)[kGroups]) {
+    auto best_of = [&](int base, double (&best)[kGroups]) {
       i32x4 qa[kSteps];
       float scale[4];
 #pragma unroll
@@ -194,24 +198,24 @@ __global__ __launch_bounds__(kBlock) void k_select_score(const CacheSelect a) {
         for (int k = 0; k < kSteps; ++k) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[k], box[i][k], sum, 0, 0, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (scale[e] > 0.0f) best[i] = fmaxf(best[i], static_cast<float>(sum[e]) * scale[e]);
+          if (scale[e] > 0.0f) best[i] = fmax(best[i], static_cast<double>(sum[e]) * static_cast<double>(scale[e]));
       }
     };
-    auto write = [&](int own, bool mine, float (&best)[kGroups]) {
+    auto write = [&](int own, bool mine, double (&best)[kGroups]) {
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        float y = best[i];
-        if (slots >= 8) y = fmaxf(y, __shfl_xor(y, 16, kWave));
-        if (slots >= 16) y = fmaxf(y, __shfl_xor(y, 32, kWave));
-        const float score = unit[i] == -INFINITY ? -INFINITY : y * unit[i] + 0.0f;  // one zero
+        double y = best[i];
+        if (slots >= 8) y = fmax(y, __shfl_xor(y, 16, kWave));
+        if (slots >= 16) y = fmax(y, __shfl_xor(y, 32, kWave));
+        const double score = unit[i] == -INFINITY ? -INFINITY : y * unit[i] + 0.0;  // one zero
         const int n = first + i * 16 + col;
         if (n < most && mine)
-          a.scores[((first_row + own - a.row0) * c.hkv + kvh) * c.width + n] = score == score ? score : INFINITY;  // not finite: first
+          a.scores[((first_row + own - a.row0) * c.hkv + kvh) * c.width + n] = high_word(score == score ? score : INFINITY);  // not finite: first
       }
     };
     if (slots <= 16) {
       for (int base = 0; base < rows * slots; base += 16) {
-        float best[kGroups];
+        double best[kGroups];
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) best[i] = -INFINITY;
         best_of(base, best);
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(kBlock) void k_select_score(const CacheSelect a) {
       }
     } else {
       for (int own = 0; own < rows; ++own) {
-        float best[kGroups];
+        double best[kGroups];
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) best[i] = -INFINITY;
         for (int h0 = 0; h0 < slots; h0 += held) {
@@ -238,10 +242,7 @@ __global__ __launch_bounds__(kBlock) void k_select_score(const CacheSelect a) {
 }
 
 // Larger scores have larger keys.
-__device__ inline uint32_t order(float x) {
-  const uint32_t b = __float_as_uint(x);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
+__device__ inline uint32_t order(uint32_t b) { return b & 0x80000000u ? ~b : b | 0x80000000u; }
 
 // A block per row and key head, its keys in registers: the count-th largest by
 // halving the range of keys (a step is one compare a key and one barrier), then the
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
     for (int i = threadIdx.x; i < a.count; i += NT) out[i] = i < seen ? i : -1;
     return;
   }
-  const float* score = a.scores + (static_cast<int64_t>(blockIdx.x) * c.hkv + kvh) * c.width;
+  const uint32_t* score = a.scores + (static_cast<int64_t>(blockIdx.x) * c.hkv + kvh) * c.width;
   uint32_t key[ITEMS];  // 0: no page (order gives no score 0)
   uint32_t top = 0;
 #pragma unroll
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(NT) void k_select_pick_any(const CacheSelect a) {
     for (int i = threadIdx.x; i < a.count; i += NT) out[i] = i < seen ? i : -1;
     return;
   }
-  const float* score = a.scores + (static_cast<int64_t>(blockIdx.x) * c.hkv + kvh) * c.width;
+  const uint32_t* score = a.scores + (static_cast<int64_t>(blockIdx.x) * c.hkv + kvh) * c.width;
   uint32_t prefix = 0;
   int left = a.count;  // still to be found among the keys with this prefix
   for (int shift = 24; shift >= 0; shift -= 8) {
@@ -469,7 +470,7 @@ constexpr int64_t kMostUnits = 65535;  // tiles lie along a launch's second axis
 }  // namespace
 
 size_t plan_cache_select(const CacheSelect& a, int64_t* tokens) {
-  const size_t one = static_cast<size_t>(a.c.hkv) * std::max<int64_t>(a.c.width, 1) * sizeof(float);
+  const size_t one = static_cast<size_t>(a.c.hkv) * std::max<int64_t>(a.c.width, 1) * sizeof(uint32_t);
   *tokens = 0;
   if (a.c.rows == 0 || a.c.seqs == 0) return 0;
   *tokens = std::min<int64_t>(a.c.rows, std::max<int64_t>(1, kMostScoreBytes / one));

@@ -158,3 +158,27 @@ def test_rows_that_take_several_windows_of_scores(new, padded):
     last = int(off[-1]) - 1
     want = ref.select(q[last], c, table[-1].tolist(), int(lens[-1]), int(lens[-1]) - 1, count, True)
     assert got[last].tolist() == want
+
+
+# ---------------------------------------------------------------------------
+# scores and values at the ends of their types' ranges
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("q_by,unit_by", [(2.0 ** -120, 2.0 ** -100), (2.0 ** -40, 2.0 ** -126), (2.0 ** 120, 2.0 ** 100), (2.0 ** 110, 1.0)])
+def test_scores_outside_fp32_choose_exactly(dtype, q_by, unit_by):
+    """Whole numbers times powers of two: the choice is exact where the scores pass fp32's range, too, and between heads far apart."""
+    c = _cache(200, 1, 1, 128, 32, "i8", dtype, bounds=True, causal=False)
+    g = ref.fill(c, 61)
+    c.units.copy_(unit_by * 2.0 ** torch.randint(0, 4, c.units.shape, generator=g, device="cuda"))
+    q = torch.randn(6, 5, 128, generator=g, device="cuda") * q_by
+    q[1, 1:] = 0
+    q[2, 0] = torch.randn(128, generator=g, device="cuda")
+    q[3] *= torch.tensor([1.0, 2.0 ** -2, 0.0, 2.0 ** -5, 1.0], device="cuda")[:, None]
+    q[4] = -q[4].abs()
+    q = q.to(dtype)
+    table = torch.randperm(200, generator=g, device="cuda").to(torch.int32)[None]
+    got = c.select(q, _dev([0, 6]), _dev([200 * 32]), table, 17)
+    for i in range(6):
+        assert got[i].tolist() == ref.select(q[i], c, table[0].tolist(), 200 * 32, 0, 17, False), i
