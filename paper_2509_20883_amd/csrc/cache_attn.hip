@@ -52,8 +52,11 @@ struct Pieces {
   static constexpr int N = sizeof(T) == 2 ? 1 : 3;
 };
 
-template <int N>
+// ANY: the values may pass bf16's largest, which a first piece then stays at (rounded, it
+// would be infinite and the others NaN).
+template <bool ANY, int N>
 __device__ inline void split(const float (&x)[8], bf16x8 (&f)[N]) {
+  constexpr float kMost = 0x1.FEp127f;
   float r[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = x[e];
@@ -62,7 +65,9 @@ __device__ inline void split(const float (&x)[8], bf16x8 (&f)[N]) {
     u32x4 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
+      const bool cut = ANY && n == 0 && N > 1;
+      w[e] = cut ? pack_bf16(__builtin_amdgcn_fmed3f(r[2 * e], -kMost, kMost), __builtin_amdgcn_fmed3f(r[2 * e + 1], -kMost, kMost))
+                 : pack_bf16(r[2 * e], r[2 * e + 1]);
       if (n + 1 < N) {
         r[2 * e] -= __uint_as_float(w[e] << 16);
         r[2 * e + 1] -= __uint_as_float(w[e] & 0xFFFF0000u);
@@ -117,7 +122,7 @@ __device__ inline void load8(const uint16_t* p, bf16x8 (&f)[1]) { f[0] = *reinte
 __device__ inline void load8(const float* p, bf16x8 (&f)[3]) {
   const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
   const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  split(x, f);
+  split<true>(x, f);
 }
 __device__ inline void pieces_of(const uint16_t (&x)[8], bf16x8 (&f)[1]) {
   typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
@@ -126,7 +131,7 @@ __device__ inline void pieces_of(const uint16_t (&x)[8], bf16x8 (&f)[1]) {
   for (int e = 0; e < 8; ++e) w[e] = x[e];
   f[0] = __builtin_bit_cast(bf16x8, w);
 }
-__device__ inline void pieces_of(const float (&x)[8], bf16x8 (&f)[3]) { split(x, f); }
+__device__ inline void pieces_of(const float (&x)[8], bf16x8 (&f)[3]) { split<true>(x, f); }
 
 constexpr int kKeyWaves = 4;  // of a block whose waves lie along the keys
 constexpr int kPartBlocks = 2 * kKeyWaves;
@@ -504,7 +509,7 @@ __global__ __launch_bounds__(WR* WK* kWave, (kResident<T, HD, M>)) void k_cache_
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = p[8 * u + e];
-      split(y, pf[u]);
+      split<false>(y, pf[u]);
     }
   };
 

@@ -182,3 +182,33 @@ def test_scores_outside_fp32_choose_exactly(dtype, q_by, unit_by):
     got = c.select(q, _dev([0, 6]), _dev([200 * 32]), table, 17)
     for i in range(6):
         assert got[i].tolist() == ref.select(q[i], c, table[0].tolist(), 200 * 32, 0, 17, False), i
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_fp32_values_past_the_largest_bf16_number(rows):
+    """fp32 numbers above bf16's largest are numbers, in queries, keys and values of an open page."""
+    d, n = 64, 9
+    c = _cache(1, 1, 1, d, 32, "i8", F32, causal=False)
+    g = torch.Generator(device="cuda").manual_seed(62)
+    top = 3.4e38
+    assert torch.tensor(top).bfloat16().isinf()
+    c.open[0, 0, 0, :, :n] = torch.randn(2, n, d, generator=g, device="cuda")
+    c.open[0, 0, 0, 0, :n, 0] = torch.linspace(-3, 3, n, device="cuda").bfloat16().float() * 2.0 ** -125  # times 3.4e38: -240 to 240
+    c.open[0, 0, 0, 0, 2, 0] = 0
+    c.open[0, 0, 0, 1, 3, 5] = top
+    c.open[0, 0, 0, 1, 4, 6] = -top
+    q = torch.randn(rows, 2, d, generator=g, device="cuda")
+    q[0, 0, 0], q[-1, 1, 0] = top, -top
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), _dev([n])
+    k, v, there = ref.tokens_of(c, table, [n], [0])[0]
+    out = c.attend(q, _dev([0, rows]), lens, table)
+    pos = torch.arange(rows, device="cuda") + n - rows
+    want, bound = ref.attention(q, k, v, pos, torch.arange(n, device="cuda"), there.long(), False, 0.0, None, d ** -0.5, False, 2)
+    _close(out, want, bound, F32)
+    # a key of its own, past bf16's largest
+    c.open[0, 0, 0, 0, 1, 7] = top
+    q[:, :, 7] = torch.randn(rows, 2, generator=g, device="cuda").sign() * 2.0 ** -126
+    k, v, there = ref.tokens_of(c, table, [n], [0])[0]
+    out = c.attend(q, _dev([0, rows]), lens, table)
+    want, bound = ref.attention(q, k, v, pos, torch.arange(n, device="cuda"), there.long(), False, 0.0, None, d ** -0.5, False, 2)
+    _close(out, want, bound, F32)
