@@ -655,6 +655,10 @@ rs_status seq_cache_read(const rs_seq_cache* c, const rs_cache_batch* b, const i
  * [count], page numbers of the sequence), row i of a key head sees only the keys
  * of those full pages and of the open page; entries that name no full page are
  * passed over, a page named twice counts twice.  A query without a key gets 0.
+ * The open page is the one after the sequence's last token: a row of a causal chunk
+ * that stands in a page which the chunk itself has filled sees that page, and its own
+ * key, only where its list names it (fed a token at a time it saw the page open); the
+ * caller adds that page where it is wanted.
  * q is as append turned it (as it is without rotation); out is contiguous and
  * does not overlap q.  Scores, statistics and sums are fp32; bf16 probabilities
  * are rounded as operands of the matrix instructions, fp32 ones keep 24 bits.
@@ -685,7 +689,8 @@ rs_status seq_cache_attention(const rs_seq_cache* c, const rs_cache_batch* b, co
  *   units * max_h sq_h sum_c max(q8_c maximum_c, q8_c minimum_c)
  * over the query heads h of the key head, with q8 = round(q / sq_h), ties to
  * even, and sq_h the least power of two with max |q_h| <= 127 sq_h.  Whole numbers
- * and powers of two: the choice is exact, equal scores go to the lower page.  A
+ * and powers of two: the choice is exact, equal scores go to the lower page.  The
+ * bounds are a whole page's: those of a row's own page take in keys behind the row.  A
  * query that is not finite counts as 0, a page that is not finite comes first, one
  * outside the cache last.  Workspace as above. */
 size_t seq_cache_select_workspace_bytes(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_query* q);

@@ -658,8 +658,9 @@ class SeqCache(_Workspace):
     [rows, heads_kv, d] with CSR offsets, or padded [seqs, pad, heads_kv, d])
     and returns (lens afterwards, q turned).  ``attend`` is SeqAttention over
     the tokens held (inference only), with `pages` over the listed ones;
-    ``select`` lists the pages of the highest score for each row and key head;
-    ``read`` returns tokens as rows.  scale, softcap, causal and slopes are
+    ``select`` lists the pages of the highest score for each row and key head
+    (a row of a causal chunk sees its own page, once the chunk has filled it,
+    only where the list names it); ``read`` returns tokens as rows.  scale, softcap, causal and slopes are
     SeqAttention's.  max_q and max_len bound a sequence's queries and tokens
     where the caller knows: they only shape the launches.
 

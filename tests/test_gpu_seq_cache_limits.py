@@ -212,3 +212,126 @@ def test_fp32_values_past_the_largest_bf16_number(rows):
     out = c.attend(q, _dev([0, rows]), lens, table)
     want, bound = ref.attention(q, k, v, pos, torch.arange(n, device="cuda"), there.long(), False, 0.0, None, d ** -0.5, False, 2)
     _close(out, want, bound, F32)
+
+
+# ---------------------------------------------------------------------------
+# padded rows in every tile, and more blocks than a launch takes
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,codes", [(BF, "e4m3"), (F32, "i8")])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,pad,lens,new", [
+    (8, 2, 64, 7, [3000, 5, 64, 20000], [7, 3, 0, 5]),       # 28 rows: tiles of 32
+    (6, 2, 40, 9, [300, 0, 31], [9, 1, 12]),                 # 27
+    (8, 2, 64, 40, [3000, 0, 64, 500], [40, 3, 0, 17]),      # 160: tiles of 128, waves of absent rows alone
+    (4, 2, 128, 70, [70000, 100], [70, 65]),                 # 140, split along the keys
+    (5, 1, 24, 33, [0, 40, 200], [33, 40, 2]),               # 165, cut to the pad length
+])
+def test_padded_rows_in_wider_tiles(dtype, codes, causal, hq, hkv, d, pad, lens, new):
+    base._attend_case(hq, hkv, d, 32, codes, dtype, lens, new, causal, padded=pad, seed=71)
+    base._attend_case(hq, hkv, d, 64, codes, dtype, lens, new, causal, 9.0, True, padded=pad, seed=72, max_q=pad, max_len=max(lens))
+
+
+@pytest.mark.parametrize("dtype,codes", [(BF, "i8"), (F32, "e4m3")])
+@pytest.mark.parametrize("hq,hkv,pad,new", [(40, 1, 3, [3, 0, 2]), (36, 2, 4, [1, 4, 6]), (4, 2, 40, [40, 3, 17])])
+def test_padded_rows_over_listed_pages(dtype, codes, hq, hkv, pad, new):
+    base._attend_case(hq, hkv, 64, 32, codes, dtype, [700, 40, 2000], new, True, padded=pad, count=5, seed=73)
+
+
+@pytest.mark.parametrize("padded", [0, 6])
+def test_lists_end_in_minus_one(padded):
+    """Whole lists: the chosen pages, ascending, then -1, for rows that see fewer pages than are asked for and for absent ones."""
+    c = _cache(90, 5, 2, 64, 32, "i8", F32, bounds=True)
+    g = ref.fill(c, 74)
+    lens, new = [32 * 12, 0, 5, 700, 33], [6, 2, 3, 4, 0]
+    table = torch.randint(0, 90, (5, 25), generator=g, device="cuda").to(torch.int32)
+    off = ref.offsets(new)
+    q = torch.randn(*((5, padded) if padded else (sum(new),)), 4, 64, generator=g, device="cuda")
+    for count in (1, 11, 12, 40):
+        got = c.select(q, off, _dev(lens), table, count)
+        for b, n in enumerate(new):
+            rows, lists = (q[b], got[b]) if padded else (q[off[b]:off[b + 1]], got[off[b]:off[b + 1]])
+            for i in range(n):
+                want = ref.select(rows[i], c, table[b].tolist(), lens[b], lens[b] - n + i, count, True)
+                assert lists[i].tolist() == [h + [-1] * (count - len(h)) for h in want], (b, i, count)
+            assert (lists[n:] == -1).all()
+
+
+def test_more_blocks_than_a_launch_takes():
+    """2,200,000 sequences that share one page and one open page: reading, choice and both attentions go in several launches."""
+    seqs, d = 2200000, 8
+    c = _cache(2, 1, 1, d, 32, "i8", BF, bounds=True, causal=False)
+    g = ref.fill(c, 75)
+    table = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").expand(seqs, 2).contiguous()
+    slots = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+    off, lens = torch.arange(seqs + 1, device="cuda"), torch.full((seqs,), 70, device="cuda")
+    start = torch.randint(0, 70, (seqs,), generator=g, device="cuda")
+    k, v = c.read(_dev([0, 70]), _dev([70]), table[:1], 70, slots=slots[:1])
+    gk, gv = c.read(off, lens, table, seqs, start=start, slots=slots)
+    assert torch.equal(gk, k[start]) and torch.equal(gv, v[start])
+    q = torch.randn(64, 1, d, generator=g, device="cuda").bfloat16()
+    at = torch.randint(0, 64, (seqs,), generator=g, device="cuda")
+    few = _dev(list(range(65)))
+    pages = c.select(q, few, lens[:64], table[:64], 1)
+    out = c.attend(q, few, lens[:64], table[:64], slots=slots[:64], max_q=1)
+    listed = c.attend(q, few, lens[:64], table[:64], pages=pages, slots=slots[:64])
+    many = q[at]
+    assert torch.equal(c.select(many, off, lens, table, 1), pages[at])
+    assert torch.equal(c.attend(many, off, lens, table, slots=slots, max_q=1), out[at])
+    assert torch.equal(c.attend(many, off, lens, table, pages=pages[at], slots=slots), listed[at])
+
+
+def test_append_of_more_blocks_than_a_launch_takes():
+    """35,000 sequences of 16 key heads, 2.2 million blocks: open pages, turned queries and lengths of the second launch, too."""
+    seqs, hkv, d = 35000, 16, 8
+    g = torch.Generator(device="cuda").manual_seed(76)
+    c = R.SeqCache(4, seqs, hkv, d, page=32, rotary=8)
+    table = torch.zeros(seqs, 1, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(seqs, hkv, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    lens = torch.randint(0, 30, (seqs,), generator=g, device="cuda")
+    off = torch.arange(seqs + 1, device="cuda")
+    after, turned = c.append(k, v, off, lens, table, q=k)
+    assert torch.equal(after, lens + 1)
+    rows = torch.arange(seqs, device="cuda")
+    assert torch.equal(c.open[rows, 0, :, 0, lens], turned) and torch.equal(c.open[rows, 0, :, 1, lens], v)
+    some = slice(seqs - 50, seqs)
+    want = ref.turned(k[some], lens[some], [10000.0 ** (-i / 4) for i in range(4)], 8, False)
+    assert ((turned[some].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -28).all()
+
+
+# ---------------------------------------------------------------------------
+# chunks of queries over listed pages
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,codes", [(BF, "e4m3"), (F32, "i8")])
+def test_a_row_sees_its_own_full_page_where_its_list_names_it(dtype, codes):
+    """The open page is that after the call: rows of a chunk whose page the chunk filled see it, and themselves, only where it is
+    listed; of the open page each sees what is not behind it."""
+    hq, hkv, d, P, n = 4, 2, 64, 32, 120
+    c = _cache(8, 1, hkv, d, P, codes, dtype, bounds=True)
+    g = ref.fill(c, 81)
+    table = torch.tensor([[5, 2, 7, 0]], dtype=torch.int32, device="cuda")
+    new = 60  # positions 60 .. 119: 4 in page 1, page 2 whole, 24 in the open one
+    q = torch.randn(new, hq, d, generator=g, device="cuda").to(dtype)
+    off, lens = _dev([0, new]), _dev([n])
+    picks = c.select(q, off, lens, table, 1)
+    pos = torch.arange(n - new, n, device="cuda")
+    own = (pos // P).int()
+    own = torch.where((own < 3)[:, None] & (picks[..., 0] != own[:, None]), own[:, None], -1)[..., None]  # named once
+    k, v, there = ref.tokens_of(c, table, [n], [0])[0]
+    key_pos = torch.arange(n, device="cuda")
+    for pages in (picks, torch.cat([picks, own], 2)):
+        out = c.attend(q, off, lens, table, pages=pages.contiguous())
+        for i in range(new):
+            for h in range(hkv):
+                w = (key_pos >= 96).long()
+                for x in pages[i, h].tolist():
+                    if x >= 0:
+                        w[x * P:(x + 1) * P] += 1
+                G = hq // hkv
+                want, bound = ref.attention(q[i:i + 1, h * G:(h + 1) * G], k[:, h:h + 1], v[:, h:h + 1], pos[i:i + 1], key_pos, w, True, 0.0, None,
+                                            d ** -0.5, dtype == BF, G)
+                _close(out[i:i + 1, h * G:(h + 1) * G], want, bound, dtype)
+                assert pages is picks or int(w[pos[i]]) == 1
