@@ -733,7 +733,7 @@ __global__ __launch_bounds__(NT < kBlock ? kBlock : NT) void k_cache_join(const 
   __shared__ float sh_l[kThreads], sh_m[kThreads / kWave];
   const CacheArgs& c = a.c;
   const int th = threadIdx.x % NT, row = threadIdx.x / NT;
-  const uint32_t u = a.unit0 + blockIdx.x;
+  const uint32_t u = blockIdx.x;
   TileAt t;
   int64_t token;
   if (c.pad > 0) {
@@ -835,10 +835,8 @@ hipError_t run(CacheAttn a, hipStream_t s) {
     else if (a.tile_log == 5) k_cache_attn<T, E4M3, HD, 32, 1, kKeyWaves><<<grid, kKeyWaves * kWave, 0, s>>>(a);
     else k_cache_attn<T, E4M3, HD, 32, 4, 1><<<grid, 4 * kWave, 0, s>>>(a);
   }
-  const int64_t tokens = a.splits > 1 ? a.c.rows : 0;
-  for (int64_t u = 0; u < tokens; u += kMostUnits) {
-    a.unit0 = static_cast<uint32_t>(u);
-    const unsigned n = static_cast<unsigned>(std::min(tokens - u, kMostUnits));
+  if (a.splits > 1) {  // fewer than kSplitBlocks tiles: at most 2^18 rows
+    const unsigned n = static_cast<unsigned>(a.c.rows);
     if (a.splits > 32) k_cache_join<T, 1024><<<dim3(n, a.hq), 1024, 0, s>>>(a);
     else k_cache_join<T, kWave><<<dim3(n, (a.hq + 3) / 4), kBlock, 0, s>>>(a);
   }
