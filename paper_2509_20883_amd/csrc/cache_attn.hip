@@ -241,40 +241,45 @@ __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[NS], con
     c = r.cap * kLog2e;
     capped_scores<T>(p, r.scale / r.cap * ks);
   }
-  if (!sloped) {
+  // Distances are taken from the lane's nearest key, `near` away, and that one's term with
+  // the maximum: two large numbers near each other where the key counts at all, so that
+  // their sum is exact (from the row's position at once, a key next to the row after one
+  // a million back was off by their distance's last bit: fp32 rows by 4e-4 of their norm).
+  float near = 0.0f;
+  if (sloped) {
+    const int dist = j - r.pos;
+    const float e = static_cast<float>(min(max(dist, 1 - NS), 0));
+    near = r.slope * static_cast<float>(max(max(dist, 1 - NS - dist), 0));
 #pragma unroll
-    for (int i = 0; i < NS; ++i) p[i] = p[i] * c - st.m;
-  } else {
-    const float dist = static_cast<float>(j - r.pos);
-#pragma unroll
-    for (int i = 0; i < NS; ++i) p[i] = p[i] * c - (r.slope * fabsf(dist + static_cast<float>(i)) + st.m);
+    for (int i = 0; i < NS; ++i) p[i] = p[i] * c - r.slope * fabsf(e + static_cast<float>(i));
+    c = 1.0f;
   }
   if (masked) {
     const int left = r.limit - j;
 #pragma unroll
     for (int i = 0; i < NS; ++i) p[i] = i < left ? p[i] : -INFINITY;
+    c = c == 0.0f ? 0x1p-149f : c;  // a product that is gone in fp32 keeps them out all the same
   }
   float top = p[0];
 #pragma unroll
   for (int i = 1; i < NS; ++i) top = fmaxf(top, p[i]);
-  top = Shape<M>::column_max(top);
+  top = Shape<M>::column_max(top * c - (near + st.m));
   // the running maximum moves only when a score passes it by 2^8
   if (__any(top > st.move)) {
     const bool up = top > st.move;
-    const float by = up ? top : 0.0f;
-    const float alpha = st.move == -INFINITY ? 0.0f : exp2_hw(-by);
-    st.m += by;
+    const float m = up ? st.m + top : st.m;
+    const float alpha = st.move == -INFINITY ? 0.0f : exp2_hw(st.m - m);
+    st.m = m;
     st.move = up ? 8.0f : st.move;
     st.l *= alpha;
 #pragma unroll
     for (int i = 0; i < HD / M; ++i) st.acc[i] *= alpha;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) p[i] -= by;
   }
+  const float past = near + st.m;
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    p[i] = exp2_hw(p[i]);
+    p[i] = exp2_hw(p[i] * c - past);
     sum += p[i];
     if (SCALED) p[i] *= vs;
   }
@@ -283,7 +288,7 @@ __device__ __forceinline__ void soften(AttnState<M, HD>& st, float (&p)[NS], con
 
 // Waves of a SIMD that the registers are kept down for.
 template <typename T, int HD, int M>
-constexpr int kResident = M == 16 ? (sizeof(T) == 4 ? (HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 3) : HD <= 64 ? (sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? 3 : 1;
+constexpr int kResident = M == 16 ? (sizeof(T) == 4 ? (HD <= 64 ? 3 : 2) : HD <= 64 ? 4 : 3) : HD <= 64 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) == 2 ? 3 : 1;
 
 __device__ inline float lane_value(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));

@@ -335,3 +335,83 @@ def test_a_row_sees_its_own_full_page_where_its_list_names_it(dtype, codes):
                                             d ** -0.5, dtype == BF, G)
                 _close(out[i:i + 1, h * G:(h + 1) * G], want, bound, dtype)
                 assert pages is picks or int(w[pos[i]]) == 1
+
+
+# ---------------------------------------------------------------------------
+# slopes: keys next to a row beside keys far from it
+# ---------------------------------------------------------------------------
+
+
+def _sloped(q, k, v, pos, key_pos, weight, slopes, scale, bf16):
+    """One row's attention over its keys, causal, and the bound of cache_reference.attention with the normaliser's error taken as what
+    it is, the mean of the keys' errors by their probabilities (there: the largest of the row's, which a far key's distance sets).
+    Distances are exact up to 2^24, their terms rounded twice, so 8 u of each score's parts stay.  q [hq, d], k, v [nk, d]."""
+    d = q.shape[-1]
+    x = q.double() @ k.transpose(0, 1) * scale
+    es = (6 * d + 16) * ref.U * (q.double().abs() @ k.abs().transpose(0, 1)) * scale
+    dist = (pos - key_pos).abs().double()
+    m = slopes.double()[:, None]
+    x = x - m * dist
+    es = es + 8 * ref.U * (m.abs() * dist + x.abs())
+    x = torch.where((weight > 0) & (key_pos <= pos), x + weight.clamp(min=1).double().log(), -math.inf)
+    P = torch.softmax(x, 1)
+    r = 2.0 ** -8 if bf16 else 0.0
+    e = es + (P * es).sum(1, keepdim=True) + 16 * ref.U
+    out = P @ v
+    return out, (P * (e + r + (2 * k.shape[0] + 128) * ref.U)) @ v.abs() + (r + 4 * ref.U) * out.abs()
+
+
+@pytest.mark.parametrize("dtype,codes", [(F32, "i8"), (F32, "e4m3"), (BF, "i8")])
+@pytest.mark.parametrize("hq,d", [(4, 64), (40, 32)])
+@pytest.mark.parametrize("tail", [0, 1, 9])
+def test_near_keys_beside_far_ones(dtype, codes, hq, d, tail):
+    """Listed pages a million positions back and those next to the row: what the near ones are worth does not depend on how far the
+    others lie, in whatever order the list names them."""
+    P = 64
+    c = _cache(12, 1, 1, d, P, codes, dtype)
+    g = ref.fill(c, 91)
+    n = 16000 * P + tail
+    table = torch.arange(16001, device="cuda").remainder(12).to(torch.int32)[None]
+    slopes = torch.linspace(0.03, 0.9, hq, device="cuda")
+    q = torch.randn(3, hq, d, generator=g, device="cuda").to(dtype)
+    off, lens = _dev([0, 3]), _dev([n])
+    pages = torch.tensor([[0, 1, 700, 8000, 15998, 15999], [15999, 3, 15000, 2, 15998, 1], [5, 15999, 4, 15998, 3, 2]], dtype=torch.int32,
+                         device="cuda")[:, None]
+    out = c.attend(q, off, lens, table, pages=pages, slopes=slopes)
+    vals, scales = ref.pages_of(c)
+    for i in range(3):
+        ids = table[0, pages[i, 0].long()].long()
+        kv = (vals[ids, 0] * scales[ids, 0][..., None, None]).transpose(0, 1).reshape(2, -1, d)
+        key_pos = (pages[i, 0].long()[:, None] * P + torch.arange(P, device="cuda")).flatten()
+        if tail:
+            kv = torch.cat([kv, c.open[0, 0, 0, :, :tail].double()], 1)
+            key_pos = torch.cat([key_pos, torch.arange(n - tail, n, device="cuda")])
+        want, bound = _sloped(q[i], kv[0], kv[1], n - 3 + i, key_pos, torch.ones_like(key_pos), slopes, d ** -0.5, dtype == BF)
+        _close(out[i], want, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype,codes", [(F32, "i8"), (BF, "e4m3")])
+@pytest.mark.parametrize("rows", [1, 8, 60])
+def test_steep_slopes_over_a_whole_history(dtype, codes, rows):
+    """A step of keys after the other, each far above the one before: rows of every tile, one and several parts."""
+    hq, d, P, n = 4, 64, 32, 9000
+    c = _cache(30, 1, 1, d, P, codes, dtype)
+    g = ref.fill(c, 92)
+    table = torch.arange(282, device="cuda").remainder(30).to(torch.int32)[None]
+    slopes = torch.tensor([0.01, 0.7, 8.0, -0.004], device="cuda")
+    q = torch.randn(rows, hq, d, generator=g, device="cuda").to(dtype)
+    out = c.attend(q, _dev([0, rows]), _dev([n]), table, slopes=slopes)
+    k, v, there = ref.tokens_of(c, table, [n], [0])[0]
+    key_pos = torch.arange(n, device="cuda")
+    for i in range(rows):
+        want, bound = _sloped(q[i], k[:, 0], v[:, 0], n - rows + i, key_pos, there.long(), slopes, d ** -0.5, dtype == BF)
+        _close(out[i], want, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale,cap", [(1e-300, 0.0), (1e-300, 5.0), (1e-42, 0.0)])
+def test_scales_that_vanish_in_fp32_keep_the_mask(dtype, scale, cap):
+    """Every key that a row sees counts alike, and those behind it not at all."""
+    for new in ([3, 2], [40, 9]):
+        base._attend_case(4, 1, 64, 64, "i8", dtype, [700, 33], new, True, cap, scale=scale, seed=93)
+        base._attend_case(4, 1, 64, 64, "e4m3", dtype, [700, 33], new, True, cap, True, scale=scale, count=3, seed=94)
