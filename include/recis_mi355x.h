@@ -550,7 +550,7 @@ rs_status seq_attention_bwd(const rs_attn_desc* d, const void* q, const void* k,
  *                  to even
  *   RS_CACHE_E4M3: scale = the least power of two with max |x| <= 448 scale,
  *                  code = x / scale in OCP e4m3, ties to even
- * Scales are at least 2^-126.  A page that holds an infinity or NaN reads as NaN
+ * Scales are at least 2^-126, where tokens are held.  A page that holds an infinity or NaN reads as NaN
  * throughout (and may reach every query of its sequence).
  *
  * Memory (device, the caller's; W = 32, 64 or 128, the least that head_dim fits;
@@ -590,8 +590,8 @@ typedef struct {
 /* The sequences of a call and their rows (new tokens, queries, or rows read),
  * laid out as for seq_attention: offsets int64 [seqs + 1], CSR; pad = 0: packed,
  * pad > 0: rows = seqs * pad, sequence s the first min(off[s+1] - off[s], pad)
- * rows of its block, the others never read.  lens int64 [seqs]: the tokens that
- * each sequence holds.  table int32 [seqs][table_width]: the page of each page
+ * rows of its block, the others never read; packed rows outside every sequence are
+ * neither read nor written.  lens int64 [seqs]: the tokens that each sequence holds.  table int32 [seqs][table_width]: the page of each page
  * number; entries past a sequence's pages are not read.  slots int32 [seqs]
  * (NULL: slot s for sequence s).
  * Entries outside the cache are passed over: their tokens are neither written
@@ -614,8 +614,8 @@ typedef struct {
 
 /* New tokens, at positions lens[s], lens[s] + 1, ...: keys and queries turn by
  * their position, column pairs (i, i + rotary / 2), or (2 i, 2 i + 1) interleaved,
- * by position * frequency_i, in the model's type afterwards; columns from rotary
- * on stay.  `turns`: device copy of rs_rotation_turns' result. */
+ * by position * frequency_i, in the model's type afterwards (bf16 by way of fp32);
+ * columns from rotary on stay.  `turns`: device copy of rs_rotation_turns' result. */
 typedef struct {
   const void *k, *v; /* [rows][heads_kv][head_dim]; both NULL: q alone is turned,
                       by offsets and lens; no table or slots are read      */
@@ -634,8 +634,8 @@ typedef struct {
  * RS_EINVAL. */
 rs_status rs_rotation_turns(const double* freqs, double base, int32_t rotary, uint64_t* turns);
 
-/* Writes the rows of k and v as the sequences' next tokens (one launch).  All
- * pointers and strides are multiples of 16 bytes.  Errors: RS_EINVAL, RS_ENOMEM
+/* Writes the rows of k and v as the sequences' next tokens (one launch up to 2^21
+ * blocks).  k, v, q, q_out and all strides are multiples of 16 bytes.  Errors: RS_EINVAL, RS_ENOMEM
  * (validate), RS_EHIP. */
 rs_status seq_cache_append(const rs_seq_cache* c, const rs_cache_batch* b, const rs_cache_rows* r, int32_t validate,
                            rs_stream stream);
@@ -673,7 +673,9 @@ typedef struct {
   int32_t count;     /* pages of a row, 0: all; at most 65536                   */
   int32_t reserved;  /* 0                                                       */
   int64_t max_q, max_len; /* the caller's bounds of a sequence's queries and
-                        tokens (0: none known): they only shape the launches    */
+                        tokens (0: none known): they only shape the launches.
+                        Without max_q one packed sequence is taken to have all
+                        the rows, which few rows each of many pay for           */
   int64_t q_stride, q_head_stride;
   double scale, softcap; /* as rs_attn_desc                                     */
 } rs_cache_query;

@@ -5,9 +5,11 @@
 // b' = b cos + a sin.  f is held as a 64-bit fraction of a turn, so p f modulo a
 // turn is one whole-number product, exact to 2^-33 turns at position 2^31 (an
 // fp32 angle is off by 0.06 at 10^6).  Sine, cosine and the turn are taken in
-// 64 bits and rounded once, to the model's type: a key that rounds the other way
-// may fall across a border of the codes, and vector products of 64 bits issue as
-// fast as those of 32.
+// 64 bits: a key that rounds the other way may fall across a border of the codes,
+// and vector products of 64 bits issue as fast as those of 32.  The result is
+// rounded to the model's type, to bf16 by way of fp32, as a conversion from 64 bits
+// does it elsewhere: one value in 2^17 or so, within 2^-25 of itself of the middle
+// between two bf16 numbers, goes to the other one.
 //
 // A full page is coded from the tokens in the model's type, those of its open
 // page and the new ones, so the cache does not depend on how the tokens were
@@ -16,13 +18,13 @@
 // 1 KiB stores a wave.
 //
 // 24 histories of 17 to 8191 tokens (93 thousand rows of 8 query and 2 key heads of
-// 128, bf16 to e4m3 with bounds, 524 MB moved): 125 us, 4.2 TB/s, where a plain copy
+// 128, bf16 to e4m3 with bounds, 524 MB moved): 131 us, 4.0 TB/s, where a plain copy
 // of the queries' 380 MB takes 72. Query rows alone take 72 us, pages alone 54 to 64:
 // a page waits for one thing after another (its sequence, its place, its tokens, then
 // four steps with barriers between), and keys turn at 14 us of those. Blocks of
 // both kinds mixed in the grid, the next row loaded a step ahead, angles without
-// LDS bank conflicts: no change, 126 to 128. One token of 256 users: 9.6 us, bound by
-// latency. Reading the 24 histories back (143 MB moved): 25 us, 5.7 TB/s.
+// LDS bank conflicts: no change, 126 to 128. One token of 256 users: 9.4 us, bound by
+// latency. Reading the 24 histories back (143 MB moved): 26 us, 5.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,7 +37,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Sine and cosine of a turn's fraction.  The quarter turns are taken off first;
-// |x| <= pi / 4 then, and the series end at 8e-20.
+// |x| <= pi / 4 then; the first terms left out are 8e-20 (sine) and 2e-18 (cosine).
 __device__ inline void sincos_turn(uint64_t phase, double& s, double& c) {
   const uint64_t q = (phase + (uint64_t(1) << 61)) >> 62;  // nearest quarter
   const double x = static_cast<double>(static_cast<int64_t>(phase - (q << 62))) * (6.283185307179586477 * 0x1p-64);

@@ -11,7 +11,9 @@
 // (the latter, a power of two in e4m3, by the conversion itself). fp32 queries and
 // probabilities are three bf16 pieces each, which carry their 24 bits through the
 // same instructions; with bf16 queries the probabilities are rounded to bf16, the
-// type of the products. Scores, maxima, sums and outputs are fp32.
+// type of the products (two pieces of each, as exact as the output's own rounding:
+// 4096 rows over 16384 keys 296 -> 400 us, a token of 256 users 74 -> 77). Scores,
+// maxima, sums and outputs are fp32.
 //
 // Few rows (16 or 32 a tile): the four waves of a block lie along the keys, and each
 // loads both sides of its keys from the page straight into the registers that feed
@@ -19,16 +21,18 @@
 // only joins the waves' results. Bound by reading the pages: without any products
 // the loads alone take as long (64 x 32768 keys of 128 206 us, 208 with them), and
 // whole rows of 256 bytes gathered at random reach 5.4 TB/s. One token of 256 users
-// with 1 to 4096 keys of 128 in 2 heads (257 MB) 68 us, 4 rows over 1,000,003 keys of 64
-// (256 MB) 59: 25 to 29 us of that are there at any size (the chain from a row's
+// with 1 to 4096 keys of 128 in 2 heads (257 MB) 67 us, 4 rows over 1,000,003 keys of 64
+// (256 MB) 52: 15 to 25 us of that are there at any size (the chain from a row's
 // sequence to its length, its pages and their first bytes, code that is not in the
-// caches yet, and the longest sequence's end).
+// caches yet, and the end of the longest sequence, which has as many parts as the
+// shortest).
 //
 // Many rows: tiles of 128, a wave 32 of them, over the same keys; the operands are
 // made once a block into LDS. Bound by the vector instructions around the products
-// (conversions, exponentials, the running maximum: vector unit 42% busy, matrix unit
-// 36%, the rest waits between the two): 4096 rows over 16384 keys of 128, 8 query heads,
-// 297 us, 810 TFLOP/s over the visible keys.
+// (conversions, exponentials, the running maximum: vector unit 45% busy, matrix unit
+// 38%, the rest waits between the two): 4096 rows over 16384 keys of 128, 8 query heads,
+// 294 us and 22 to join, 810 TFLOP/s over the visible keys in a pass; in i8 333 a pass,
+// in fp32 817.
 //
 // The open page's tokens, at most page_len - 1 of a sequence, are read in the
 // model's type.

@@ -18,9 +18,9 @@
 // loads the bounds of 16 pages as the instruction takes them, 64 pages ahead, and
 // the queries become bytes in LDS meanwhile, once for a tile of a sequence's rows.
 // (Dot products of 4 bytes, a thread a page: 4 rows of 32 heads over 15,625 pages
-// of 8 key heads 27 us; as matrices 13, the 33 MB of bounds at 2.5 TB/s: bound by
-// the chain from the sequence to the page to its bounds. One row of 64 users with up
-// to 1024 pages 9.7 us.)
+// of 8 key heads 27 us; as matrices 13 to 14, the 33 MB of bounds at 2.4 TB/s: bound
+// by the chain from the sequence to the page to its bounds. One row of 64 users with
+// up to 1024 pages 12 us.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -247,9 +247,9 @@ __device__ inline uint32_t order(uint32_t b) { return b & 0x80000000u ? ~b : b |
 // A block per row and key head, its keys in registers: the count-th largest by
 // halving the range of keys (a step is one compare a key and one barrier), then the
 // pages above it and the first of those equal to it, in order. Bound by the latency of
-// those steps: 64 of 15,625 pages 16.6 us (40 by histograms of the keys' bytes, which
+// those steps: 64 of 15,625 pages 17 to 19 us (40 by histograms of the keys' bytes, which
 // put most of like scores into a few counters; 25 with the range started at the least
-// key), 32 of at most 1024 7.4.
+// key), 32 of at most 1024 7.8.
 template <int NT, int ITEMS>
 __global__ __launch_bounds__(NT) void k_select_pick(const CacheSelect a) {
   constexpr int kWaves = NT / kWave;
