@@ -614,8 +614,9 @@ typedef struct {
 
 /* New tokens, at positions lens[s], lens[s] + 1, ...: keys and queries turn by
  * their position, column pairs (i, i + rotary / 2), or (2 i, 2 i + 1) interleaved,
- * by position * frequency_i, in the model's type afterwards (bf16 by way of fp32);
- * columns from rotary on stay.  `turns`: device copy of rs_rotation_turns' result. */
+ * by position * frequency_i, in the model's type afterwards (bf16 by way of fp32), the
+ * same to the last bit in every call and for keys as for queries; columns from rotary
+ * on stay.  `turns`: device copy of rs_rotation_turns' result. */
 typedef struct {
   const void *k, *v; /* [rows][heads_kv][head_dim]; both NULL: q alone is turned,
                       by offsets and lens; no table or slots are read      */

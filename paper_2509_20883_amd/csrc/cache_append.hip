@@ -76,21 +76,54 @@ __device__ inline Angle angle_of(uint64_t phase) {
 // The angle further on by another: off by 2^-53, where a series takes 15 times as
 // many instructions.
 __device__ inline void advance(Angle& g, const Angle& by) {
-  const double s = g.s * by.c + g.c * by.s;
-  g.c = g.c * by.c - g.s * by.s;
+  const double s = fma(g.s, by.c, g.c * by.s);
+  g.c = fma(g.c, by.c, -(g.s * by.s));
   g.s = s;
 }
+// The angles of one frequency at one position after another. A series every 16 positions,
+// from there by fours, from a multiple of four by ones: an angle is a function of its
+// position to the last bit, not of where a call, a tile or a thread began. (Which product
+// is fused is written out, above and below: left to the compiler it is another one in
+// another place.)
+struct Turning {
+  uint64_t turns;
+  int64_t pos;
+  Angle one, four, group, g;
+  __device__ inline explicit Turning(uint64_t t) : turns(t) {
+    one = four = angle_of(t);
+    advance(four, one);
+    const Angle two = four;
+    advance(four, two);
+  }
+  __device__ inline void start(int64_t p) {
+    pos = p;
+    group = angle_of(static_cast<uint64_t>(p & ~int64_t(15)) * turns);
+    for (int i = static_cast<int>(p >> 2 & 3); i > 0; --i) advance(group, four);
+    g = group;
+    for (int i = static_cast<int>(p & 3); i > 0; --i) advance(g, one);
+  }
+  // to the next position, not a multiple of 16
+  __device__ inline void next() {
+    ++pos;
+    if (pos & 3) {
+      advance(g, one);
+    } else {
+      advance(group, four);
+      g = group;
+    }
+  }
+};
 // A pair of columns turned, in the model's type.
 __device__ inline void turn(const Angle& g, uint16_t& a, uint16_t& b) {
   const double x = bf16_to_f32(a), y = bf16_to_f32(b);
-  const uint32_t w = pack_bf16(static_cast<float>(x * g.c - y * g.s), static_cast<float>(y * g.c + x * g.s));
+  const uint32_t w = pack_bf16(static_cast<float>(fma(x, g.c, -(y * g.s))), static_cast<float>(fma(y, g.c, x * g.s)));
   a = static_cast<uint16_t>(w);
   b = static_cast<uint16_t>(w >> 16);
 }
 __device__ inline void turn(const Angle& g, float& a, float& b) {
   const double x = a, y = b;
-  a = static_cast<float>(x * g.c - y * g.s);
-  b = static_cast<float>(y * g.c + x * g.s);
+  a = static_cast<float>(fma(x, g.c, -(y * g.s)));
+  b = static_cast<float>(fma(y, g.c, x * g.s));
 }
 
 __device__ inline float to_f32(uint16_t x) { return bf16_to_f32(x); }
@@ -189,17 +222,20 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
   }
   __syncthreads();
   if (side == 0 && half_rot > 0) {
-    const int f = threadIdx.x & (pw - 1), per = NT / pw;
-    if (f < half_rot) {
-      const uint64_t step = a.turns[f];
-      int t = max(t0, old) + threadIdx.x / pw;
-      if (t < last) {
-        Angle g = angle_of(static_cast<uint64_t>(first + t) * step);
-        const Angle by = angle_of(static_cast<uint64_t>(per) * step);
-        for (; t < last; t += per) {
-          T* x = reinterpret_cast<T*>(lds + t * stride) + ca * f;
-          turn(g, x[0], x[cb]);
-          advance(g, by);
+    // a thread turns a run of tokens, of at most as many as leave every thread one
+    const int f = threadIdx.x & (pw - 1), per = NT / pw, run = min(16, max(1, P / per));
+    int t = (old & ~(run - 1)) + threadIdx.x / pw * run;
+    if (f < half_rot && t < last) {
+      Turning turning(a.turns[f]);
+      for (; t < last; t += per * run) {
+        const int from = max(t, old), to = min(t + run, last);
+        if (from >= to) continue;
+        turning.start(first + from);
+#pragma unroll 1
+        for (int i = from; i < to; ++i) {
+          if (i > from) turning.next();
+          T* x = reinterpret_cast<T*>(lds + i * stride) + ca * f;
+          turn(turning.g, x[0], x[cb]);
         }
       }
     }
@@ -325,9 +361,10 @@ struct Eight {
   }
 };
 
-// Query rows: a wave takes four of a sequence, one after another, an angle a lane
-// and by LDS to every head, then eight pairs of a head a lane where the columns allow
-// whole 16-byte loads.
+// Query rows: a wave takes four of a sequence. A lane makes a pair's angles in all four,
+// which go by LDS to every head (kept in registers beside the rows' columns they cost
+// waves a SIMD: 24 histories 187 us a pass, so 160); then row after row, eight pairs of a
+// head a lane where the columns allow whole 16-byte loads.
 constexpr int kTurnRows = 4;
 template <typename T, int NT>
 __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64_t b) {
@@ -349,12 +386,18 @@ __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64
   if (tile < 0 || first >= all) return;
   const int64_t base = max(c.lens[s], int64_t(0));
   const RotPairs rp(a);
-  Angle* angles = reinterpret_cast<Angle*>(lds) + wave * kWave;  // rotary / 2 is at most 64
-  Angle g = {0.0, 1.0}, by = g;
+  Angle* angles = reinterpret_cast<Angle*>(lds) + wave * kTurnRows * kWave;  // rotary / 2 is at most 64
   if (lane < rp.count) {
-    g = angle_of(static_cast<uint64_t>(base + first) * a.turns[lane]);
-    by = angle_of(a.turns[lane]);
+    Turning turning(a.turns[lane]);
+#pragma unroll 1
+    for (int i = 0; i < kTurnRows; ++i) {
+      const int64_t p = base + first + i;
+      if (i == 0 || (p & 15) == 0) turning.start(p);
+      else turning.next();
+      angles[i * kWave + lane] = turning.g;
+    }
   }
+  __builtin_amdgcn_wave_barrier();
   const uint32_t chunks = rp.count / 8, rest = (d - a.rotary) / 8, per = chunks + rest;
   for (int64_t token = first; token < min(all, first + kTurnRows); ++token) {
     const int64_t row = span.start + token;
@@ -364,9 +407,7 @@ __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64
       continue;
     }
     const T* q = static_cast<const T*>(a.q.p) + row * a.q.row;
-    angles[lane] = g;
-    advance(g, by);
-    __builtin_amdgcn_wave_barrier();
+    const Angle* turned = angles + (token - first) * kWave;
     if (rp.count % 8 == 0) {
       for (uint32_t i = lane; i < per * a.hq; i += kWave) {
         const uint32_t h = i / per, k = i - h * per;
@@ -383,7 +424,7 @@ __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64
         y.load(from + cb);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const Angle at = angles[f + e];
+          const Angle at = turned[f + e];
           if (a.next) {
             Eight<T>& z = e < 4 ? x : y;
             T v = z.get(2 * (e & 3)), w = z.get(2 * (e & 3) + 1);
@@ -405,14 +446,13 @@ __device__ __forceinline__ void turn_rows(const CacheAppend& a, char* lds, int64
       if (f < rp.count)
         for (int h = lane / rp.lanes; h < a.hq; h += step) {
           T x = q[h * a.q.head + rp.step * f], y = q[h * a.q.head + rp.step * f + rp.apart];
-          turn(angles[f], x, y);
+          turn(turned[f], x, y);
           out[h * d + rp.step * f] = x;
           out[h * d + rp.step * f + rp.apart] = y;
         }
       for (int h = 0; h < a.hq && a.rotary < d; ++h)
         for (int i = a.rotary + lane; i < d; i += kWave) out[h * d + i] = q[h * a.q.head + i];
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -592,7 +632,7 @@ hipError_t append(CacheAppend a, int bytes, hipStream_t s) {
 
 template <typename T, bool E4M3>
 hipError_t append_type(const CacheAppend& a, hipStream_t s) {
-  const int angles = kBlock * static_cast<int>(sizeof(Angle)), page = lds_stride<T>(a.c.d) << a.c.plog;
+  const int angles = kTurnRows * kBlock * static_cast<int>(sizeof(Angle)), page = lds_stride<T>(a.c.d) << a.c.plog;
   const bool large = page + kOwnLds<256> > kPlainLds;
   const int bytes = std::max(page, large ? 4 * angles : angles);
   // a large page fills a CU's LDS by itself: more waves on it then (else 256 threads: 24

@@ -415,3 +415,39 @@ def test_scales_that_vanish_in_fp32_keep_the_mask(dtype, scale, cap):
     for new in ([3, 2], [40, 9]):
         base._attend_case(4, 1, 64, 64, "i8", dtype, [700, 33], new, True, cap, scale=scale, seed=93)
         base._attend_case(4, 1, 64, 64, "e4m3", dtype, [700, 33], new, True, cap, True, scale=scale, count=3, seed=94)
+
+
+# ---------------------------------------------------------------------------
+# rotation is a function of the position
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("d,rotary,interleaved,page", [(128, 128, False, 256), (64, 48, True, 64), (16, 2, False, 32), (32, 32, False, 128)])
+@pytest.mark.parametrize("held", [0, 3, 1000003 * 256])
+def test_turned_rows_do_not_depend_on_the_cuts(d, rotary, interleaved, page, held):
+    """Pairs that turn to nearly nothing show the last bit of their angle: keys and queries are the same however calls cut them, and
+    the same as each other."""
+    g = torch.Generator(device="cuda").manual_seed(95)
+    n, h = page - 1 - held % page, rotary // 2
+    freqs = [1.0 + 0.37 * i for i in range(h)]
+    pos = held + torch.arange(n, device="cuda")
+    w = pos.double()[:, None] * torch.tensor(freqs, dtype=torch.float64, device="cuda")
+    x = torch.randn(n, 2, d, generator=g, device="cuda")
+    a, b = (slice(0, rotary, 2), slice(1, rotary, 2)) if interleaved else (slice(0, h), slice(h, rotary))
+    x[:, 0, a], x[:, 0, b] = torch.sin(w).float(), torch.cos(w).float()
+    x[:, 1, a], x[:, 1, b] = torch.cos(w).float(), -torch.sin(w).float()
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    at = held // page % 2, held % page
+    got = []
+    for cuts in ([n], [1] * n, [5, 1, 2, n - 8], [n // 2, n - n // 2]):
+        c = R.SeqCache(1, 1, 2, d, page=page, dtype=F32, rotary=rotary, freqs=freqs, interleaved=interleaved)
+        lens, done, rows = _dev([held]), 0, []
+        for m in cuts:
+            part = x[done:done + m]
+            lens, q = c.append(part, part, _dev([0, m]), lens, table, q=part)
+            rows.append(q)
+            done += m
+        got.append((c.open[0, at[0], :, 0, at[1]:at[1] + n].transpose(0, 1), torch.cat(rows)))
+    for k, q in got:
+        assert torch.equal(k, got[0][0]) and torch.equal(q, got[0][1])
+    assert torch.equal(got[0][0], got[0][1])
