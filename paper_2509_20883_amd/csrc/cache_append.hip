@@ -129,12 +129,13 @@ __device__ inline void turn(const Angle& g, float& a, float& b) {
 __device__ inline float to_f32(uint16_t x) { return bf16_to_f32(x); }
 __device__ inline float to_f32(float x) { return x; }
 
-// rne(x / s) exactly: the product by the reciprocal, then the remainder decides.
+// rne(x / s) exactly: the product by the reciprocal, then the remainder decides (twice
+// it against s: half of the least scales is not a number).
 __device__ inline int code_i8(float x, float s, float inv) {
   float n = rintf(x * inv);
-  const float e = fmaf(-n, s, x), half = 0.5f * s;
-  if (fabsf(e) > half) n += copysignf(1.0f, e);
-  else if (fabsf(e) == half && (static_cast<int>(n) & 1)) n += copysignf(1.0f, e);
+  const float e = 2.0f * fmaf(-n, s, x);
+  if (fabsf(e) > s) n += copysignf(1.0f, e);
+  else if (fabsf(e) == s && (static_cast<int>(n) & 1)) n += copysignf(1.0f, e);
   return static_cast<int>(fminf(fmaxf(n, -127.0f), 127.0f));
 }
 

@@ -451,3 +451,33 @@ def test_turned_rows_do_not_depend_on_the_cuts(d, rotary, interleaved, page, hel
     for k, q in got:
         assert torch.equal(k, got[0][0]) and torch.equal(q, got[0][1])
     assert torch.equal(got[0][0], got[0][1])
+
+
+# ---------------------------------------------------------------------------
+# codes and bounds at the ends of fp32
+# ---------------------------------------------------------------------------
+
+
+def _written(x, codes, dtype):
+    """Pages of x [pages, P, d] written and looked at: codes, scales, bounds."""
+    n, P, d = x.shape
+    c = _cache(n, n, 1, d, P, codes, dtype, bounds=True)
+    table = torch.arange(n, dtype=torch.int32, device="cuda")[:, None]
+    k = x.view(n * P, 1, d)
+    c.append(k, k, ref.offsets([P] * n), _dev([0] * n), table)
+    tokens = [torch.stack([x[i][:, None], x[i][:, None]], 2) for i in range(n)]
+    base._check_pages(c, table, tokens, None, None, codes, [(i, 0) for i in range(n)])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_codes_next_to_ties_under_the_least_scales(dtype):
+    """Scales from 2^-126 to 2^-120, whose halves may not be numbers: codes are x / scale to the nearest, ties to even."""
+    g = torch.Generator(device="cuda").manual_seed(96)
+    x = torch.randn(64, 32, 64, generator=g, device="cuda", dtype=torch.float64) * 2.0 ** -121
+    x *= 2.0 ** torch.arange(-4, 4, dtype=torch.float64, device="cuda").repeat(8)[:, None, None]
+    x = x.to(dtype)
+    s = (x.double().abs().amax((1, 2)) / 127).float().clamp(min=2.0 ** -126).double()
+    half = (torch.randint(-100, 100, (64, 8, 64), generator=g, device="cuda") + 0.5) * s[:, None, None]  # next to ties
+    x[:, 8:16] = half.to(dtype)
+    x[:, 8:16] = torch.where(x[:, 8:16].abs() <= 126 * s[:, None, None], x[:, 8:16], 0)
+    _written(x, "i8", dtype)
