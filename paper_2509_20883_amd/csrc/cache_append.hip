@@ -332,8 +332,11 @@ __device__ __forceinline__ void append_page(const CacheAppend& a, char* lds, uin
       }
       int8_t* to = c.bounds + at * 2 * W + col;
       const bool none = bad || col >= d;
-      to[0] = none ? 0 : static_cast<int8_t>(ceilf(high * unit_inv));
-      to[W] = none ? 0 : static_cast<int8_t>(floorf(low * unit_inv));
+      // outward, also where the product is too small for a number
+      const float up = high > 0.0f ? fmaxf(ceilf(high * unit_inv), 1.0f) : ceilf(high * unit_inv);
+      const float down = low < 0.0f ? fminf(floorf(low * unit_inv), -1.0f) : floorf(low * unit_inv);
+      to[0] = none ? 0 : static_cast<int8_t>(up);
+      to[W] = none ? 0 : static_cast<int8_t>(down);
       if (col == 0) c.units[at] = bad ? __uint_as_float(0x7FC00000u) : exp2_int(k);
     }
   }

@@ -481,3 +481,16 @@ def test_codes_next_to_ties_under_the_least_scales(dtype):
     x[:, 8:16] = half.to(dtype)
     x[:, 8:16] = torch.where(x[:, 8:16].abs() <= 126 * s[:, None, None], x[:, 8:16], 0)
     _written(x, "i8", dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_bounds_of_columns_far_below_the_largest(dtype):
+    """A column whose numbers vanish beside the page's largest is bounded from outside all the same."""
+    x = torch.zeros(5, 32, 16, device="cuda")
+    x[:, 0, 0] = torch.tensor([3e38, 2e6, 1.0, 1e30, 2.0 ** -20], device="cuda")
+    for i, v in enumerate((1e-38, 1e-41, 1e-20, 2.0 ** -133, 1e-10)):
+        x[:, :, 2 + 2 * i] = v
+        x[:, :, 3 + 2 * i] = -v
+    x[:, 5, 13], x[:, 6, 13] = 1e-38, -1e-30
+    _written(x.to(dtype), "i8", dtype)
+    _written(x.to(dtype), "e4m3", dtype)
