@@ -664,7 +664,8 @@ rs_status seq_cache_read(const rs_seq_cache* c, const rs_cache_batch* b, const i
  * does not overlap q.  Scores, statistics and sums are fp32; bf16 probabilities
  * are rounded as operands of the matrix instructions, fp32 ones keep 24 bits.
  * Products of q with the keys' codes, and sums of 2^8 |v| over the keys, have to
- * stay in fp32: past it a row may be infinite or NaN.
+ * stay in fp32: past it a row may be infinite or NaN.  Queries, keys or values all
+ * below 2^-100 lose digits.
  * Workspace: seq_cache_attention_workspace_bytes(...), 256-byte aligned, free for
  * the next call once this one has completed in stream order; 0 for arguments the
  * call refuses, or where none is needed. */

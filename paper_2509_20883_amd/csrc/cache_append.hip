@@ -18,13 +18,13 @@
 // 1 KiB stores a wave.
 //
 // 24 histories of 17 to 8191 tokens (93 thousand rows of 8 query and 2 key heads of
-// 128, bf16 to e4m3 with bounds, 524 MB moved): 131 us, 4.0 TB/s, where a plain copy
+// 128, bf16 to e4m3 with bounds, 524 MB moved): 133 us, 3.9 TB/s, where a plain copy
 // of the queries' 380 MB takes 72. Query rows alone take 72 us, pages alone 54 to 64:
 // a page waits for one thing after another (its sequence, its place, its tokens, then
 // four steps with barriers between), and keys turn at 14 us of those. Blocks of
 // both kinds mixed in the grid, the next row loaded a step ahead, angles without
-// LDS bank conflicts: no change, 126 to 128. One token of 256 users: 9.4 us, bound by
-// latency. Reading the 24 histories back (143 MB moved): 26 us, 5.5 TB/s.
+// LDS bank conflicts: no change (126 to 128 where 125 was). One token of 256 users: 9.9 us, bound by
+// latency. Reading the 24 histories back (143 MB moved): 25 us, 5.7 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
